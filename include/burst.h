@@ -291,6 +291,73 @@ int burst_local_bwd_materialized(const void* Q, const void* K_chunk, const void*
                                  void* workspace, size_t workspace_bytes,
                                  const burst_params* p, void* stream);
 
+/* Positions beside the attention, and a cache of keys and values in pages (not in the paper: the rotation that models apply to Q and
+ * K before the walks above, with the positions that a ring's slices have; and what serves the sequence afterwards, token by
+ * token).  The arrays of numbers that these calls read on the device (starts, lengths, table, positions, offsets) are aligned to
+ * their element type, and no value in them leads to an access outside the tensors. */
+
+/* Rotation of pairs of columns by an angle of 2 pi x position x turns[pair]: a pair (a, b) becomes
+ * (a cos - b sin, b cos + a sin) x amplitude.  The angle is computed in 64 bits from the position, cos and sin to 24 bits. */
+typedef struct burst_rotary {
+  const double* turns;  /* DEVICE [dims / 2]: turns per position of every pair */
+  int32_t dims;         /* rotated columns, even, 2 .. d; the columns from dims on are copied */
+  int32_t interleaved;  /* 0: columns i and i + dims / 2 are a pair; 1: columns 2 i and 2 i + 1 */
+  float   amplitude;    /* finite, normally 1 */
+  int32_t inverse;      /* 1: by the negative angle, which takes the gradient of the output to that of the input */
+} burst_rotary;
+/* One tensor [B, heads, rows, d] and its rotated copy. */
+typedef struct burst_rows {
+  const void* x; void* y;            /* y: written; x itself (then with the same strides) or memory that x does not share */
+  const int64_t* positions;          /* DEVICE: row n of batch entry b is at offset + positions[b * positions_stride + n]; NULL: offset + n */
+  int64_t positions_stride, offset;
+  int64_t x_strides[3], y_strides[3];/* element strides {batch, head, row}; all zero = contiguous */
+  int32_t B, heads, rows;            /* >= 0 */
+  int32_t reserved;                  /* 0 */
+} burst_rows;
+/* Rotates n tensors (queries and the chunks' keys of a walk) of head dimension d, 2 <= d <= 128, and type `dtype`.  Rows may start anywhere
+ * (elements aligned to their own size); rows and column pairs on 16-byte boundaries are read and written 16 bytes at a time. */
+int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d, int dtype, void* stream);
+
+/* The new tokens of several sequences and the pages of their caches.  New tokens lie packed, sequence after sequence:
+ * sequence s has rows starts[s] .. starts[s + 1] - 1 of the token tensors, which are indexed [row, head, d].  lengths[s] counts
+ * the tokens of the sequence, the new ones among them: new token t of n is at position lengths[s] - n + t, and position p
+ * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to width * page and to >= 0, starts to 0 .. rows
+ * and to ascending order; a page that is not in 0 .. pages - 1 holds no keys. */
+typedef struct burst_paged_params {
+  int32_t sequences, rows;           /* >= 0, < 2^30; rows: of the token tensors, those behind the last sequence among them */
+  int32_t H, kv_heads, d, dtype;     /* H a multiple of kv_heads; d a multiple of 8 (bf16) or 4 (fp32), at most 128 */
+  int32_t pages, page, width;        /* pages; rows of a page: a power of two, 16 or more; pages of a table row; width * page < 2^30 */
+  int32_t max_new;                   /* most new tokens of any sequence as far as the caller knows it, 0 = not known: chooses kernels only */
+  int32_t causal;                    /* burst_paged_fwd: 0 = every key of the sequence is visible, 1 = those up to the token's position */
+  int32_t out_f32;                   /* burst_paged_fwd: 1 = O is fp32 whatever the dtype */
+  float   scale;                     /* burst_paged_fwd: as in burst_params */
+  int32_t reserved;                  /* 0 */
+  int64_t window;                    /* burst_paged_fwd: as in burst_params */
+  const int32_t* starts; const int32_t* lengths; const int32_t* table;   /* DEVICE [sequences + 1], [sequences], [sequences][width] */
+  int64_t table_stride;              /* entries from one sequence's pages to the next's; 0 = width */
+  int64_t page_strides[3];           /* elements {page, head, row} of K_pages and V_pages; all zero = dense [pages, kv_heads, page, d] */
+  int64_t q_strides[2], kv_strides[2], o_strides[2];   /* elements {row, head} of Q; of K and V (new tokens); of O or Q_out; both zero = dense.
+                                      * Strides of 16 bytes' multiples (burst_cache_append: any), none negative */
+} burst_paged_params;
+/* Writes the new tokens' keys and values (K, V [rows, kv_heads, d]) to their places in K_pages and V_pages, the keys rotated by their
+ * positions + offsets[s] (int64 DEVICE [sequences], NULL: 0; what the ring keeps before this device's share).  r = NULL: nothing is rotated.
+ * Q, if not NULL: the queries [rows, H, d] are rotated likewise to Q_out.  Tokens at positions below 0 or in pages that are none are left
+ * out (their queries are rotated if they have a position), rows of Q_out behind the last sequence left as they were.  One launch.
+ * Pages that share a place, by equal table entries of two sequences say, must not both get a new token there. */
+int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_pages, const void* Q, void* Q_out,
+                       const int64_t* offsets, const burst_rotary* r, const burst_paged_params* p, void* stream);
+/* Attention of the new tokens over their sequences' pages: O [rows, H, d] of `dtype` (fp32 with out_f32) and lse [rows, H] fp32,
+ * dense.  Tokens that see no key get O = 0 and lse = -inf; rows behind the last sequence are left as they were.  (O as fp32, lse, 1) is
+ * a state that burst_merge_state takes: sequences whose cache is spread over a ring are put together so.
+ * Hidden keys have no effect whatever they hold.  The order of the sums depends on the sizes, lengths and max_new of the call, all sequences'
+ * among them; a call repeated gives the same bits.  bf16 probabilities are rounded to bf16 before the second product.
+ * workspace: burst_paged_workspace_bytes(p) bytes of device memory, 16-byte aligned, contents undefined before and after; two
+ * calls that may run at the same time need one each. */
+int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,
+                    size_t workspace_bytes, const burst_paged_params* p, void* stream);
+/* Does not depend on what the arrays on the device hold; 0 for invalid parameters.  Host logic, no device call. */
+size_t burst_paged_workspace_bytes(const burst_paged_params* p);
+
 /* For tests and tuning (no counterpart in the paper): which of the two kernel families serves
  * bf16, d = 128 calls.  0 = chosen per call (the default): forward and dQ from how well the call's
  * workgroups fill the chip and from the flags' block edge, dK/dV always hand-scheduled, with 64

@@ -24,6 +24,7 @@ EXPORTS = [
     "burst_materialized_bwd_workspace_bytes", "burst_local_bwd_materialized", "burst_set_kernel_family",
     "burst_kernel_family_for", "burst_local_bwd_static", "burst_probe_mfma", "burst_probe_atomic_dq",
     "burst_walk_fwd", "burst_walk_bwd", "burst_walk_workspace_bytes", "burst_walk_dkv_form",
+    "burst_rotate", "burst_cache_append", "burst_paged_fwd", "burst_paged_workspace_bytes",
 ]
 
 
@@ -44,6 +45,27 @@ class BurstChunk(ctypes.Structure):
         ("block_mask", ctypes.c_void_p), ("block_mask_stride", ctypes.c_int64), ("k_off", ctypes.c_int64),
         ("kv_strides", ctypes.c_int64 * 3), ("Nc", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class BurstRotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_float), ("inverse", ctypes.c_int32)]
+
+
+class BurstRows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("positions_stride", ctypes.c_int64), ("offset", ctypes.c_int64),
+                ("x_strides", ctypes.c_int64 * 3), ("y_strides", ctypes.c_int64 * 3),
+                ("B", ctypes.c_int32), ("heads", ctypes.c_int32), ("rows", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class BurstPagedParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "rows", "H", "kv_heads", "d", "dtype", "pages", "page", "width",
+                                              "max_new", "causal", "out_f32")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("window", ctypes.c_int64),
+        ("starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("page_strides", ctypes.c_int64 * 3), ("q_strides", ctypes.c_int64 * 2), ("kv_strides", ctypes.c_int64 * 2),
+        ("o_strides", ctypes.c_int64 * 2)]
 
 
 class BurstError(RuntimeError):
@@ -132,6 +154,14 @@ def load():
     lib.burst_walk_fwd.restype = ctypes.c_int
     lib.burst_walk_bwd.argtypes = [vp, cp, ci, vp, vp, fp, fp, vp, ci, ci, ci, vp, sz, pp, vp]
     lib.burst_walk_bwd.restype = ctypes.c_int
+    rp, gp = ctypes.POINTER(BurstRotary), ctypes.POINTER(BurstPagedParams)
+    lib.burst_rotate.argtypes = [ctypes.POINTER(BurstRows), ci, rp, ci, ci, vp]
+    lib.burst_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, rp, gp, vp]
+    lib.burst_paged_fwd.argtypes = [vp, vp, vp, vp, fp, vp, sz, gp, vp]
+    for name in ("burst_rotate", "burst_cache_append", "burst_paged_fwd"):
+        getattr(lib, name).restype = ci
+    lib.burst_paged_workspace_bytes.argtypes = [gp]
+    lib.burst_paged_workspace_bytes.restype = sz
     lib.burst_event_create.argtypes = []
     lib.burst_event_create.restype = vp
     lib.burst_event_record.argtypes = [vp, vp]
@@ -430,6 +460,62 @@ def burst_walk_bwd(Q, chunks, O, dO, lse, D, dQ, p, accumulate_dq=True, accumula
     _check(load().burst_walk_bwd(_q(Q, p), chunks, len(chunks), _q(O, p), _q(dO, p), _f32(lse), _f32(D), _ptr(dQ),
                                  1 if accumulate_dq else 0, 1 if accumulate_dkv else 0, 1 if half else 0,
                                  _ptr(workspace), _bytes(workspace), ctypes.byref(p), _stream()), "burst_walk_bwd")
+
+
+def rotary(turns, interleaved=False, amplitude=1.0, inverse=False):
+    """turns: a contiguous float64 device tensor with an entry for every pair of columns (see burst.h)."""
+    if turns.dtype != torch.float64:
+        raise ValueError("turns: float64 tensor expected")
+    return BurstRotary(_ptr(turns), 2 * turns.numel(), 1 if interleaved else 0, amplitude, 1 if inverse else 0)
+
+
+def burst_rotate(xs, ys, r, offsets=None, positions=None):
+    """xs, ys: lists of [B, heads, rows, d] tensors with a contiguous last dimension, of one type and d; offsets: the position of row 0
+    of each; positions: None, or for each None or an int64 device tensor [B, rows] with contiguous rows, to which its offset is added."""
+    items = (BurstRows * len(xs))()
+    for i, (x, y, c) in enumerate(zip(xs, ys, items)):
+        if x.shape != y.shape or x.dtype != y.dtype or not x.is_cuda or not y.is_cuda:
+            raise ValueError("x, y: device tensors of the same sizes and type expected")
+        c.x_strides[:], c.y_strides[:] = strides_of(x) or (0, 0, 0), strides_of(y) or (0, 0, 0)
+        c.x, c.y, c.B, c.heads, c.rows = x.data_ptr(), y.data_ptr(), x.shape[0], x.shape[1], x.shape[2]
+        c.offset = 0 if offsets is None else offsets[i]
+        if positions is not None and positions[i] is not None:
+            at = positions[i]
+            if at.dtype != torch.int64 or not at.is_cuda or tuple(at.shape) != (x.shape[0], x.shape[2]) or at.stride(1) not in (0, 1):
+                raise ValueError("positions: int64 device tensor [B, rows] expected")
+            c.positions, c.positions_stride = at.data_ptr(), at.stride(0)
+    dtype = BURST_BF16 if not len(xs) or xs[0].dtype == torch.bfloat16 else BURST_F32
+    _check(load().burst_rotate(items, len(xs), ctypes.byref(r), xs[0].shape[3] if len(xs) else 2, dtype, _stream()), "burst_rotate")
+
+
+def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts, scale=1.0, causal=True, window=0, max_new=0, out_f32=False):
+    """k_pages: [pages, kv_heads, page, d] (its strides go into the block; V_pages lies likewise); table [sequences, width], lengths
+    [sequences], starts [sequences + 1]: int32 device tensors.  Token tensors are dense unless their strides are set in the block."""
+    code = {torch.bfloat16: BURST_BF16, torch.float32: BURST_F32, "bf16": BURST_BF16, "f32": BURST_F32}.get(dtype, dtype)
+    p = BurstPagedParams(sequences=lengths.shape[0], rows=q_rows, H=H, kv_heads=kv_heads, d=d, dtype=code, pages=k_pages.shape[0],
+                         page=k_pages.shape[2], width=table.shape[1], max_new=max_new, causal=1 if causal else 0,
+                         out_f32=1 if out_f32 else 0, scale=scale, window=window, starts=starts.data_ptr(), lengths=lengths.data_ptr(),
+                         table=table.data_ptr(), table_stride=table.stride(0))
+    if not k_pages.is_contiguous():
+        p.page_strides[:] = [k_pages.stride(i) for i in range(3)]
+    return p
+
+
+def burst_cache_append(K, V, k_pages, v_pages, Q, Q_out, offsets, r, p):
+    """Q, Q_out, offsets, r: None where there are none."""
+    at = lambda t: None if t is None else ctypes.c_void_p(t.data_ptr())      # noqa: E731  (strided: see the block)
+    _check(load().burst_cache_append(at(K), at(V), at(k_pages), at(v_pages), at(Q), at(Q_out), _ptr(offsets),
+                                     None if r is None else ctypes.byref(r), ctypes.byref(p), _stream()), "burst_cache_append")
+
+
+def burst_paged_workspace_bytes(p):
+    return int(load().burst_paged_workspace_bytes(ctypes.byref(p)))
+
+
+def burst_paged_fwd(Q, k_pages, v_pages, O, lse, p, workspace=None):
+    at = lambda t: ctypes.c_void_p(t.data_ptr())                             # noqa: E731
+    _check(load().burst_paged_fwd(at(Q), at(k_pages), at(v_pages), at(O), _f32(lse), _ptr(workspace), _bytes(workspace),
+                                  ctypes.byref(p), _stream()), "burst_paged_fwd")
 
 
 class Event:

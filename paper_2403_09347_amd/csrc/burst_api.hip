@@ -8,6 +8,8 @@
 #include <mutex>
 #include <vector>
 #include "burst_common.h"
+#include "burst_paged_kernels.h"
+#include "burst_rotary.h"
 
 namespace burst {
 int launch_state_init(const KParams&, float*, float*, float*, hipStream_t);
@@ -655,6 +657,97 @@ size_t split_bytes(const KParams& k, int splits) {
   return splits > 1 ? (size_t)splits * k.B * k.H * k.Nq * ((size_t)k.d + 2) * sizeof(float) : 0;
 }
 
+// ---- positions and the paged cache
+int check_rotary(const burst_rotary* r, int d) {
+  if (r == nullptr || r->turns == nullptr) return BURST_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(r->turns) & 7u) != 0) return BURST_ERR_ALIGN;
+  if (r->dims < 2 || r->dims % 2 != 0 || r->dims > d || !std::isfinite(r->amplitude)) return BURST_ERR_SHAPE;
+  return BURST_OK;
+}
+void set_rotary(burst::RotateArgs& a, const burst_rotary* r) {
+  if (r == nullptr) return;
+  a.turns = r->turns; a.dims = r->dims; a.interleaved = r->interleaved != 0; a.amplitude = r->amplitude; a.inverse = r->inverse != 0;
+}
+#define REQUIRE_ALIGNED(ptr, bytes)                                                       \
+  do {                                                                                    \
+    if ((ptr) == nullptr) return BURST_ERR_NULL;                                          \
+    if ((reinterpret_cast<uintptr_t>(ptr) & ((bytes) - 1u)) != 0) return BURST_ERR_ALIGN; \
+  } while (0)
+
+// Element strides {outer .., row}: those given, or dense ones.  False: negative or not a multiple of `unit`.
+template <int N>
+bool set_strides(long long (&out)[N], const int64_t* in, const long long (&dense)[N], long long unit) {
+  bool none = true;
+  for (int i = 0; i < N; i++) none = none && in[i] == 0;
+  for (int i = 0; i < N; i++) {
+    out[i] = none ? dense[i] : in[i];
+    if (out[i] < 0 || out[i] % unit != 0) return false;
+  }
+  return true;
+}
+struct Paged {
+  long long q[2], kv[2], o[2], page[3];
+  int page_shift;
+  long long table_stride;
+};
+int check_paged(const burst_paged_params* p, Paged& g, bool attend) {
+  if (p == nullptr) return BURST_ERR_NULL;
+  if (p->dtype != BURST_BF16 && p->dtype != BURST_F32) return BURST_ERR_DTYPE;
+  const long long unit = p->dtype == BURST_BF16 ? 8 : 4, d = p->d;
+  if (p->sequences < 0 || p->sequences >= 1 << 30 || p->rows < 0 || p->rows >= 1 << 30 || p->max_new < 0 || p->pages < 0 || p->width < 0 || p->window < 0) return BURST_ERR_SHAPE;
+  if (d < 1 || d > 128 || d % unit != 0 || p->H < 1 || p->kv_heads < 1 || p->H % p->kv_heads != 0) return BURST_ERR_SHAPE;
+  if (p->page < 16 || (p->page & (p->page - 1)) != 0 || (long long)p->width * p->page >= 1LL << 30) return BURST_ERR_SHAPE;
+  if (attend && (!(p->scale > 0.f) || !std::isfinite(p->scale))) return BURST_ERR_SHAPE;
+  if (p->table_stride != 0 && p->table_stride < p->width) return BURST_ERR_SHAPE;
+  g.table_stride = p->table_stride != 0 ? p->table_stride : p->width;
+  g.page_shift = __builtin_ctz((unsigned)p->page);
+  const long long q[2] = {p->H * d, d}, kv[2] = {p->kv_heads * d, d}, page[3] = {p->kv_heads * p->page * d, p->page * d, d};
+  // (the attention reads and writes 16 bytes at a time; rows of a page must not overlap, and 16 of them lie within 2 GiB)
+  const long long u = attend ? unit : 1;
+  if (!set_strides(g.q, p->q_strides, q, u) || !set_strides(g.kv, p->kv_strides, kv, u) || !set_strides(g.o, p->o_strides, q, u) ||
+      !set_strides(g.page, p->page_strides, page, u)) return BURST_ERR_SHAPE;
+  if (g.page[2] < d || g.page[2] >= 1LL << 25) return BURST_ERR_SHAPE;
+  return BURST_OK;
+}
+// The launches of burst_paged_fwd: what each takes, and its runs (as many as the chip holds, or as many units as there can be).
+struct PagedPlan { bool shorts, chunks; int least; burst::PagedArgs a[2]; size_t bytes; };
+void plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
+  const int group = p->H / p->kv_heads, cap = p->width * p->page;
+  const int most = p->max_new > 0 && p->max_new < p->rows ? p->max_new : p->rows;
+  // A sequence whose rows fill 16 rows of an item at most is the short kernel's; longer ones the chunk kernel's (bf16).
+  const int fit = group <= burst::kShortRows ? burst::kShortRows / group : 0;
+  plan.chunks = p->dtype == BURST_BF16 && most > fit;
+  plan.shorts = !plan.chunks || (p->sequences > 1 && fit > 0);
+  plan.bytes = 0;
+  for (int i = 0; i < 2; i++) {
+    burst::PagedArgs& a = plan.a[i];
+    a = burst::PagedArgs{};
+    const int rows = i == 0 ? burst::kShortRows : burst::kChunkRows;
+    a.group = group; a.heads = p->H; a.d = p->d; a.pages = p->pages; a.page_shift = g.page_shift;
+    a.part_heads = group < rows ? group : rows;
+    a.parts_each = (group + rows - 1) / rows;
+    a.table = p->table; a.table_stride = g.table_stride;
+    a.q_row = g.q[0]; a.q_head = g.q[1]; a.o_row = g.o[0]; a.o_head = g.o[1];
+    a.p_page = g.page[0]; a.p_head = g.page[1]; a.p_row = g.page[2];
+    a.o_f32 = p->out_f32 != 0 || p->dtype == BURST_F32;
+    a.scale = p->scale;
+    burst::PagedWork& w = a.w;
+    w.starts = p->starts; w.lengths = p->lengths; w.sequences = p->sequences; w.rows = p->rows; w.cap = cap;
+    w.tokens = group <= rows ? rows / group : 1;
+    w.parts = p->kv_heads * a.parts_each;
+    w.least = i == 0 || !plan.shorts ? 1 : fit + 1;
+    w.most = i == 0 && plan.chunks ? fit : 0x7fffffff;
+    w.causal = p->causal != 0; w.window = p->window;
+    const double units = ((double)p->rows / w.tokens + p->sequences) * w.parts * (cap / burst::kUnit + 1);
+    const int slots = i == 0 ? 1024 : 512;
+    a.runs = units < slots ? (int)units : slots;
+    if (a.runs < 1) a.runs = 1;
+    if (a.runs > 8) a.runs &= ~7;
+    const size_t bytes = a.runs < 2 ? 0 : (size_t)2 * a.runs * rows * (p->d + 2) * sizeof(float);
+    if ((i == 0 ? plan.shorts : plan.chunks) && bytes > plan.bytes) plan.bytes = bytes;
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -1036,6 +1129,129 @@ int burst_walk_bwd(const void* Q, const burst_chunk* chunks, int n_chunks, const
   });
 }
 
+int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d, int dtype, void* stream) {
+  if (n < 0 || d < 2 || d > 128) return BURST_ERR_SHAPE;
+  if (dtype != BURST_BF16 && dtype != BURST_F32) return BURST_ERR_DTYPE;
+  int st = check_rotary(r, d);
+  if (st != BURST_OK) return st;
+  if (n > 0 && tensors == nullptr) return BURST_ERR_NULL;
+  const unsigned size = dtype == BURST_BF16 ? 2 : 4;
+  auto item = [&](const burst_rows& t, burst::RotateItem& it, bool& some) -> int {
+    it = burst::RotateItem{};
+    if (t.B < 0 || t.heads < 0 || t.rows < 0) return BURST_ERR_SHAPE;
+    some = t.B > 0 && t.heads > 0 && t.rows > 0;
+    if (!some) return BURST_OK;
+    REQUIRE_ALIGNED(t.x, size); REQUIRE_ALIGNED(t.y, size);
+    if ((reinterpret_cast<uintptr_t>(t.positions) & 7u) != 0) return BURST_ERR_ALIGN;
+    const long long dense[3] = {(long long)t.heads * t.rows * d, (long long)t.rows * d, d};
+    long long xs[3], ys[3];
+    if (!set_strides(xs, t.x_strides, dense, 1) || !set_strides(ys, t.y_strides, dense, 1)) return BURST_ERR_SHAPE;
+    if (t.positions != nullptr && t.positions_stride < 0) return BURST_ERR_SHAPE;
+    if (t.x == t.y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2])) return BURST_ERR_SHAPE;
+    it.x = t.x; it.y = t.y;
+    it.positions = (const long long*)t.positions; it.positions_stride = t.positions_stride; it.offset = t.offset;
+    it.xs_b = xs[0]; it.xs_h = xs[1]; it.xs_r = xs[2]; it.ys_b = ys[0]; it.ys_h = ys[1]; it.ys_r = ys[2];
+    it.B = t.B; it.heads = t.heads; it.rows = t.rows; it.d = d; it.rotated = 1;
+    return BURST_OK;
+  };
+  burst::RotateItem it;
+  bool some = false, any = false;
+  for (int i = 0; i < n; i++) {
+    if ((st = item(tensors[i], it, some)) != BURST_OK) return st;
+    any = any || some;
+  }
+  if (!any) return BURST_OK;
+  if ((st = check_arch()) != BURST_OK) return st;
+  return validated([&] {
+    for (int i = 0; i < n;) {
+      burst::RotateArgs a = {};
+      set_rotary(a, r);
+      for (; i < n && a.n < burst::kMaxRotateItems; i++) {
+        (void)item(tensors[i], it, some);
+        if (some) a.it[a.n++] = it;
+      }
+      const int e = a.n > 0 ? burst::launch_rotate(a, dtype, (hipStream_t)stream) : (int)BURST_OK;
+      if (e != BURST_OK) return e;
+    }
+    return (int)BURST_OK;
+  });
+}
+
+int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_pages, const void* Q, void* Q_out,
+                       const int64_t* offsets, const burst_rotary* r, const burst_paged_params* p, void* stream) {
+  Paged g;
+  int st = check_paged(p, g, false);
+  if (st != BURST_OK) return st;
+  if (r != nullptr && (st = check_rotary(r, p->d)) != BURST_OK) return st;
+  if (p->sequences == 0 || p->rows == 0) return BURST_OK;
+  const unsigned size = p->dtype == BURST_BF16 ? 2 : 4;
+  REQUIRE_ALIGNED(K, size); REQUIRE_ALIGNED(V, size);
+  if (p->pages > 0) { REQUIRE_ALIGNED(K_pages, size); REQUIRE_ALIGNED(V_pages, size); }
+  REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4);
+  if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
+  if (Q != nullptr) { REQUIRE_ALIGNED(Q, size); REQUIRE_ALIGNED(Q_out, size); }
+  if ((reinterpret_cast<uintptr_t>(offsets) & 7u) != 0) return BURST_ERR_ALIGN;
+  if (Q != nullptr && Q == Q_out && (g.q[0] != g.o[0] || g.q[1] != g.o[1])) return BURST_ERR_SHAPE;
+  if ((st = check_arch()) != BURST_OK) return st;
+  burst::RotateArgs a = {};
+  set_rotary(a, r);
+  a.starts = p->starts; a.lengths = p->lengths; a.table = p->table; a.offsets = (const long long*)offsets;
+  a.table_stride = g.table_stride; a.sequences = p->sequences; a.tokens = p->rows; a.cap = p->width * p->page;
+  a.pages = p->pages; a.page_shift = g.page_shift;
+  auto add = [&](const void* x, void* y, const long long (&xs)[2], int heads, int rotated, int paged) {
+    burst::RotateItem& it = a.it[a.n++];
+    it.x = x; it.y = y; it.xs_r = xs[0]; it.xs_h = xs[1];
+    if (paged) { it.ys_b = g.page[0]; it.ys_h = g.page[1]; it.ys_r = g.page[2]; }
+    else { it.ys_r = g.o[0]; it.ys_h = g.o[1]; }
+    it.B = 1; it.heads = heads; it.rows = p->rows; it.d = p->d; it.rotated = rotated; it.paged = paged;
+  };
+  if (Q != nullptr) add(Q, Q_out, g.q, p->H, r != nullptr, 0);
+  add(K, K_pages, g.kv, p->kv_heads, r != nullptr, 1);
+  add(V, V_pages, g.kv, p->kv_heads, 0, 1);
+  return burst::launch_rotate(a, p->dtype, (hipStream_t)stream);
+}
+
+size_t burst_paged_workspace_bytes(const burst_paged_params* p) {
+  Paged g;
+  if (check_paged(p, g, true) != BURST_OK) return 0;
+  PagedPlan plan;
+  plan_paged(p, g, plan);
+  return plan.bytes;
+}
+
+int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,
+                    size_t workspace_bytes, const burst_paged_params* p, void* stream) {
+  Paged g;
+  int st = check_paged(p, g, true);
+  if (st != BURST_OK) return st;
+  if (p->sequences == 0 || p->rows == 0) return BURST_OK;
+  REQUIRE_PTR(Q); REQUIRE_PTR(O); REQUIRE_PTR(lse);
+  if (p->pages > 0) { REQUIRE_PTR(K_pages); REQUIRE_PTR(V_pages); }
+  REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4);
+  if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
+  PagedPlan plan;
+  plan_paged(p, g, plan);
+  if (plan.bytes > 0) {
+    REQUIRE_PTR(workspace);
+    if (workspace_bytes < plan.bytes) return BURST_ERR_SHAPE;
+  }
+  if ((st = check_arch()) != BURST_OK) return st;
+  for (burst::PagedArgs& a : plan.a) { a.Q = Q; a.O = O; a.lse = lse; a.K = K_pages; a.V = V_pages; a.part = (float*)workspace; }
+  hipStream_t s = (hipStream_t)stream;
+  return validated([&] {
+    int e = BURST_OK;
+    if (plan.chunks) {
+      if ((e = burst::launch_paged_chunk(plan.a[1], s)) != BURST_OK) return e;
+      if ((e = burst::launch_paged_merge(plan.a[1], burst::kChunkRows, s)) != BURST_OK) return e;
+    }
+    if (plan.shorts) {
+      if ((e = burst::launch_paged_short(plan.a[0], p->dtype, s)) != BURST_OK) return e;
+      e = burst::launch_paged_merge(plan.a[0], burst::kShortRows, s);
+    }
+    return e;
+  });
+}
+
 void* burst_event_create(void) {
   hipEvent_t e = nullptr;
   if (hipEventCreate(&e) != hipSuccess) return nullptr;
@@ -1069,6 +1285,6 @@ const char* burst_strerror(int status) {
   }
 }
 
-int burst_version(void) { return 113; }
+int burst_version(void) { return 114; }
 
 }  // extern "C"

@@ -1,0 +1,649 @@
+// Attention of new tokens over a paged cache (burst_paged_fwd): O = softmax(scale Q K^T) V over the keys that a token's
+// position and window leave, K and V in pages, with the running maximum and sum of burst_local_fwd and nothing but
+// O and lse stored.
+//
+// Two kernels.  paged_short_kernel: one wavefront and 16 rows (tokens x the heads of a group) at a time, every wavefront
+// with a stream of K and V tiles of its own through LDS: single tokens, where reading the cache is the work (HBM), and fp32.
+// paged_chunk_kernel (bf16): 128 rows and four wavefronts that share the tiles, bound by the matrix and vector units.
+// Either way the work is a sequence of units (64 keys of 16 or 128 rows, see burst_paged.h) that is cut into runs of equal length,
+// as many as the chip holds at once, whatever the lengths of the sequences are: the arrays that say so are on the device, and a
+// captured call is replayed with others.  Where a run ends inside an item, the item's partial results go to the workspace
+// and paged_merge_kernel joins them, in their order: no atomics, the same bits every time.
+#include "burst_paged_kernels.h"
+
+namespace burst {
+
+// Lanes' values of the four groups of 16 lanes, combined: every lane gets the result of the lanes equal to it modulo 16.
+__device__ __forceinline__ float max_over_groups(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float sum_over_groups(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+__device__ __forceinline__ bool is_zero(float x) { return (__builtin_bit_cast(unsigned, x) << 1) == 0; }
+
+// An item's row: its token and query head, if it has one.
+struct ItemRow { bool there; int token, head; };
+__device__ __forceinline__ ItemRow item_row(const PagedArgs& a, const PagedSegment& g, int r) {
+  const int kvhead = g.part / a.parts_each, part = g.part - kvhead * a.parts_each;
+  const int t = r / a.part_heads, j = part * a.part_heads + r - t * a.part_heads;
+  ItemRow x;
+  x.token = g.block * a.w.tokens + t;
+  x.head = kvhead * a.group + j;
+  x.there = t < a.w.tokens && x.token < g.q.n && j < a.group;
+  return x;
+}
+// The keys [lo, hi] that a token sees
+struct KeyRange { int lo, hi; };
+__device__ __forceinline__ KeyRange seen_keys(const PagedWork& w, const PagedSeq& q, int token) {
+  const int pos = q.len - q.n + token;
+  KeyRange k = {0, w.causal ? min(pos, q.len - 1) : q.len - 1};
+  if (w.window > 0) {
+    const long long first = (long long)pos - w.window + 1;
+    k.lo = first > 0 ? (int)min(first, (long long)0x7fffffff) : 0;
+  }
+  return k;
+}
+
+// A finished row (m in natural units, l, and its columns by `each`): the output and lse, or its partial result.
+struct RowPlace {
+  bool whole;
+  float* part; float* ml;            // partial: columns; m and l
+  size_t o;                          // element offset in O
+  size_t lse;
+};
+__device__ __forceinline__ RowPlace row_place(const PagedArgs& a, const PagedSegment& g, int run, int rows_of_item, int r, const ItemRow& x) {
+  RowPlace p;
+  p.whole = g.whole();
+  float* const base = a.part + (size_t)partial_slot(g, run) * rows_of_item * (a.d + 2);
+  p.part = base + (size_t)r * a.d;
+  p.ml = base + (size_t)rows_of_item * a.d + r;
+  p.o = (size_t)(g.q.first + x.token) * a.o_row + (size_t)x.head * a.o_head;
+  p.lse = (size_t)(g.q.first + x.token) * a.heads + x.head;
+  return p;
+}
+__device__ __forceinline__ void store4(const PagedArgs& a, size_t at, const f32x4& v) {
+  if (a.o_f32) {
+    *reinterpret_cast<f32x4*>((float*)a.O + at) = v;
+  } else {
+    bf16x4 h;
+#pragma unroll
+    for (int k = 0; k < 4; k++) h[k] = (bf16)v[k];
+    *reinterpret_cast<bf16x4*>((bf16*)a.O + at) = h;
+  }
+}
+__device__ __forceinline__ void store1(const PagedArgs& a, size_t at, float v) {
+  if (a.o_f32) ((float*)a.O)[at] = v;
+  else ((bf16*)a.O)[at] = (bf16)v;
+}
+__device__ __forceinline__ float row_lse(float m, float l) { return is_zero(l) ? BURST_NEG_INF : m + __logf(l); }
+
+// Rows whose accumulators came out infinite or NaN, by themselves with scalar products of the visible pairs only: a matrix product
+// multiplies hidden pairs too (by a probability of 0, and 0 x inf is NaN).  One wavefront, one row at a time.
+template <typename T>
+__device__ __forceinline__ void row_again(const PagedArgs& a, const PagedSegment& g, int run, int rows_of_item, int r, int lane) {
+  const ItemRow x = item_row(a, g, r);
+  if (!x.there) return;
+  const int d = a.d, kvhead = g.part / a.parts_each;
+  const T* const q = (const T*)a.Q + (size_t)(g.q.first + x.token) * a.q_row + (size_t)x.head * a.q_head;
+  KeyRange k = seen_keys(a.w, g.q, x.token);
+  k.lo = max(k.lo, g.from << kUnitShift);
+  k.hi = min(k.hi, (g.to << kUnitShift) - 1);
+  float m = BURST_NEG_INF, l = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll 1
+  for (int k0 = k.lo; k0 <= k.hi; k0 += 64) {
+    const int key = k0 + lane;
+    int page = -1;
+    if (key <= k.hi) page = checked_page(a.table[(long long)g.s * a.table_stride + (key >> a.page_shift)], a.pages);
+    const bool seen = page >= 0;
+    const long long row = (long long)page * a.p_page + (long long)kvhead * a.p_head + (long long)(key & ((1 << a.page_shift) - 1)) * a.p_row;
+    float s = 0.f;
+    if (seen) {
+      const T* const kr = (const T*)a.K + row;
+#pragma unroll 1
+      for (int c = 0; c < d; c++) s = __builtin_fmaf((float)q[c], (float)kr[c], s);
+      s = product(s, a.scale);
+    } else {
+      s = BURST_NEG_INF;
+    }
+    float mx = s;
+    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+    const float to = fmaxf(m, mx), ref = to == BURST_NEG_INF ? 0.f : to, alpha = fast_exp2((m - ref) * kLog2e);
+    const float p = seen ? fast_exp2((s - ref) * kLog2e) : 0.f;
+    m = to;
+    float sum = p;
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    l = l * alpha + sum;
+    o0 *= alpha; o1 *= alpha;
+    unsigned long long left = __builtin_amdgcn_ballot_w64(seen);
+    const int row_lo = (int)row, row_hi = (int)(row >> 32);
+#pragma unroll 1
+    while (left != 0) {
+      const int j = __builtin_ctzll(left);
+      left &= left - 1;
+      const float pj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p), j));
+      const long long at = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane(row_hi, j) << 32) |
+                                       (unsigned)__builtin_amdgcn_readlane(row_lo, j));
+      const T* const vr = (const T*)a.V + at;
+      if (lane < d) o0 = __builtin_fmaf(pj, (float)vr[lane], o0);
+      if (lane + 64 < d) o1 = __builtin_fmaf(pj, (float)vr[lane + 64], o1);
+    }
+  }
+  const RowPlace at = row_place(a, g, run, rows_of_item, r, x);
+  const float inv = is_zero(l) ? 0.f : 1.f / l;
+#pragma unroll
+  for (int j = 0; j < 2; j++) {
+    const int c = lane + 64 * j;
+    if (c >= d) continue;
+    const float v = j ? o1 : o0;
+    if (at.whole) store1(a, at.o + c, is_zero(l) ? 0.f : v * inv);
+    else at.part[c] = v;
+  }
+  if (lane == 0) {
+    if (at.whole) a.lse[at.lse] = row_lse(m, l);
+    else { at.ml[0] = m; at.ml[rows_of_item] = l; }
+  }
+}
+
+// vmcnt(N), the other counters untouched; nothing moves across it
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// ------------------------------------------------------------------------------- short
+// S^T = K Q^T of 16 keys x 16 rows: lane (r = lane % 16, g = lane / 16) gets row r, keys 4g .. 4g + 3, which is also how the second
+// product, O^T += V^T P^T, wants P.  The order of the summed columns is free, so a lane's operands are 16-byte pieces of a row of K or
+// Q: granule 4 ks + g in step ks.  A stage is 16 keys, K and V, brought to LDS by DMA (rows beyond the sequence arrive as
+// zeros) in a ring of stages that runs on across the items of the run; a wavefront waits for its own loads alone, there are no barriers.
+// LDS rows of 8, 16 or 32 granules, permuted so that 16 rows of one granule column fall into different banks.
+template <int GR>
+__device__ __forceinline__ int short_code(int row) { return GR == 8 ? (row >> 1) & 7 : row_code(row & 15); }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(64, 1)
+paged_short_kernel(PagedArgs a) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int ROWB = D * (int)sizeof(T), GR = ROWB / 16, TILE = 16 * ROWB;
+  constexpr int NST = kShortLds / (2 * TILE);      // stages
+  constexpr int RPL = 1024 / ROWB, NL = TILE / 1024, LOADS = 2 * NL;   // rows of a load; loads of K, of a stage
+  constexpr int KS = GR / 4;                       // granule steps of a product over d
+  constexpr int OB = D / 16;                       // 16-column blocks of O^T
+  static_assert(NST >= 2 && (NST - 1) * LOADS < 64, "the ring fits LDS and the counter of loads");
+  __shared__ __attribute__((aligned(16))) char smem[NST * 2 * TILE];
+  const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
+  const int run = run_of(blockIdx.x, a.runs);
+  DeviceCursor cur;
+  if (!locate_run(a, run, lane, cur)) return;
+  DeviceCursor fet = cur;
+  const unsigned lds0 = lds_addr(smem);
+  const int d = a.d;
+
+  int goff[NL];
+#pragma unroll
+  for (int i = 0; i < NL; i++) {
+    const int row = i * RPL + lane / GR, granule = (lane % GR) ^ short_code<GR>(row);
+    goff[i] = granule * (16 / (int)sizeof(T)) < d ? row * (int)(a.p_row * sizeof(T)) + granule * 16 : (int)0x80000000u;
+  }
+  const unsigned pitch = (unsigned)(a.p_row * sizeof(T)), row_bytes = (unsigned)(d * sizeof(T));
+
+  // The fetching side.  `page` is that of stage f_at, asked for one fetch ahead.
+  int f_at, f_end, page = -1;
+  bool f_more = true;
+  auto page_of = [&](int stage) __attribute__((always_inline)) {
+    return scalar_at(a.table, (long long)fet.g.s * a.table_stride + ((stage << 4) >> a.page_shift));
+  };
+  auto settle = [&]() __attribute__((always_inline)) {   // f_at to the next stage there is
+    while (f_at >= f_end) {
+      if (!fet.next(a.w)) { f_more = false; return; }
+      segment_tiles(a.w, fet.g, 4, f_at, f_end);
+    }
+    page = page_of(f_at);
+  };
+  segment_tiles(a.w, fet.g, 4, f_at, f_end);
+  settle();
+  unsigned bad = 0;                                // stages of the ring whose page is none
+  int f_slot = 0, ahead = 0;                       // slot that is filled next; stages asked for and not yet used
+  auto fetch = [&]() __attribute__((always_inline)) {
+    if (!f_more) return;
+    const int key0 = f_at << 4, ok = checked_page(page, a.pages), kvhead = fet.g.part / a.parts_each;
+    const int rows = ok >= 0 ? min(16, fet.g.q.len - key0) : 0;
+    const long long at = (long long)max(ok, 0) * a.p_page + (long long)kvhead * a.p_head + (long long)(key0 & ((1 << a.page_shift) - 1)) * a.p_row;
+    const unsigned span = rows > 0 ? (unsigned)(rows - 1) * pitch + row_bytes : 0u;
+    const __amdgpu_buffer_rsrc_t krs = make_rsrc((const T*)a.K + at, span), vrs = make_rsrc((const T*)a.V + at, span);
+    const unsigned to = lds0 + (unsigned)f_slot * (2 * TILE);
+#pragma unroll
+    for (int i = 0; i < NL; i++) dma_b128_to_lds(krs, to + i * 1024u, goff[i]);
+#pragma unroll
+    for (int i = 0; i < NL; i++) dma_b128_to_lds(vrs, to + TILE + i * 1024u, goff[i]);
+    bad = ok >= 0 ? bad & ~(1u << f_slot) : bad | (1u << f_slot);
+    f_slot = f_slot + 1 == NST ? 0 : f_slot + 1;
+    ahead++;
+    f_at++;
+    settle();
+  };
+#pragma unroll 1
+  for (int i = 0; i < NST; i++) fetch();
+
+  // addresses of the operands in a tile
+  int kaddr[KS], vaddr[F32 ? GR / 16 : OB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) kaddr[ks] = r * ROWB + (((4 * ks + g) ^ short_code<GR>(r)) << 4);
+  if constexpr (!F32) {                            // transposing reads: keys 4g .. 4g + 3, columns 16 ob .. 16 ob + 15
+    const int row = 4 * g + (r >> 2);
+#pragma unroll
+    for (int ob = 0; ob < OB; ob++) vaddr[ob] = row * ROWB + (((2 * ob + ((r & 3) >> 1)) ^ short_code<GR>(row)) << 4) + (r & 1) * 8;
+  }
+  int slot = 0;
+  do {
+    const PagedSegment& s = cur.g;
+    const ItemRow x = item_row(a, s, r);
+    const KeyRange see = seen_keys(a.w, s.q, x.token);
+    i32x4 q[KS];
+    {
+      const T* const qr = (const T*)a.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * a.q_row + (size_t)(x.there ? x.head : 0) * a.q_head;
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) {
+        const int c = (4 * ks + g) * (16 / (int)sizeof(T));
+        q[ks] = x.there && c < d ? *reinterpret_cast<const i32x4*>(qr + c) : i32x4{0, 0, 0, 0};
+      }
+    }
+    f32x4 o[OB];
+#pragma unroll
+    for (int b = 0; b < OB; b++) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = BURST_NEG_INF, l = 0.f;              // the row's reference (natural units); its sum over this lane's keys
+    const int t0 = s.block * a.w.tokens, t1 = min(s.q.n, t0 + a.w.tokens) - 1;
+    const KeyRange all = {seen_keys(a.w, s.q, t1).lo, seen_keys(a.w, s.q, t0).hi};   // seen by every row
+    int st, end;
+    segment_tiles(a.w, s, 4, st, end);
+#pragma unroll 1
+    for (; st < end; st++) {
+      if (ahead == NST) wait_loads<(NST - 1) * LOADS>();
+      else wait_loads<0>();
+      const char* const kl = smem + slot * (2 * TILE);
+      const char* const vl = kl + TILE;
+      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) {
+        const i32x4 k = *reinterpret_cast<const i32x4*>(kl + kaddr[ks]);
+        if constexpr (F32) {
+          const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q[ks]);
+#pragma unroll
+          for (int j = 0; j < 4; j++) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j], qf[j], sc, 0, 0, 0);
+        } else {
+          sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[ks]), sc, 0, 0, 0);
+        }
+      }
+      const int key0 = st << 4;
+      const bool gone = ((bad >> slot) & 1) != 0;
+#pragma unroll
+      for (int j = 0; j < 4; j++) sc[j] = product(sc[j], a.scale);
+      if (gone || key0 < all.lo || key0 + 15 > all.hi) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int key = key0 + 4 * g + j;
+          if (gone || key < see.lo || key > see.hi) sc[j] = BURST_NEG_INF;
+        }
+      }
+      const float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+      // A row's first reference, or one that has been exceeded by more than a factor of e^8 (P is then still a bf16 with
+      // all its bits, and l far from its range's end).
+      if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
+        const float to = fmaxf(m, max_over_groups(mx)), alpha = fast_exp2((m - (to == BURST_NEG_INF ? 0.f : to)) * kLog2e);
+        m = to;
+        l *= alpha;
+#pragma unroll
+        for (int b = 0; b < OB; b++) o[b] *= alpha;
+      }
+      const float ref = m == BURST_NEG_INF ? 0.f : m;
+      float p[4];
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        p[j] = fast_exp2((sc[j] - ref) * kLog2e);
+        l += p[j];
+      }
+      if constexpr (F32) {                         // block 4 half + c: columns 64 half + 4 (lane % 16) + c of V
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+          for (int half = 0; half < GR / 16; half++) {
+            const int row = 4 * g + j;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(vl + row * ROWB + (((r + 16 * half) ^ short_code<GR>(row)) << 4));
+#pragma unroll
+            for (int c = 0; c < 4; c++) o[4 * half + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[c], p[j], o[4 * half + c], 0, 0, 0);
+          }
+      } else {
+        bf16x4 pb;
+#pragma unroll
+        for (int j = 0; j < 4; j++) pb[j] = (bf16)p[j];
+#pragma unroll
+        for (int b = 0; b < OB; b++)
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, lds_read_tr(vl, vaddr[b])), __builtin_bit_cast(s16x4, pb), o[b], 0, 0, 0);
+      }
+      wait_lds();                                  // (the tile has been read: its slot is filled again)
+      ahead--;
+      slot = slot + 1 == NST ? 0 : slot + 1;
+      fetch();
+    }
+    l = sum_over_groups(l);
+    unsigned most = larger_of(0, l);
+#pragma unroll
+    for (int b = 0; b < OB; b++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) most = larger_of(most, o[b][j]);
+    const unsigned long long bal = __builtin_amdgcn_ballot_w64(x.there && most >= kInfBits);
+    unsigned redo = (unsigned)(bal | (bal >> 16) | (bal >> 32) | (bal >> 48)) & 0xffffu;
+    if (x.there && !((redo >> r) & 1)) {
+      const RowPlace at = row_place(a, s, run, 16, r, x);
+      const float inv = is_zero(l) ? 0.f : 1.f / l;
+#pragma unroll
+      for (int b = 0; b < OB; b++) {
+        f32x4 v;
+        int c;
+        if constexpr (F32) {                       // block b of lane group g: row 4g + j of block 4 half + i holds column 64 half + 16 g + 4 j + i
+          const int half = b >> 2, j = b & 3;
+          c = 64 * half + 16 * g + 4 * j;
+          v = f32x4{o[4 * half][j], o[4 * half + 1][j], o[4 * half + 2][j], o[4 * half + 3][j]};
+        } else {
+          c = 16 * b + 4 * g;
+          v = o[b];
+        }
+        if (c >= d) continue;
+        if (at.whole) store4(a, at.o + c, v * inv);
+        else *reinterpret_cast<f32x4*>(at.part + c) = v;
+      }
+      if (g == 0) {
+        if (at.whole) a.lse[at.lse] = row_lse(m, l);
+        else { at.ml[0] = m; at.ml[16] = l; }
+      }
+    }
+    for (; redo != 0; redo &= redo - 1) row_again<T>(a, s, run, 16, __builtin_ctz(redo), lane);
+  } while (cur.next(a.w));
+}
+
+// ------------------------------------------------------------------------------- chunk
+// Four wavefronts of 32 rows each share K and V tiles of 64 keys, double-buffered in LDS (DMA, one barrier a tile); operand
+// orientation and LDS layout as in burst_plain_mfma.h: S^T = K Q^T with a row per lane, whose P is the operand of
+// O^T += V^T P^T as it stands.  A wavefront fetches 16 keys of every tile, which lie in one page.  Two workgroups a CU, so that one's
+// vector work overlaps the other's matrix work.
+// Scores and references are in log2 units (one fma an exponent), as in the d = 64 and d = 128 kernels of the walks.
+template <int D>
+__device__ __forceinline__ int chunk_code(int row) { return D == 64 ? (row >> 1) & 7 : row_code(row); }
+template <int D>
+__global__ void __launch_bounds__(256, 2)
+paged_chunk_kernel(PagedArgs a) {
+  constexpr int ROWB = 2 * D, GR = ROWB / 16, RPL = 1024 / ROWB, NL = 16 / RPL, TILE = kUnit * ROWB;
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
+  const int lane = threadIdx.x & 63, lr = lane & 31, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = run_of(blockIdx.x, a.runs);
+  DeviceCursor cur;
+  if (!locate_run(a, run, lane, cur)) return;
+  DeviceCursor fet = cur;
+  const unsigned lds0 = lds_addr(smem);
+  const int d = a.d;
+  const unsigned pitch = (unsigned)(a.p_row * 2), row_bytes = (unsigned)(d * 2);
+  int goff[NL];
+#pragma unroll
+  for (int i = 0; i < NL; i++) {
+    const int row = i * RPL + lane / GR, granule = (lane % GR) ^ chunk_code<D>(row);
+    goff[i] = granule * 8 < d ? row * (int)pitch + granule * 16 : (int)0x80000000u;
+  }
+
+  // The fetching side, a tile ahead; the pages of its next tile's four groups of 16 keys.
+  int f_at, f_end, page[4] = {-1, -1, -1, -1};
+  bool f_more = true;
+  auto settle = [&]() __attribute__((always_inline)) {
+    while (f_at >= f_end) {
+      if (!fet.next(a.w)) { f_more = false; return; }
+      segment_tiles(a.w, fet.g, kUnitShift, f_at, f_end);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      page[i] = scalar_at(a.table, (long long)fet.g.s * a.table_stride + (min((f_at << kUnitShift) + 16 * i, fet.g.q.len - 1) >> a.page_shift));
+  };
+  segment_tiles(a.w, fet.g, kUnitShift, f_at, f_end);
+  settle();
+  unsigned bad = 0;                                // four bits a buffer: groups of keys whose page is none
+  auto fetch = [&](int buf) __attribute__((always_inline)) {
+    if (!f_more) return;
+    unsigned none = 0;
+    int mine = -1;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int ok = checked_page(page[i], a.pages);
+      if (ok < 0) none |= 1u << i;
+      if (i == w) mine = ok;
+    }
+    const int key0 = (f_at << kUnitShift) + 16 * w, kvhead = fet.g.part / a.parts_each;
+    const int rows = mine >= 0 ? __builtin_amdgcn_readfirstlane(max(0, min(16, fet.g.q.len - key0))) : 0;
+    const long long at = (long long)max(mine, 0) * a.p_page + (long long)kvhead * a.p_head + (long long)(key0 & ((1 << a.page_shift) - 1)) * a.p_row;
+    const unsigned span = rows > 0 ? (unsigned)(rows - 1) * pitch + row_bytes : 0u;
+    const __amdgpu_buffer_rsrc_t krs = make_rsrc((const bf16*)a.K + at, span), vrs = make_rsrc((const bf16*)a.V + at, span);
+    const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)buf * TILE + (unsigned)(w * NL) * 1024u);
+#pragma unroll
+    for (int i = 0; i < NL; i++) {
+      dma_b128_to_lds(krs, to + i * 1024u, goff[i]);
+      dma_b128_to_lds(vrs, to + 2 * TILE + i * 1024u, goff[i]);
+    }
+    bad = (bad & ~(15u << (4 * buf))) | (none << (4 * buf));
+    f_at++;
+    settle();
+  };
+  fetch(0);
+
+  int kaddr[KS], taddr[DB][2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) kaddr[ks] = lr * ROWB + (((2 * ks + h) ^ chunk_code<D>(lr)) << 4);
+#pragma unroll
+  for (int db = 0; db < DB; db++)
+#pragma unroll
+    for (int sx = 0; sx < 2; sx++) {
+      const int j16 = lane & 15, row = 8 * sx + 4 * h + (j16 >> 2), granule = db * 4 + 2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1);
+      taddr[db][sx] = row * ROWB + ((granule ^ chunk_code<D>(row)) << 4) + (j16 & 1) * 8;
+    }
+  const float c = a.scale * kLog2e;
+  int buf = 0;
+  do {
+    const PagedSegment& s = cur.g;
+    const ItemRow x = item_row(a, s, 32 * w + lr);
+    const KeyRange see = seen_keys(a.w, s.q, x.token);
+    bf16x8 q[KS];
+    {
+      const bf16* const qr = (const bf16*)a.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * a.q_row + (size_t)(x.there ? x.head : 0) * a.q_head;
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) {
+        const int col = 16 * ks + 8 * h;
+        const i32x4 v = x.there && col < d ? *reinterpret_cast<const i32x4*>(qr + col) : i32x4{0, 0, 0, 0};
+        q[ks] = __builtin_bit_cast(bf16x8, v);
+      }
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; db++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) o[db][r] = 0.f;
+    float m = BURST_NEG_INF, l = 0.f;              // reference (log2 units); the row's sum over this lane's keys
+    // tokens of the wavefront's rows: what all of them see, and what any of them does
+    const int most = min(a.w.tokens, s.q.n - s.block * a.w.tokens) - 1;
+    const int t0 = s.block * a.w.tokens + 32 * w / a.part_heads, t1 = s.block * a.w.tokens + min((32 * w + 31) / a.part_heads, most);
+    const bool rows_here = 32 * w / a.part_heads <= most;
+    const KeyRange first = seen_keys(a.w, s.q, t0), last = seen_keys(a.w, s.q, t1);
+    int at, end;
+    segment_tiles(a.w, s, kUnitShift, at, end);
+#pragma unroll 1
+    for (; at < end; at++, buf ^= 1) {
+      __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      const unsigned gone = (bad >> (4 * buf)) & 15u;
+      fetch(buf ^ 1);
+      const int key0 = at << kUnitShift;
+      if (!rows_here || key0 > last.hi || key0 + kUnit - 1 < first.lo) continue;   // none of the wavefront's rows sees the tile
+      const char* const kl = smem + buf * TILE;
+      const char* const vl = smem + (2 + buf) * TILE;
+      f32x16 sc[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) sc[kb][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) sc[kb] = mfma32(lds_read_b128(kl, kb * 32 * ROWB + kaddr[ks]), q[ks], sc[kb]);
+      if (gone != 0 || key0 < last.lo || key0 + kUnit - 1 > first.hi) {   // register r of block kb: key 32 kb + 8 (r / 4) + 4 h + r % 4
+        const int lo = see.lo - key0 - 4 * h, hi = see.hi - key0 - 4 * h;
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) {
+            const int k = kb * 32 + 8 * (r >> 2) + (r & 3);
+            if (k < lo || k > hi || ((gone >> (2 * kb + (r >> 3))) & 1)) sc[kb][r] = BURST_NEG_INF;
+          }
+      }
+      float mx = sc[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) mx = fmaxf(mx, sc[kb][r]);
+      mx *= c;
+      if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {   // a row's first reference, or one exceeded by more than 2^8
+        const float to = fmaxf(m, max_both_halves(mx)), alpha = fast_exp2(m - (to == BURST_NEG_INF ? 0.f : to));
+        m = to;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; db++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) o[db][r] *= alpha;
+      }
+      const float nref = m == BURST_NEG_INF ? 0.f : -m;
+      bf16x8 p[4];
+#pragma unroll
+      for (int kg = 0; kg < 4; kg++)
+#pragma unroll
+        for (int t = 0; t < 8; t++) {
+          const float v = fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t], c, nref));
+          p[kg][t] = (bf16)v;
+          l += v;                                  // (unrounded: lse has 24 bits)
+        }
+#pragma unroll
+      for (int kg = 0; kg < 4; kg++)
+#pragma unroll
+        for (int db = 0; db < DB; db++) {
+          const bf16x4 va = lds_read_tr(vl, kg * 16 * ROWB + taddr[db][0]), vb = lds_read_tr(vl, kg * 16 * ROWB + taddr[db][1]);
+          o[db] = mfma32(__builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7), p[kg], o[db]);
+        }
+    }
+    l = sum_both_halves(l);
+    unsigned big = larger_of(0, l);
+#pragma unroll
+    for (int db = 0; db < DB; db++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) big = larger_of(big, o[db][r]);
+    const unsigned long long bal = __builtin_amdgcn_ballot_w64(x.there && big >= kInfBits);
+    unsigned redo = (unsigned)(bal | (bal >> 32));
+    if (x.there && !((redo >> lr) & 1)) {
+      const RowPlace to = row_place(a, s, run, kChunkRows, 32 * w + lr, x);
+      const float inv = is_zero(l) ? 0.f : 1.f / l;
+#pragma unroll
+      for (int db = 0; db < DB; db++)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; q4++) {
+          const int col = db * 32 + 8 * q4 + 4 * h;
+          if (col >= d) continue;
+          const f32x4 v = {o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
+          if (to.whole) store4(a, to.o + col, v * inv);
+          else *reinterpret_cast<f32x4*>(to.part + col) = v;
+        }
+      if (h == 0) {
+        const float mn = m * kLn2;
+        if (to.whole) a.lse[to.lse] = row_lse(mn, l);
+        else { to.ml[0] = mn; to.ml[kChunkRows] = l; }
+      }
+    }
+    for (; redo != 0; redo &= redo - 1) row_again<bf16>(a, s, run, kChunkRows, 32 * w + __builtin_ctz(redo), lane);
+  } while (cur.next(a.w));
+}
+
+// ------------------------------------------------------------------------------- merge
+// Joins the partial results of the items that more than one run has worked on: a workgroup for every run whose start is the
+// first one inside an item.  A wavefront takes a row; the item's first part is in slot 1 of its run, the others in slot 0 of theirs.
+__global__ void __launch_bounds__(256)
+paged_merge_kernel(PagedArgs a, int rows_of_item) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int run = blockIdx.x + 1;
+  DeviceCursor cur;
+  if (!locate_run(a, run, lane, cur)) return;
+  const PagedSegment& g = cur.g;
+  const int n = parts_to_join(g, cur.run), first = run - 1, d = a.d;
+  if (n == 0) return;
+  const size_t slot = (size_t)rows_of_item * (d + 2);
+  for (int r = blockIdx.y * 4 + wave; r < rows_of_item; r += 4 * gridDim.y) {
+    const ItemRow x = item_row(a, g, r);
+    if (!x.there) continue;
+    auto part = [&](int i) { return a.part + (2 * (size_t)(first + i) + (i == 0 ? 1 : 0)) * slot; };
+    float top = BURST_NEG_INF;
+    for (int i = lane; i < n; i += 64) top = fmaxf(top, part(i)[(size_t)rows_of_item * d + r]);
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    const float ref = top == BURST_NEG_INF ? 0.f : top;
+    float l = 0.f, o0 = 0.f, o1 = 0.f;
+    const bool c0 = lane < d, c1 = lane + 64 < d;
+    for (int base = 0; base < n; base += 64) {
+      const int i = base + lane;
+      float f = 0.f;
+      if (i < n) {
+        const float* const ml = part(i) + (size_t)rows_of_item * d + r;
+        f = fast_exp2((ml[0] - ref) * kLog2e);
+        l += is_zero(f) ? 0.f : f * ml[rows_of_item];
+      }
+      const int here = min(64, n - base);
+#pragma unroll 4
+      for (int k = 0; k < here; k++) {
+        const float fk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k));
+        const float* const o = part(base + k) + (size_t)r * d;
+        const float v0 = c0 ? o[lane] : 0.f, v1 = c1 ? o[lane + 64] : 0.f;
+        o0 += is_zero(fk) ? 0.f : fk * v0;
+        o1 += is_zero(fk) ? 0.f : fk * v1;
+      }
+    }
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+    const size_t at = (size_t)(g.q.first + x.token) * a.o_row + (size_t)x.head * a.o_head;
+    const float inv = is_zero(l) ? 0.f : 1.f / l;
+    if (c0) store1(a, at + lane, is_zero(l) ? 0.f : o0 * inv);
+    if (c1) store1(a, at + lane + 64, is_zero(l) ? 0.f : o1 * inv);
+    if (lane == 0) a.lse[(size_t)(g.q.first + x.token) * a.heads + x.head] = row_lse(top, l);
+  }
+}
+
+// ------------------------------------------------------------------------------- launches
+int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s) {
+  const dim3 grid((unsigned)a.runs), block(64);
+  if (dtype == BURST_BF16) {
+    if (a.d <= 64) BURST_LAUNCH((paged_short_kernel<bf16, 64>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_short_kernel<bf16, 128>), grid, block, 0, s, a);
+  } else {
+    if (a.d <= 64) BURST_LAUNCH((paged_short_kernel<float, 64>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_short_kernel<float, 128>), grid, block, 0, s, a);
+  }
+  return launch_status();
+}
+int launch_paged_chunk(const PagedArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.runs), block(256);
+  if (a.d <= 64) BURST_LAUNCH(paged_chunk_kernel<64>, grid, block, 0, s, a);
+  else BURST_LAUNCH(paged_chunk_kernel<128>, grid, block, 0, s, a);
+  return launch_status();
+}
+int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {
+  if (a.runs < 2) return BURST_OK;
+  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item / 16), dim3(256), 0, s, a, rows_of_item);
+  return launch_status();
+}
+
+}  // namespace burst

@@ -1,4 +1,5 @@
-// The differentiable call behind autograd.burst_attention: attention of a query slice against key/value
+// The torch calls of the package: rotary.burst_rotary and its gradient, paged's two calls, RingWalk's usual calls, and
+// the differentiable call behind autograd.burst_attention: attention of a query slice against key/value
 // chunks as one torch autograd node, in C++.  Argument marshalling and buffers only; every arithmetic
 // step is a call into libburst.so (paper Alg. 1 forward, Alg. 2 backward).
 // Why native: in Python the two halves of a call ran on two threads (autograd's backward thread is another
@@ -268,10 +269,230 @@ std::tuple<int, Tensor, std::vector<Tensor>, std::vector<Tensor>> walk_backward(
   return {st, dQ, dK, dV};
 }
 
+// ---- rotary.burst_rotary: several tensors rotated by one call, and their gradients brought back by another.
+bool rows_in_place(const Tensor& t) {              // strides that burst_rotate takes: all zero would mean dense ones
+  if (t.size(3) != 1 && t.stride(3) != 1) return false;
+  for (int i = 0; i < 3; i++) if (t.size(i) > 1 && t.stride(i) != 0) return true;
+  return t.is_contiguous();
+}
+variable_list rotate_all(const variable_list& xs, const Tensor& turns, const variable_list& positions, const std::vector<int64_t>& position_of,
+                         const std::vector<int64_t>& offsets, bool interleaved, double amplitude, bool inverse) {
+  const Tensor& like = xs[0];
+  const c10::DeviceGuard on(like.device());
+  variable_list from, out;
+  std::vector<burst_rows> items(xs.size());
+  for (size_t i = 0; i < xs.size(); i++) {
+    from.push_back(rows_in_place(xs[i]) ? xs[i] : xs[i].contiguous());
+    const Tensor& x = from[i];
+    out.push_back(torch::empty_like(x));           // lies in memory like x, without its gaps
+    burst_rows& c = items[i];
+    c = burst_rows{};
+    c.x = x.data_ptr(); c.y = out[i].data_ptr();
+    c.B = (int32_t)x.size(0); c.heads = (int32_t)x.size(1); c.rows = (int32_t)x.size(2);
+    set_strides(c.x_strides, x);
+    set_strides(c.y_strides, out[i]);
+    c.offset = offsets[i];
+    if (position_of[i] >= 0) {
+      const Tensor& p = positions[position_of[i]];
+      c.positions = p.data_ptr<int64_t>();
+      c.positions_stride = p.dim() == 2 && p.size(0) > 1 ? p.stride(0) : 0;
+    }
+  }
+  burst_rotary r{};
+  r.turns = turns.data_ptr<double>(); r.dims = (int32_t)(2 * turns.numel()); r.interleaved = interleaved; r.amplitude = (float)amplitude; r.inverse = inverse;
+  check(burst_rotate(items.data(), (int)items.size(), &r, (int)like.size(3), like.scalar_type() == torch::kBFloat16 ? BURST_BF16 : BURST_F32,
+                     stream_of(like)), "burst_rotate");
+  return out;
+}
+class Rotate : public torch::autograd::Function<Rotate> {
+ public:
+  // xp: n tensors, then the positions of those that have some (position_of)
+  static variable_list forward(AutogradContext* ctx, const Tensor& turns, at::TensorList xp, int64_t n, const std::vector<int64_t>& position_of,
+                               const std::vector<int64_t>& offsets, bool interleaved, double amplitude) {
+    const variable_list xs(xp.begin(), xp.begin() + n), positions(xp.begin() + n, xp.end());
+    variable_list saved = {turns};
+    saved.insert(saved.end(), positions.begin(), positions.end());
+    ctx->save_for_backward(saved);
+    ctx->saved_data["position_of"] = position_of;
+    ctx->saved_data["offsets"] = offsets;
+    ctx->saved_data["interleaved"] = interleaved;
+    ctx->saved_data["amplitude"] = amplitude;
+    ctx->saved_data["type"] = (int64_t)xs[0].scalar_type();
+    ctx->set_materialize_grads(false);
+    return rotate_all(xs, turns, positions, position_of, offsets, interleaved, amplitude, false);
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const variable_list s = ctx->get_saved_variables();
+    const variable_list positions(s.begin() + 1, s.end());
+    const auto position_of = ctx->saved_data["position_of"].toIntVector(), offsets = ctx->saved_data["offsets"].toIntVector();
+    variable_list out(1 + grads.size() + positions.size() + 5), some;
+    std::vector<int64_t> at, off;
+    for (size_t i = 0; i < grads.size(); i++)
+      if (grads[i].defined()) {
+        some.push_back(grads[i].to((c10::ScalarType)ctx->saved_data["type"].toInt()));
+        at.push_back(position_of[i]);
+        off.push_back(offsets[i]);
+      }
+    if (some.empty()) return out;
+    const variable_list g = rotate_all(some, s[0], positions, at, off, ctx->saved_data["interleaved"].toBool(), ctx->saved_data["amplitude"].toDouble(), true);
+    for (size_t i = 0, k = 0; i < grads.size(); i++)
+      if (grads[i].defined()) out[1 + i] = g[k++];
+    return out;
+  }
+};
+void check_turns(const Tensor& turns, int64_t d, const Tensor& like) {
+  TORCH_CHECK_VALUE(turns.scalar_type() == torch::kDouble && turns.dim() == 1 && turns.is_contiguous() && turns.device() == like.device(),
+                    "turns: contiguous float64 tensor [pairs] on the tensors' device expected");
+  TORCH_CHECK_VALUE(turns.numel() >= 1 && 2 * turns.numel() <= d, "turns: between one pair and all of the head's columns expected");
+}
+std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, const std::vector<int64_t>& offsets,
+                           const std::vector<std::optional<Tensor>>& positions, bool interleaved, double amplitude) {
+  TORCH_CHECK_VALUE(!xs.empty() && offsets.size() == xs.size() && positions.size() == xs.size(), "one offset and one entry of positions per tensor expected");
+  for (const Tensor& x : xs)
+    TORCH_CHECK_VALUE(x.dim() == 4 && x.is_cuda() && x.device() == xs[0].device() && x.scalar_type() == xs[0].scalar_type() && x.size(3) == xs[0].size(3) &&
+                      (x.scalar_type() == torch::kBFloat16 || x.scalar_type() == torch::kFloat),
+                      "[B, heads, rows, d] tensors of bfloat16 or float32, of one type, d and device, expected");
+  check_turns(turns, xs[0].size(3), xs[0]);
+  variable_list xp(xs);
+  std::vector<int64_t> position_of;
+  for (size_t i = 0; i < xs.size(); i++) {
+    const auto& p = positions[i];
+    position_of.push_back(p.has_value() ? (int64_t)(xp.size() - xs.size()) : -1);
+    if (!p.has_value()) continue;
+    TORCH_CHECK_VALUE(p->scalar_type() == torch::kLong && p->device() == xs[i].device() && (p->dim() == 1 || (p->dim() == 2 && p->size(0) == xs[i].size(0))) &&
+                      p->size(-1) == xs[i].size(2), "positions: int64 [rows] or [B, rows] on the tensors' device expected");
+    xp.push_back(p->size(-1) <= 1 || p->stride(-1) == 1 ? *p : p->contiguous());
+  }
+  return Rotate::apply(turns, at::TensorList(xp), (int64_t)xs.size(), position_of, offsets, interleaved, amplitude);
+}
+
+// ---- paged: new tokens [rows, heads, d], pages [pages, kv_heads, page, d]
+void check_tokens(const Tensor& t, const Tensor& k_pages, const char* what) {
+  TORCH_CHECK_VALUE(t.dim() == 3 && t.device() == k_pages.device() && t.scalar_type() == k_pages.scalar_type() && t.size(2) == k_pages.size(3), what,
+                    ": [rows, heads, d] of the type, device and d of the pages expected");
+  TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && t.requires_grad()), what, ": the paged calls have no gradient (call them under torch.no_grad)");
+}
+// A token tensor as it is where its strides can be handed on (unit: elements that they have to be multiples of), else a copy.
+bool tokens_in_place(const Tensor& t, int64_t unit) {
+  if (t.size(2) != 1 && t.stride(2) != 1) return false;
+  if (reinterpret_cast<uintptr_t>(t.data_ptr()) % (unit * t.element_size()) != 0) return false;
+  for (int i = 0; i < 2; i++)
+    if (t.size(i) > 1 && (t.stride(i) <= 0 || t.stride(i) % unit != 0)) return false;
+  return true;
+}
+void set_token_strides(int64_t (&out)[2], const Tensor& t) {
+  out[0] = t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+  out[1] = t.size(1) > 1 ? t.stride(1) : t.size(2);
+}
+burst_paged_params describe_paged(const Tensor& k_pages, const Tensor& v_pages, const Tensor& table, const Tensor& lengths, const Tensor& starts) {
+  TORCH_CHECK_VALUE(k_pages.dim() == 4 && k_pages.is_cuda() && (k_pages.scalar_type() == torch::kBFloat16 || k_pages.scalar_type() == torch::kFloat),
+                    "k_pages: device tensor [pages, kv_heads, page, d] of bfloat16 or float32 expected");
+  TORCH_CHECK_VALUE(v_pages.scalar_type() == k_pages.scalar_type() && v_pages.device() == k_pages.device() && v_pages.sizes() == k_pages.sizes() &&
+                    v_pages.strides() == k_pages.strides(), "v_pages: like k_pages in type, sizes and strides expected");
+  TORCH_CHECK_VALUE(k_pages.size(3) == 1 || k_pages.stride(3) == 1, "pages: a contiguous last dimension expected");
+  for (const Tensor* t : {&table, &lengths, &starts})
+    TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == k_pages.device(), "table, lengths, starts: int32 tensors on the pages' device expected");
+  TORCH_CHECK_VALUE(lengths.dim() == 1 && starts.dim() == 1 && starts.size(0) == lengths.size(0) + 1 && table.dim() == 2 && table.size(0) == lengths.size(0),
+                    "table [sequences, width], lengths [sequences], starts [sequences + 1] expected");
+  TORCH_CHECK_VALUE(lengths.is_contiguous() && starts.is_contiguous() && (table.size(1) <= 1 || table.stride(1) == 1) &&
+                    (table.size(0) <= 1 || table.stride(0) >= table.size(1)), "lengths, starts and the table's rows: contiguous expected");
+  burst_paged_params p{};
+  p.sequences = (int32_t)lengths.size(0); p.kv_heads = (int32_t)k_pages.size(1); p.d = (int32_t)k_pages.size(3);
+  p.dtype = k_pages.scalar_type() == torch::kBFloat16 ? BURST_BF16 : BURST_F32;
+  p.pages = (int32_t)k_pages.size(0); p.page = (int32_t)k_pages.size(2); p.width = (int32_t)table.size(1);
+  p.starts = starts.data_ptr<int>(); p.lengths = lengths.data_ptr<int>(); p.table = table.data_ptr<int>();
+  p.table_stride = table.size(0) > 1 ? table.stride(0) : 0;
+  for (int i = 0; i < 3; i++) p.page_strides[i] = k_pages.size(i) > 1 ? k_pages.stride(i) : i == 2 ? k_pages.size(3) : k_pages.size(2) * k_pages.size(3);
+  p.scale = 1.f;
+  return p;
+}
+
+std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const Tensor& k_pages, const Tensor& v_pages, const Tensor& table,
+                                   const Tensor& lengths, const Tensor& starts, const std::optional<Tensor>& q_in, const std::optional<Tensor>& turns,
+                                   bool interleaved, double amplitude, const std::optional<Tensor>& offsets) {
+  burst_paged_params p = describe_paged(k_pages, v_pages, table, lengths, starts);
+  check_tokens(k_in, k_pages, "k");
+  check_tokens(v_in, k_pages, "v");
+  TORCH_CHECK_VALUE(k_in.size(1) == k_pages.size(1) && v_in.sizes() == k_in.sizes(), "k, v: [rows, kv_heads, d] expected");
+  TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && (k_pages.requires_grad() || v_pages.requires_grad())), "pages that require a gradient are not written");
+  if (turns.has_value()) check_turns(*turns, k_pages.size(3), k_pages);
+  if (offsets.has_value())
+    TORCH_CHECK_VALUE(offsets->scalar_type() == torch::kLong && offsets->device() == k_pages.device() && offsets->is_contiguous() &&
+                      offsets->sizes() == lengths.sizes(), "offsets: contiguous int64 [sequences] on the pages' device expected");
+  const c10::DeviceGuard on(k_pages.device());
+  Tensor k = k_in, v = v_in, q, out;
+  if (!(tokens_in_place(k, 1) && tokens_in_place(v, 1)) || (k.size(0) > 1 && k.stride(0) != v.stride(0)) || (k.size(1) > 1 && k.stride(1) != v.stride(1))) {
+    k = k.contiguous();
+    v = v.contiguous();
+  }
+  p.rows = (int32_t)k.size(0);
+  p.H = p.kv_heads;
+  set_token_strides(p.kv_strides, k);
+  if (q_in.has_value()) {
+    TORCH_CHECK_VALUE(turns.has_value(), "q without turns: there is nothing to do to it");
+    check_tokens(*q_in, k_pages, "q");
+    TORCH_CHECK_VALUE(q_in->size(0) == k.size(0) && q_in->size(1) >= 1 && q_in->size(1) % k_pages.size(1) == 0, "q: [rows, H, d] with H a multiple of kv_heads expected");
+    q = tokens_in_place(*q_in, 1) ? *q_in : q_in->contiguous();
+    out = torch::empty(q.sizes(), q.options());
+    p.H = (int32_t)q.size(1);
+    set_token_strides(p.q_strides, q);
+  }
+  burst_rotary r{};
+  if (turns.has_value()) {
+    r.turns = turns->data_ptr<double>(); r.dims = (int32_t)(2 * turns->numel()); r.interleaved = interleaved; r.amplitude = (float)amplitude;
+  }
+  check(burst_cache_append(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ptr(q), ptr(out),
+                           offsets.has_value() ? offsets->data_ptr<int64_t>() : nullptr, turns.has_value() ? &r : nullptr, &p, stream_of(k_pages)),
+        "burst_cache_append");
+  if (!q_in.has_value()) return std::nullopt;
+  return out;
+}
+
+std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_pages, const Tensor& v_pages, const Tensor& table, const Tensor& lengths,
+                                           const Tensor& starts, double scale, bool causal, int64_t window, int64_t max_new,
+                                           const std::optional<Tensor>& o_out, const std::optional<Tensor>& lse_out) {
+  burst_paged_params p = describe_paged(k_pages, v_pages, table, lengths, starts);
+  check_tokens(q_in, k_pages, "q");
+  TORCH_CHECK_VALUE(max_new >= 0 && max_new <= 0x7fffffff && window >= 0, "max_new, window: not negative expected");
+  const c10::DeviceGuard on(k_pages.device());
+  const int64_t unit = 16 / (int64_t)q_in.element_size();
+  const Tensor q = tokens_in_place(q_in, unit) ? q_in : q_in.contiguous();
+  Tensor O, lse;
+  if (o_out.has_value()) {
+    O = *o_out;
+    TORCH_CHECK_VALUE(O.device() == q.device() && O.sizes() == q.sizes() && (O.scalar_type() == q.scalar_type() || O.scalar_type() == torch::kFloat) &&
+                      tokens_in_place(O, 16 / (int64_t)O.element_size()) && (p.dtype == BURST_F32 || O.scalar_type() == torch::kFloat || tokens_in_place(O, 8)),
+                      "out: like q in sizes, of its type or float32, on 16-byte boundaries expected");
+    TORCH_CHECK_VALUE(!O.requires_grad(), "out: a tensor that needs no gradient expected");
+  } else {
+    O = torch::empty(q.sizes(), q.options());
+  }
+  if (lse_out.has_value()) {
+    lse = *lse_out;
+    TORCH_CHECK_VALUE(lse.device() == q.device() && lse.scalar_type() == torch::kFloat && lse.is_contiguous() && lse.dim() == 2 && lse.size(0) == q.size(0) &&
+                      lse.size(1) == q.size(1), "lse: contiguous float32 [rows, H] expected");
+  } else {
+    lse = torch::empty({q.size(0), q.size(1)}, q.options().dtype(torch::kFloat));
+  }
+  p.rows = (int32_t)q.size(0); p.H = (int32_t)q.size(1);
+  p.scale = (float)scale; p.causal = causal; p.window = window; p.max_new = (int32_t)max_new;
+  p.out_f32 = O.scalar_type() == torch::kFloat;
+  set_token_strides(p.q_strides, q);
+  set_token_strides(p.o_strides, O);
+  const size_t need = burst_paged_workspace_bytes(&p);
+  const Tensor ws = need ? torch::empty({(int64_t)need}, q.options().dtype(torch::kByte)) : Tensor();
+  check(burst_paged_fwd(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), O.data_ptr(), lse.data_ptr<float>(), ptr(ws), bytes(ws), &p, stream_of(q)),
+        "burst_paged_fwd");
+  return {O, lse};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("attention", &attention, pybind11::call_guard<pybind11::gil_scoped_release>());
+  m.def("rotate", &rotate, pybind11::call_guard<pybind11::gil_scoped_release>());
+  m.def("cache_append", &cache_append, pybind11::call_guard<pybind11::gil_scoped_release>());
+  m.def("paged_attention", &paged_attention, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("walk_forward", &walk_forward, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("walk_backward", &walk_backward, pybind11::call_guard<pybind11::gil_scoped_release>());
 }

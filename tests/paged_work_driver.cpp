@@ -1,0 +1,156 @@
+// The integer logic of a paged call (csrc/burst_paged.h, the same code as on the device) on the host, over random batches: ordinary
+// ones, and arrays that hold anything.  Checks that every unit of every item belongs to exactly one run, that no key
+// outside the table or the pages is named, and that the parts of a cut item are joined once, from the slots that they were written
+// to.  Built with the address and undefined-behaviour sanitizers by tests/test_paged_work.py.
+#include <cstdio>
+#include <cstdlib>
+#include <map>
+#include <set>
+#include <tuple>
+#include <vector>
+#include "burst_paged.h"
+using namespace burst;
+
+static int bad = 0;
+#define CHECK(x) do { if (!(x)) { if (bad++ < 10) std::printf("line %d: %s (case %d)\n", __LINE__, #x, g_case); } } while (0)
+static int g_case = 0;
+
+static std::vector<int> g_starts, g_lengths;
+struct HostRead {
+  static int at(const int* p, int i) {
+    const std::vector<int>& v = p == g_starts.data() ? g_starts : g_lengths;
+    return v.at((size_t)i);                        // (throws outside)
+  }
+};
+typedef PagedCursor<HostRead> Cursor;
+
+static unsigned long long g_seed = 1;
+static int rnd(int n) {
+  g_seed = g_seed * 6364136223846793005ULL + 1442695040888963407ULL;
+  return n > 0 ? (int)((g_seed >> 33) % (unsigned)n) : 0;
+}
+static int wild() { const int w[] = {-1, 0, 1, 0x7fffffff, -0x7fffffff - 1, 1 << 30, -5, 64}; return rnd(2) ? w[rnd(8)] : rnd(3000) - 100; }
+
+// as locate_run does it on the device
+static bool locate(const PagedWork& w, int runs, int run, Cursor& cur, long long& each) {
+  long long total = 0;
+  std::vector<long long> units;
+  for (int s = 0; s < w.sequences; s++) {
+    units.push_back(w.cost(cur.load(w, s)) * w.parts);
+    total += units.back();
+  }
+  each = run_length(total, runs);
+  const long long begin = each * run;
+  if (begin >= total) return false;
+  long long before = 0;
+  int s = 0;
+  while (begin >= before + units[s]) before += units[s++];
+  cur.place(w, s, begin - before, each < total - begin ? each : total - begin);
+  return true;
+}
+
+static void batch(bool anything) {
+  const int S = 1 + rnd(9), page_shift = 4 + rnd(4), width = rnd(40), cap = width << page_shift, pages = 1 + rnd(50);
+  const int group = 1 + rnd(20), item_rows = rnd(2) ? 16 : 128, heads = 1 + rnd(3);
+  g_starts.assign(S + 1, 0);
+  g_lengths.assign(S, 0);
+  for (int s = 0; s < S; s++) {
+    g_lengths[s] = anything ? wild() : rnd(4) ? rnd(cap + 1) : rnd(2);
+    g_starts[s + 1] = g_starts[s] + (rnd(4) ? rnd(4) : rnd(200));
+  }
+  const int rows = g_starts[S] + rnd(3);
+  if (anything) for (int& x : g_starts) x = rnd(2) ? x : wild();
+  std::vector<int> table((size_t)S * width);
+  for (int& x : table) x = anything || rnd(20) == 0 ? wild() : rnd(pages);
+  PagedWork w = {};
+  w.starts = g_starts.data(); w.lengths = g_lengths.data();
+  w.sequences = S; w.rows = rows; w.cap = cap;
+  w.tokens = group <= item_rows ? item_rows / group : 1;
+  const int each_head = (group + item_rows - 1) / item_rows;
+  w.parts = heads * each_head;
+  w.least = 1; w.most = 0x7fffffff;
+  if (rnd(3) == 0) { w.least = 1 + rnd(5); w.most = w.least + rnd(50); }
+  w.causal = rnd(3) != 0;
+  w.window = rnd(3) ? 0 : rnd(2) ? 1 + rnd(100) : 1LL << 40;
+  const int runs = 1 + rnd(40);
+
+  typedef std::tuple<int, int, int> Item;          // sequence, part, block
+  std::map<Item, std::vector<int>> covered;
+  std::map<Item, std::vector<int>> slots;          // of the parts, in the order of their keys
+  std::set<int> used;
+  std::map<Item, int> joins;
+  for (int run = 0; run < runs; run++) {
+    Cursor cur;
+    long long each;
+    if (!locate(w, runs, run, cur, each)) continue;
+    bool first = true;
+    do {
+      const PagedSegment& g = cur.g;
+      const Item item(g.s, g.part, g.block);
+      CHECK(g.s >= 0 && g.s < S && g.part >= 0 && g.part < w.parts && g.block >= 0 && g.block < w.blocks(g.q));
+      CHECK(g.lo <= g.from && g.from < g.to && g.to <= g.hi);
+      CHECK(g.q.first >= 0 && g.q.n > 0 && g.q.first + g.q.n <= rows && g.q.len >= 0 && g.q.len <= cap);
+      std::vector<int>& c = covered[item];
+      c.resize(g.hi - g.lo);
+      for (int u = g.from; u < g.to; u++) c[u - g.lo]++;
+      if (!g.whole()) {
+        CHECK(used.insert(partial_slot(g, run)).second);
+        CHECK(partial_slot(g, run) < 2 * runs);
+        slots[item].push_back(partial_slot(g, run));
+      }
+      for (int shift = 4; shift <= kUnitShift; shift += 2) {   // what the kernels fetch: 16 keys at a time, in one page
+        int t, end;
+        segment_tiles(w, g, shift, t, end);
+        for (; t < end; t++)
+          for (int key = t << shift; key < (t + 1) << shift; key += 16) {
+            const int there = key < g.q.len - 1 ? key : g.q.len - 1;
+            CHECK(there >= 0 && (there >> page_shift) < width);
+            const int page = checked_page(table.at((size_t)g.s * width + (there >> page_shift)), pages);
+            CHECK(page >= -1 && page < pages);
+            CHECK((key & ((1 << page_shift) - 1)) + 16 <= 1 << page_shift);
+            if (shift == 4) CHECK(key < g.q.len);
+          }
+      }
+      if (first && run > 0) {
+        const int n = parts_to_join(g, each);
+        if (n > 0) {
+          joins[item]++;
+          for (int i = 0; i < n; i++) slots[Item(-1 - g.s, g.part, g.block)].push_back(2 * (run - 1 + i) + (i == 0 ? 1 : 0));
+        }
+      }
+      first = false;
+    } while (cur.next(w));
+    CHECK(cur.left == 0);
+  }
+  for (int s = 0; s < S; s++) {
+    Cursor cur;
+    const PagedSeq q = cur.load(w, s);
+    if (!w.mine(q)) continue;
+    for (int part = 0; part < w.parts; part++)
+      for (int b = 0; b < w.blocks(q); b++) {
+        int lo, hi;
+        w.units(q, b, lo, hi);
+        const std::vector<int>& c = covered[Item(s, part, b)];
+        CHECK((int)c.size() == hi - lo);
+        for (int x : c) CHECK(x == 1);
+        const std::vector<int>&parts = slots[Item(s, part, b)], &joined = slots[Item(-1 - s, part, b)];
+        CHECK(joins[Item(s, part, b)] == (parts.empty() ? 0 : 1));
+        CHECK(parts == joined);
+      }
+  }
+  size_t items = 0;
+  for (auto& x : covered) items += !x.second.empty();
+  size_t want = 0;
+  for (int s = 0; s < S; s++) {
+    Cursor cur;
+    const PagedSeq q = cur.load(w, s);
+    if (w.mine(q)) want += (size_t)w.parts * w.blocks(q);
+  }
+  CHECK(items == want);
+}
+
+int main() {
+  for (g_case = 0; g_case < 6000; g_case++) batch(g_case % 3 == 2);
+  std::printf("work checks failed: %d\n", bad);
+  return bad != 0;
+}
