@@ -711,7 +711,7 @@ int check_paged(const burst_paged_params* p, Paged& g, bool attend) {
 }
 // The launches of burst_paged_fwd: what each takes, and its runs (as many as the chip holds, or as many units as there can be).
 struct PagedPlan { bool shorts, chunks; int least; burst::PagedArgs a[2]; size_t bytes; };
-void plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
+bool plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {   // false: more units than 32 bits count
   const int group = p->H / p->kv_heads, cap = p->width * p->page;
   const int most = p->max_new > 0 && p->max_new < p->rows ? p->max_new : p->rows;
   // A sequence whose rows fill 16 rows of an item at most is the short kernel's; longer ones the chunk kernel's (bf16).
@@ -737,15 +737,23 @@ void plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
     w.parts = p->kv_heads * a.parts_each;
     w.least = i == 0 || !plan.shorts ? 1 : fit + 1;
     w.most = i == 0 && plan.chunks ? fit : 0x7fffffff;
-    w.causal = p->causal != 0; w.window = p->window;
-    const double units = ((double)p->rows / w.tokens + p->sequences) * w.parts * (cap / burst::kUnit + 1);
+    w.causal = p->causal != 0;
+    w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
+    double units;                                  // at most so many: 32 bits hold them
+    for (w.unit_shift = burst::kTileShift;; w.unit_shift++) {
+      units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2);
+      if (units < 2e9 || w.unit_shift == 20) break;
+    }
+    if (units >= 2e9) return false;
     const int slots = i == 0 ? 1024 : 512;
     a.runs = units < slots ? (int)units : slots;
     if (a.runs < 1) a.runs = 1;
     if (a.runs > 8) a.runs &= ~7;
-    const size_t bytes = a.runs < 2 ? 0 : (size_t)2 * a.runs * rows * (p->d + 2) * sizeof(float);
+    a.slack = i == 0 ? 2 : 8;
+    const size_t bytes = a.runs < 2 ? 0 : (size_t)a.runs * (2 * rows * (p->d + 2) * sizeof(float) + sizeof(burst::PagedJoin));
     if ((i == 0 ? plan.shorts : plan.chunks) && bytes > plan.bytes) plan.bytes = bytes;
   }
+  return true;
 }
 
 }  // namespace
@@ -1215,8 +1223,7 @@ size_t burst_paged_workspace_bytes(const burst_paged_params* p) {
   Paged g;
   if (check_paged(p, g, true) != BURST_OK) return 0;
   PagedPlan plan;
-  plan_paged(p, g, plan);
-  return plan.bytes;
+  return plan_paged(p, g, plan) ? plan.bytes : 0;
 }
 
 int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,
@@ -1230,13 +1237,16 @@ int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, voi
   REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4);
   if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
   PagedPlan plan;
-  plan_paged(p, g, plan);
+  if (!plan_paged(p, g, plan)) return BURST_ERR_SHAPE;
   if (plan.bytes > 0) {
     REQUIRE_PTR(workspace);
     if (workspace_bytes < plan.bytes) return BURST_ERR_SHAPE;
   }
   if ((st = check_arch()) != BURST_OK) return st;
-  for (burst::PagedArgs& a : plan.a) { a.Q = Q; a.O = O; a.lse = lse; a.K = K_pages; a.V = V_pages; a.part = (float*)workspace; }
+  for (burst::PagedArgs& a : plan.a) {
+    a.Q = Q; a.O = O; a.lse = lse; a.K = K_pages; a.V = V_pages; a.part = (float*)workspace;
+    a.join = a.runs < 2 ? nullptr : (burst::PagedJoin*)(a.part + (size_t)2 * a.runs * (&a == plan.a ? burst::kShortRows : burst::kChunkRows) * (p->d + 2));
+  }
   hipStream_t s = (hipStream_t)stream;
   return validated([&] {
     int e = BURST_OK;

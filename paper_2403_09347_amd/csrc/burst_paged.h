@@ -24,16 +24,17 @@ BURST_HD PagedSeq paged_seq(int start, int end, int length, int rows, int cap) {
 
 // An item: a block of `tokens` tokens of a sequence with the query heads of one part of a key/value head's group.  Groups of more
 // heads than a block has rows are cut into parts of so many heads (and then a block has one token).
-// A unit: kUnit keys of an item.  An item has the units that some row of it sees, and at least one, so that rows that
-// see nothing are written too.
-constexpr int kUnitShift = 6, kUnit = 1 << kUnitShift;
+// A unit: 1 << unit_shift keys of an item (64, more only where a call could have 2^31 units).  An item has the units that some
+// row of it sees, and at least one, so that rows that see nothing are written too.
+constexpr int kTileShift = 6;                      // tiles of the chunk kernel; units are not smaller
+struct PagedTotals { int units, items, most; };    // most: units of the largest item
 struct PagedWork {
   const int* starts; const int* lengths;
   int sequences, rows, cap;          // rows of the packed tensors; keys that a row of the table has pages for
   int tokens, parts;                 // of an item; parts of all key/value heads
   int least, most;                   // sequences of fewer or more new tokens are another launch's
-  int causal;
-  long long window;
+  int causal, window;                // window: 0 = none
+  int unit_shift;
   BURST_HD bool mine(const PagedSeq& q) const { return q.n > 0 && q.n >= least && q.n <= most; }
   BURST_HD int blocks(const PagedSeq& q) const { return (q.n + tokens - 1) / tokens; }
   // keys [lo, hi) that the rows of a block see between them
@@ -42,76 +43,84 @@ struct PagedWork {
     lo = 0; hi = q.len;
     if (causal && q.len - q.n + t1 + 1 < hi) hi = q.len - q.n + t1 + 1;
     if (window > 0) {
-      const long long first = (long long)(q.len - q.n + t0) - window + 1;
-      if (first > 0) lo = first < hi ? (int)first : hi;
+      const int first = q.len - q.n + t0 - window + 1;   // (all of them below 2^30)
+      if (first > 0) lo = first < hi ? first : hi;
     }
     if (hi < lo) hi = lo;
   }
   BURST_HD void units(const PagedSeq& q, int block, int& lo, int& hi) const {
     int k0, k1;
     keys(q, block, k0, k1);
-    lo = k0 >> kUnitShift;
-    hi = k1 > k0 ? ((k1 - 1) >> kUnitShift) + 1 : lo + 1;
+    lo = k0 >> unit_shift;
+    hi = k1 > k0 ? ((k1 - 1) >> unit_shift) + 1 : lo + 1;
   }
-  // units of all blocks of a sequence, for one part of a head
-  BURST_HD long long cost(const PagedSeq& q) const {
-    if (!mine(q)) return 0;
-    long long sum = 0;
+  // all blocks of a sequence, for one part of a head
+  BURST_HD PagedTotals totals(const PagedSeq& q) const {
+    PagedTotals t = {0, 0, 0};
+    if (!mine(q)) return t;
     const int n = blocks(q);
+    t.items = n;
     for (int b = 0; b < n; b++) {
       int lo, hi;
       units(q, b, lo, hi);
-      sum += hi - lo;
+      t.units += hi - lo;
+      if (hi - lo > t.most) t.most = hi - lo;
     }
-    return sum;
+    return t;
   }
 };
 
-// A run: the units [at, at + left) of the sequence that the parts, blocks and units of all sequences make (sequence, part, block, unit,
-// the last one fastest).  Runs of a launch have the same length, the last one excepted.
-BURST_HD long long run_length(long long total, int runs) {
-  const long long n = (total + runs - 1) / runs;
-  return n > 0 ? n : 1;
+// How the parts, blocks and units of all sequences (sequence, part, block, unit, the last one fastest) are dealt out to runs: `each` units a
+// run, the same number wherever it begins, or, where that costs less, `each` whole items, of which nothing has to be joined.
+// `slack`: the units that a run may have more for that.
+struct PagedDeal { int each, by_items; };
+BURST_HD PagedDeal paged_deal(const PagedTotals& t, int runs, int slack) {
+  PagedDeal d;
+  const int each = (int)(((unsigned)t.units + runs - 1) / (unsigned)runs), per = (int)(((unsigned)t.items + runs - 1) / (unsigned)runs);
+  d.by_items = (long long)per * t.most <= each + each / 16 + slack;
+  d.each = d.by_items ? per : each;
+  if (d.each < 1) d.each = 1;
+  return d;
 }
 // A run's part of one item.
 struct PagedSegment {
   PagedSeq q;
-  int s, part, block;
+  int part, block;
   int lo, hi;                        // the item's units
   int from, to;                      // those of this segment
   BURST_HD bool whole() const { return from == lo && to == hi; }
 };
-// Read: element i of one of the caller's arrays (device: by a scalar load).
+// Where a run is.  Read: element i of one of the caller's arrays (device: by a scalar load).
 template <typename Read>
 struct PagedCursor {
   PagedSegment g;
-  long long left;
-  int skip;                          // units of the item before the segment
-  BURST_HD PagedSeq load(const PagedWork& w, int s) const {
+  int s;                             // sequence
+  int left;                          // units (items) of the run behind the segment
+  int by_items;
+  static BURST_HD PagedSeq load(const PagedWork& w, int s) {
     return paged_seq(Read::at(w.starts, s), Read::at(w.starts, s + 1), Read::at(w.lengths, s), w.rows, w.cap);
   }
-  // the place `rem` units into sequence s (rem < its units)
-  BURST_HD void place(const PagedWork& w, int s, long long rem, long long run) {
-    g.s = s;
-    g.q = load(w, s);
-    const long long one = w.cost(g.q);
-    g.part = (int)(rem / one);
+  // the place `rem` units (items) into sequence s, which has more of them (`one` for each part of a head)
+  BURST_HD void place(const PagedWork& w, int at, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run) {
+    by_items = d.by_items;
+    s = at;
+    g.q = q;
+    g.part = (int)((unsigned)rem / (unsigned)one);
     rem -= g.part * one;
-    g.block = 0;
+    g.block = by_items ? rem : 0;
     for (;;) {
       w.units(g.q, g.block, g.lo, g.hi);
-      if (rem < g.hi - g.lo) break;
+      if (by_items || rem < g.hi - g.lo) break;
       rem -= g.hi - g.lo;
       g.block++;
     }
-    skip = (int)rem;
     left = run;
-    cut();
+    cut(by_items ? 0 : rem);
   }
-  BURST_HD void cut() {
+  BURST_HD void cut(int skip) {
     g.from = g.lo + skip;
-    g.to = left < g.hi - g.from ? g.from + (int)left : g.hi;
-    left -= g.to - g.from;
+    g.to = !by_items && left < g.hi - g.from ? g.from + left : g.hi;
+    left -= by_items ? 1 : g.to - g.from;
   }
   // the run's next segment; false: there is none
   BURST_HD bool next(const PagedWork& w) {
@@ -121,39 +130,40 @@ struct PagedCursor {
       if (++g.part >= w.parts) {
         g.part = 0;
         do {
-          if (++g.s >= w.sequences) return false;
-          g.q = load(w, g.s);
+          if (++s >= w.sequences) return false;
+          g.q = load(w, s);
         } while (!w.mine(g.q));
       }
     }
     w.units(g.q, g.block, g.lo, g.hi);
-    skip = 0;
-    cut();
+    cut(0);
     return true;
   }
 };
-
-// The tiles of 1 << shift keys (shift <= kUnitShift) of a segment that hold a key which some row of its item sees: [first, end).  All of them
-// begin before the end of the sequence, and so within the pages of its table row.
+// The tiles of 1 << shift keys (shift <= unit_shift) of a segment that hold a key which some row of its item sees: [first, end).  A segment
+// without any has one tile all the same (its rows are written), the only one that may begin at the end of the sequence or behind it.
 BURST_HD void segment_tiles(const PagedWork& w, const PagedSegment& g, int shift, int& first, int& end) {
   int k0, k1;
   w.keys(g.q, g.block, k0, k1);
-  const int u = kUnitShift - shift, e = (k1 + (1 << shift) - 1) >> shift;
+  const int u = w.unit_shift - shift, e = (k1 + (1 << shift) - 1) >> shift;
   first = k0 >> shift > g.from << u ? k0 >> shift : g.from << u;
   end = e < g.to << u ? e : g.to << u;
+  if (end <= first) end = first + 1;
 }
 // Where a run leaves the partial results of an item that is not all its own: the first part of an item is its run's last segment, every
 // other part its run's first one.
 BURST_HD int partial_slot(const PagedSegment& g, int run) { return 2 * run + (g.from == g.lo ? 1 : 0); }
 // The number of parts (from run - 1 on) of the item that a run's first segment `g` belongs to, if this run is the first one that starts inside
 // it; else 0.
-BURST_HD int parts_to_join(const PagedSegment& g, long long run_units) {
+BURST_HD int parts_to_join(const PagedSegment& g, int run_units) {
   const int before = g.from - g.lo;
   if (before == 0 || before > run_units) return 0;
-  return 2 + (int)((g.hi - g.from - 1) / run_units);
+  return 2 + (g.hi - g.from - 1) / run_units;
 }
 
 // An entry of the page table, or -1 if it is no page.
 BURST_HD int checked_page(int page, int pages) { return page >= 0 && page < pages ? page : -1; }
+// The entry of a table row to read for the 16 keys from `key` on; -1: none, they are behind the sequence's end.
+BURST_HD int table_entry(int key, int len, int page_shift) { return key < len ? key >> page_shift : -1; }
 
 }  // namespace burst

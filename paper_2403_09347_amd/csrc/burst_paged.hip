@@ -26,24 +26,22 @@ __device__ __forceinline__ bool is_zero(float x) { return (__builtin_bit_cast(un
 
 // An item's row: its token and query head, if it has one.
 struct ItemRow { bool there; int token, head; };
-__device__ __forceinline__ ItemRow item_row(const PagedArgs& a, const PagedSegment& g, int r) {
-  const int kvhead = g.part / a.parts_each, part = g.part - kvhead * a.parts_each;
+__device__ __forceinline__ ItemRow item_row(const PagedArgs& a, int of_heads, int block, int tokens, int r) {
+  const int kvhead = of_heads / a.parts_each, part = of_heads - kvhead * a.parts_each;
   const int t = r / a.part_heads, j = part * a.part_heads + r - t * a.part_heads;
   ItemRow x;
-  x.token = g.block * a.w.tokens + t;
+  x.token = block * a.w.tokens + t;
   x.head = kvhead * a.group + j;
-  x.there = t < a.w.tokens && x.token < g.q.n && j < a.group;
+  x.there = t < a.w.tokens && x.token < tokens && j < a.group;
   return x;
 }
+__device__ __forceinline__ ItemRow item_row(const PagedArgs& a, const PagedSegment& g, int r) { return item_row(a, g.part, g.block, g.q.n, r); }
 // The keys [lo, hi] that a token sees
 struct KeyRange { int lo, hi; };
 __device__ __forceinline__ KeyRange seen_keys(const PagedWork& w, const PagedSeq& q, int token) {
   const int pos = q.len - q.n + token;
   KeyRange k = {0, w.causal ? min(pos, q.len - 1) : q.len - 1};
-  if (w.window > 0) {
-    const long long first = (long long)pos - w.window + 1;
-    k.lo = first > 0 ? (int)min(first, (long long)0x7fffffff) : 0;
-  }
+  if (w.window > 0) k.lo = max(0, pos - w.window + 1);
   return k;
 }
 
@@ -83,20 +81,20 @@ __device__ __forceinline__ float row_lse(float m, float l) { return is_zero(l) ?
 // Rows whose accumulators came out infinite or NaN, by themselves with scalar products of the visible pairs only: a matrix product
 // multiplies hidden pairs too (by a probability of 0, and 0 x inf is NaN).  One wavefront, one row at a time.
 template <typename T>
-__device__ __forceinline__ void row_again(const PagedArgs& a, const PagedSegment& g, int run, int rows_of_item, int r, int lane) {
+__device__ __forceinline__ void row_again(const PagedArgs& a, const PagedSegment& g, int s_of, int run, int rows_of_item, int r, int lane) {
   const ItemRow x = item_row(a, g, r);
   if (!x.there) return;
   const int d = a.d, kvhead = g.part / a.parts_each;
   const T* const q = (const T*)a.Q + (size_t)(g.q.first + x.token) * a.q_row + (size_t)x.head * a.q_head;
   KeyRange k = seen_keys(a.w, g.q, x.token);
-  k.lo = max(k.lo, g.from << kUnitShift);
-  k.hi = min(k.hi, (g.to << kUnitShift) - 1);
+  k.lo = max(k.lo, g.from << a.w.unit_shift);
+  k.hi = min(k.hi, (g.to << a.w.unit_shift) - 1);
   float m = BURST_NEG_INF, l = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll 1
   for (int k0 = k.lo; k0 <= k.hi; k0 += 64) {
     const int key = k0 + lane;
     int page = -1;
-    if (key <= k.hi) page = checked_page(a.table[(long long)g.s * a.table_stride + (key >> a.page_shift)], a.pages);
+    if (key <= k.hi) page = checked_page(a.table[(long long)s_of * a.table_stride + (key >> a.page_shift)], a.pages);
     const bool seen = page >= 0;
     const long long row = (long long)page * a.p_page + (long long)kvhead * a.p_head + (long long)(key & ((1 << a.page_shift) - 1)) * a.p_row;
     float s = 0.f;
@@ -175,61 +173,56 @@ paged_short_kernel(PagedArgs a) {
   constexpr int RPL = 1024 / ROWB, NL = TILE / 1024, LOADS = 2 * NL;   // rows of a load; loads of K, of a stage
   constexpr int KS = GR / 4;                       // granule steps of a product over d
   constexpr int OB = D / 16;                       // 16-column blocks of O^T
-  static_assert(NST >= 2 && (NST - 1) * LOADS < 64, "the ring fits LDS and the counter of loads");
+  constexpr int NSEG = 16;                         // segments on their way: at most one a stage, and the one at work
+  static_assert(NST >= 2 && NST < NSEG && (NST - 1) * LOADS < 64, "the ring fits LDS and the counter of loads");
   __shared__ __attribute__((aligned(16))) char smem[NST * 2 * TILE];
+  __shared__ i32x4 segs[NSEG][3];
   const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
   const int run = run_of(blockIdx.x, a.runs);
-  DeviceCursor cur;
-  if (!locate_run(a, run, lane, cur)) return;
-  DeviceCursor fet = cur;
+  DeviceCursor fet;
+  if (!start_run(a, run, lane, lane == 0, fet)) return;
   const unsigned lds0 = lds_addr(smem);
   const int d = a.d;
+  const unsigned pitch = (unsigned)(a.p_row * sizeof(T)), row_bytes = (unsigned)(d * sizeof(T));
+  const long long v_off = (const char*)a.V - (const char*)a.K;
 
   int goff[NL];
 #pragma unroll
   for (int i = 0; i < NL; i++) {
     const int row = i * RPL + lane / GR, granule = (lane % GR) ^ short_code<GR>(row);
-    goff[i] = granule * (16 / (int)sizeof(T)) < d ? row * (int)(a.p_row * sizeof(T)) + granule * 16 : (int)0x80000000u;
+    goff[i] = granule * (16 / (int)sizeof(T)) < d ? row * (int)pitch + granule * 16 : (int)0x80000000u;
   }
-  const unsigned pitch = (unsigned)(a.p_row * sizeof(T)), row_bytes = (unsigned)(d * sizeof(T));
-
-  // The fetching side.  `page` is that of stage f_at, asked for one fetch ahead.
-  int f_at, f_end, page = -1;
-  bool f_more = true;
-  auto page_of = [&](int stage) __attribute__((always_inline)) {
-    return scalar_at(a.table, (long long)fet.g.s * a.table_stride + ((stage << 4) >> a.page_shift));
+  // The fetching side: stages [f_at, f_end) of fet.g are still to be asked for; the lanes hold the places of the 64 stages from f_base on.
+  int f_at, f_end, f_base, seg_in = 0;
+  int where_lo, where_hi;
+  unsigned long long pages = 0;                    // those of the 64 that have a page
+  auto look_up = [&]() __attribute__((always_inline)) {
+    const PagedArgs& b = args_again<PagedArgs>();
+    const int key = (f_at + lane) << 4, entry = table_entry(key, fet.g.q.len, b.page_shift);
+    int page = -1;
+    if (entry >= 0) page = checked_page(b.table[(long long)fet.s * b.table_stride + entry], b.pages);
+    const long long at = (long long)max(page, 0) * b.p_page + (long long)((unsigned)fet.g.part / (unsigned)b.parts_each) * b.p_head +
+                         (long long)(key & ((1 << b.page_shift) - 1)) * b.p_row;
+    const long long where = (long long)(size_t)b.K + at * (long long)sizeof(T);
+    where_lo = (int)where; where_hi = (int)(where >> 32);
+    pages = __builtin_amdgcn_ballot_w64(page >= 0);
+    f_base = f_at;
   };
-  auto settle = [&]() __attribute__((always_inline)) {   // f_at to the next stage there is
-    while (f_at >= f_end) {
-      if (!fet.next(a.w)) { f_more = false; return; }
-      segment_tiles(a.w, fet.g, 4, f_at, f_end);
+  auto enter = [&]() __attribute__((always_inline)) {
+    segment_tiles(args_again<PagedArgs>().w, fet.g, 4, f_at, f_end);
+    if (lane == 0) {
+      i32x4* const to = segs[seg_in % NSEG];
+      to[0] = i32x4{fet.g.q.first, fet.g.q.n, fet.g.q.len, fet.g.part};
+      to[1] = i32x4{fet.g.block, fet.g.from, fet.g.to, fet.s};
+      to[2] = i32x4{f_at, f_end, fet.g.whole() ? 1 : 0, fet.g.from == fet.g.lo ? 1 : 0};
     }
-    page = page_of(f_at);
+    seg_in++;
+    look_up();
   };
-  segment_tiles(a.w, fet.g, 4, f_at, f_end);
-  settle();
-  unsigned bad = 0;                                // stages of the ring whose page is none
+  enter();
+  unsigned gone = 0;                               // stages of the ring without a page
   int f_slot = 0, ahead = 0;                       // slot that is filled next; stages asked for and not yet used
-  auto fetch = [&]() __attribute__((always_inline)) {
-    if (!f_more) return;
-    const int key0 = f_at << 4, ok = checked_page(page, a.pages), kvhead = fet.g.part / a.parts_each;
-    const int rows = ok >= 0 ? min(16, fet.g.q.len - key0) : 0;
-    const long long at = (long long)max(ok, 0) * a.p_page + (long long)kvhead * a.p_head + (long long)(key0 & ((1 << a.page_shift) - 1)) * a.p_row;
-    const unsigned span = rows > 0 ? (unsigned)(rows - 1) * pitch + row_bytes : 0u;
-    const __amdgpu_buffer_rsrc_t krs = make_rsrc((const T*)a.K + at, span), vrs = make_rsrc((const T*)a.V + at, span);
-    const unsigned to = lds0 + (unsigned)f_slot * (2 * TILE);
-#pragma unroll
-    for (int i = 0; i < NL; i++) dma_b128_to_lds(krs, to + i * 1024u, goff[i]);
-#pragma unroll
-    for (int i = 0; i < NL; i++) dma_b128_to_lds(vrs, to + TILE + i * 1024u, goff[i]);
-    bad = ok >= 0 ? bad & ~(1u << f_slot) : bad | (1u << f_slot);
-    f_slot = f_slot + 1 == NST ? 0 : f_slot + 1;
-    ahead++;
-    f_at++;
-    settle();
-  };
-#pragma unroll 1
-  for (int i = 0; i < NST; i++) fetch();
+  bool more = true;
 
   // addresses of the operands in a tile
   int kaddr[KS], vaddr[F32 ? GR / 16 : OB];
@@ -240,131 +233,174 @@ paged_short_kernel(PagedArgs a) {
 #pragma unroll
     for (int ob = 0; ob < OB; ob++) vaddr[ob] = row * ROWB + (((2 * ob + ((r & 3) >> 1)) ^ short_code<GR>(row)) << 4) + (r & 1) * 8;
   }
-  int slot = 0;
-  do {
-    const PagedSegment& s = cur.g;
-    const ItemRow x = item_row(a, s, r);
-    const KeyRange see = seen_keys(a.w, s.q, x.token);
-    i32x4 q[KS];
-    {
-      const T* const qr = (const T*)a.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * a.q_row + (size_t)(x.there ? x.head : 0) * a.q_head;
+  // The segment at work
+  PagedSegment s = {};
+  int seg_s = 0, seg_out = 0, st = 0, end = 0, slot = 0;
+  ItemRow x = {};
+  KeyRange see = {}, all = {};                     // keys of the lane's row; keys that every row sees
+  i32x4 q[KS];
+  f32x4 o[OB];
+  float m = BURST_NEG_INF, l = 0.f;                // the row's reference (natural units); its sum over this lane's keys
+#pragma unroll 1
+  for (;;) {
+#pragma unroll 1
+    while (ahead < NST && more) {                  // (one stage a turn once the ring is full)
+      if (f_at == f_end) {
+        if (!fet.next(args_again<PagedArgs>().w)) { more = false; break; }
+        enter();
+      } else if (f_at - f_base == 64) {
+        look_up();
+      }
+      const int i = f_at - f_base;
+      const bool ok = ((pages >> i) & 1) != 0;
+      const int rows = ok ? min(16, fet.g.q.len - (f_at << 4)) : 0;
+      const unsigned span = rows > 0 ? (unsigned)(rows - 1) * pitch + row_bytes : 0u;
+      const long long at = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane(where_hi, i) << 32) |
+                                       (unsigned)__builtin_amdgcn_readlane(where_lo, i));
+      const __amdgpu_buffer_rsrc_t krs = make_rsrc((const void*)at, span), vrs = make_rsrc((const void*)(at + v_off), span);
+      const unsigned to = lds0 + (unsigned)f_slot * (2 * TILE);
+#pragma unroll
+      for (int k = 0; k < NL; k++) dma_b128_to_lds(krs, to + k * 1024u, goff[k]);
+#pragma unroll
+      for (int k = 0; k < NL; k++) dma_b128_to_lds(vrs, to + TILE + k * 1024u, goff[k]);
+      gone = ok ? gone & ~(1u << f_slot) : gone | (1u << f_slot);
+      f_slot = f_slot + 1 == NST ? 0 : f_slot + 1;
+      ahead++;
+      f_at++;
+    }
+    if (ahead == 0) break;
+    if (st == end) {                               // the next segment
+      const PagedArgs& b = args_again<PagedArgs>();
+      const i32x4 *const from = segs[seg_out % NSEG], d0 = from[0], d1 = from[1], d2 = from[2];
+      auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+      seg_out++;
+      s.q = PagedSeq{one(d0[0]), one(d0[1]), one(d0[2])};
+      s.part = one(d0[3]); s.block = one(d1[0]); s.from = one(d1[1]); s.to = one(d1[2]);
+      seg_s = one(d1[3]);
+      st = one(d2[0]); end = one(d2[1]);
+      s.lo = one(d2[3]) ? s.from : s.from - 1;     // (as far as whole() and partial_slot() look at them)
+      s.hi = one(d2[2]) ? s.to : s.to + 1;
+      x = item_row(b, s, r);
+      see = seen_keys(b.w, s.q, x.token);
+      const T* const qr = (const T*)b.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * b.q_row + (size_t)(x.there ? x.head : 0) * b.q_head;
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) {
         const int c = (4 * ks + g) * (16 / (int)sizeof(T));
         q[ks] = x.there && c < d ? *reinterpret_cast<const i32x4*>(qr + c) : i32x4{0, 0, 0, 0};
       }
+#pragma unroll
+      for (int b = 0; b < OB; b++) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m = BURST_NEG_INF; l = 0.f;
+      const int t0 = s.block * b.w.tokens, t1 = min(s.q.n, t0 + b.w.tokens) - 1;
+      all = KeyRange{seen_keys(b.w, s.q, t1).lo, seen_keys(b.w, s.q, t0).hi};
     }
-    f32x4 o[OB];
+    if (ahead == NST) wait_loads<(NST - 1) * LOADS>();
+    else wait_loads<0>();
+    const char* const kl = smem + slot * (2 * TILE);
+    const char* const vl = kl + TILE;
+    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int b = 0; b < OB; b++) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = BURST_NEG_INF, l = 0.f;              // the row's reference (natural units); its sum over this lane's keys
-    const int t0 = s.block * a.w.tokens, t1 = min(s.q.n, t0 + a.w.tokens) - 1;
-    const KeyRange all = {seen_keys(a.w, s.q, t1).lo, seen_keys(a.w, s.q, t0).hi};   // seen by every row
-    int st, end;
-    segment_tiles(a.w, s, 4, st, end);
-#pragma unroll 1
-    for (; st < end; st++) {
-      if (ahead == NST) wait_loads<(NST - 1) * LOADS>();
-      else wait_loads<0>();
-      const char* const kl = smem + slot * (2 * TILE);
-      const char* const vl = kl + TILE;
-      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+    for (int ks = 0; ks < KS; ks++) {
+      const i32x4 k = *reinterpret_cast<const i32x4*>(kl + kaddr[ks]);
+      if constexpr (F32) {
+        const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q[ks]);
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) {
-        const i32x4 k = *reinterpret_cast<const i32x4*>(kl + kaddr[ks]);
-        if constexpr (F32) {
-          const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q[ks]);
-#pragma unroll
-          for (int j = 0; j < 4; j++) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j], qf[j], sc, 0, 0, 0);
-        } else {
-          sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[ks]), sc, 0, 0, 0);
-        }
+        for (int j = 0; j < 4; j++) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j], qf[j], sc, 0, 0, 0);
+      } else {
+        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[ks]), sc, 0, 0, 0);
       }
-      const int key0 = st << 4;
-      const bool gone = ((bad >> slot) & 1) != 0;
+    }
+    const int key0 = st << 4;
+    const bool none = ((gone >> slot) & 1) != 0;
 #pragma unroll
-      for (int j = 0; j < 4; j++) sc[j] = product(sc[j], a.scale);
-      if (gone || key0 < all.lo || key0 + 15 > all.hi) {
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const int key = key0 + 4 * g + j;
-          if (gone || key < see.lo || key > see.hi) sc[j] = BURST_NEG_INF;
-        }
-      }
-      const float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
-      // A row's first reference, or one that has been exceeded by more than a factor of e^8 (P is then still a bf16 with
-      // all its bits, and l far from its range's end).
-      if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
-        const float to = fmaxf(m, max_over_groups(mx)), alpha = fast_exp2((m - (to == BURST_NEG_INF ? 0.f : to)) * kLog2e);
-        m = to;
-        l *= alpha;
-#pragma unroll
-        for (int b = 0; b < OB; b++) o[b] *= alpha;
-      }
-      const float ref = m == BURST_NEG_INF ? 0.f : m;
-      float p[4];
+    for (int j = 0; j < 4; j++) sc[j] = product(sc[j], a.scale);
+    if (none || key0 < all.lo || key0 + 15 > all.hi) {
 #pragma unroll
       for (int j = 0; j < 4; j++) {
-        p[j] = fast_exp2((sc[j] - ref) * kLog2e);
-        l += p[j];
+        const int key = key0 + 4 * g + j;
+        if (none || key < see.lo || key > see.hi) sc[j] = BURST_NEG_INF;
       }
-      if constexpr (F32) {                         // block 4 half + c: columns 64 half + 4 (lane % 16) + c of V
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-          for (int half = 0; half < GR / 16; half++) {
-            const int row = 4 * g + j;
-            const f32x4 v = *reinterpret_cast<const f32x4*>(vl + row * ROWB + (((r + 16 * half) ^ short_code<GR>(row)) << 4));
-#pragma unroll
-            for (int c = 0; c < 4; c++) o[4 * half + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[c], p[j], o[4 * half + c], 0, 0, 0);
-          }
-      } else {
-        bf16x4 pb;
-#pragma unroll
-        for (int j = 0; j < 4; j++) pb[j] = (bf16)p[j];
-#pragma unroll
-        for (int b = 0; b < OB; b++)
-          o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, lds_read_tr(vl, vaddr[b])), __builtin_bit_cast(s16x4, pb), o[b], 0, 0, 0);
-      }
-      wait_lds();                                  // (the tile has been read: its slot is filled again)
-      ahead--;
-      slot = slot + 1 == NST ? 0 : slot + 1;
-      fetch();
     }
+    const float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+    // A row's first reference, or one that has been exceeded by more than a factor of e^8 (l stays far from its range's end).
+    if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
+      const float to = fmaxf(m, max_over_groups(mx)), alpha = fast_exp2((m - (to == BURST_NEG_INF ? 0.f : to)) * kLog2e);
+      m = to;
+      l *= alpha;
+#pragma unroll
+      for (int b = 0; b < OB; b++) o[b] *= alpha;
+    }
+    const float ref = m == BURST_NEG_INF ? 0.f : m;
+    float p[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      p[j] = fast_exp2((sc[j] - ref) * kLog2e);
+      l += p[j];
+    }
+    if constexpr (F32) {                           // block 4 half + c: columns 64 half + 4 (lane % 16) + c of V
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+#pragma unroll
+        for (int half = 0; half < GR / 16; half++) {
+          const int row = 4 * g + j;
+          const f32x4 v = *reinterpret_cast<const f32x4*>(vl + row * ROWB + (((r + 16 * half) ^ short_code<GR>(row)) << 4));
+#pragma unroll
+          for (int c = 0; c < 4; c++) o[4 * half + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[c], p[j], o[4 * half + c], 0, 0, 0);
+        }
+    } else {                                       // P in two terms, 16 bits of it: the second products are not what bounds these calls
+      bf16x4 p0, p1;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        p0[j] = (bf16)p[j];
+        p1[j] = (bf16)(p[j] - (float)p0[j]);
+      }
+#pragma unroll
+      for (int b = 0; b < OB; b++) {
+        const s16x4 v = __builtin_bit_cast(s16x4, lds_read_tr(vl, vaddr[b]));
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(s16x4, p1), o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(s16x4, p0), o[b], 0, 0, 0);
+      }
+    }
+    wait_lds();                                    // (the tile has been read: its slot is filled again)
+    ahead--;
+    slot = slot + 1 == NST ? 0 : slot + 1;
+    if (++st < end) continue;
+
+    const PagedArgs& b = args_again<PagedArgs>();
     l = sum_over_groups(l);
     unsigned most = larger_of(0, l);
 #pragma unroll
-    for (int b = 0; b < OB; b++)
+    for (int k = 0; k < OB; k++)
 #pragma unroll
-      for (int j = 0; j < 4; j++) most = larger_of(most, o[b][j]);
+      for (int j = 0; j < 4; j++) most = larger_of(most, o[k][j]);
     const unsigned long long bal = __builtin_amdgcn_ballot_w64(x.there && most >= kInfBits);
     unsigned redo = (unsigned)(bal | (bal >> 16) | (bal >> 32) | (bal >> 48)) & 0xffffu;
     if (x.there && !((redo >> r) & 1)) {
-      const RowPlace at = row_place(a, s, run, 16, r, x);
+      const RowPlace at = row_place(b, s, run, kShortRows, r, x);
       const float inv = is_zero(l) ? 0.f : 1.f / l;
 #pragma unroll
-      for (int b = 0; b < OB; b++) {
+      for (int k = 0; k < OB; k++) {
         f32x4 v;
         int c;
-        if constexpr (F32) {                       // block b of lane group g: row 4g + j of block 4 half + i holds column 64 half + 16 g + 4 j + i
-          const int half = b >> 2, j = b & 3;
+        if constexpr (F32) {                       // row 4g + j of block 4 half + i holds column 64 half + 16 g + 4 j + i
+          const int half = k >> 2, j = k & 3;
           c = 64 * half + 16 * g + 4 * j;
           v = f32x4{o[4 * half][j], o[4 * half + 1][j], o[4 * half + 2][j], o[4 * half + 3][j]};
         } else {
-          c = 16 * b + 4 * g;
-          v = o[b];
+          c = 16 * k + 4 * g;
+          v = o[k];
         }
         if (c >= d) continue;
-        if (at.whole) store4(a, at.o + c, v * inv);
+        if (at.whole) store4(b, at.o + c, v * inv);
         else *reinterpret_cast<f32x4*>(at.part + c) = v;
       }
       if (g == 0) {
-        if (at.whole) a.lse[at.lse] = row_lse(m, l);
-        else { at.ml[0] = m; at.ml[16] = l; }
+        if (at.whole) b.lse[at.lse] = row_lse(m, l);
+        else { at.ml[0] = m; at.ml[kShortRows] = l; }
       }
     }
-    for (; redo != 0; redo &= redo - 1) row_again<T>(a, s, run, 16, __builtin_ctz(redo), lane);
-  } while (cur.next(a.w));
+    for (; redo != 0; redo &= redo - 1) row_again<T>(b, s, seg_s, run, kShortRows, __builtin_ctz(redo), lane);
+  }
 }
 
 // ------------------------------------------------------------------------------- chunk
@@ -373,69 +409,77 @@ paged_short_kernel(PagedArgs a) {
 // O^T += V^T P^T as it stands.  A wavefront fetches 16 keys of every tile, which lie in one page.  Two workgroups a CU, so that one's
 // vector work overlaps the other's matrix work.
 // Scores and references are in log2 units (one fma an exponent), as in the d = 64 and d = 128 kernels of the walks.
+constexpr int kTile = 1 << kTileShift;             // keys
 template <int D>
 __device__ __forceinline__ int chunk_code(int row) { return D == 64 ? (row >> 1) & 7 : row_code(row); }
 template <int D>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_kernel(PagedArgs a) {
-  constexpr int ROWB = 2 * D, GR = ROWB / 16, RPL = 1024 / ROWB, NL = 16 / RPL, TILE = kUnit * ROWB;
+  constexpr int ROWB = 2 * D, GR = ROWB / 16, RPL = 1024 / ROWB, NL = 16 / RPL, TILE = kTile * ROWB;
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
   const int lane = threadIdx.x & 63, lr = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int run = run_of(blockIdx.x, a.runs);
-  DeviceCursor cur;
-  if (!locate_run(a, run, lane, cur)) return;
-  DeviceCursor fet = cur;
-  const unsigned lds0 = lds_addr(smem);
+  DeviceCursor fet;
+  if (!start_run(a, run, lane, threadIdx.x == 0, fet)) return;
+  const unsigned lds0 = lds_addr(smem) + (unsigned)(w * NL) * 1024u;
   const int d = a.d;
   const unsigned pitch = (unsigned)(a.p_row * 2), row_bytes = (unsigned)(d * 2);
+  const long long v_off = (const char*)a.V - (const char*)a.K;
   int goff[NL];
 #pragma unroll
   for (int i = 0; i < NL; i++) {
     const int row = i * RPL + lane / GR, granule = (lane % GR) ^ chunk_code<D>(row);
     goff[i] = granule * 8 < d ? row * (int)pitch + granule * 16 : (int)0x80000000u;
   }
-
-  // The fetching side, a tile ahead; the pages of its next tile's four groups of 16 keys.
-  int f_at, f_end, page[4] = {-1, -1, -1, -1};
-  bool f_more = true;
-  auto settle = [&]() __attribute__((always_inline)) {
-    while (f_at >= f_end) {
-      if (!fet.next(a.w)) { f_more = false; return; }
-      segment_tiles(a.w, fet.g, kUnitShift, f_at, f_end);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-      page[i] = scalar_at(a.table, (long long)fet.g.s * a.table_stride + (min((f_at << kUnitShift) + 16 * i, fet.g.q.len - 1) >> a.page_shift));
+  // The fetching side, a tile ahead: tiles [f_at, f_end) of fet.g are still to be asked for; the lanes hold the places of the 64 groups of
+  // 16 keys of the 16 tiles from f_base on.
+  int f_first, f_at, f_end, f_base;
+  int where_lo, where_hi;
+  unsigned long long pages = 0;                    // those of the 64 groups that have a page
+  auto look_up = [&]() __attribute__((always_inline)) {
+    const PagedArgs& b = args_again<PagedArgs>();
+    const int key = (f_at << kTileShift) + 16 * lane, entry = table_entry(key, fet.g.q.len, b.page_shift);
+    int page = -1;
+    if (entry >= 0) page = checked_page(b.table[(long long)fet.s * b.table_stride + entry], b.pages);
+    const long long at = (long long)max(page, 0) * b.p_page + (long long)((unsigned)fet.g.part / (unsigned)b.parts_each) * b.p_head +
+                         (long long)(key & ((1 << b.page_shift) - 1)) * b.p_row;
+    const long long where = (long long)(size_t)b.K + at * 2;
+    where_lo = (int)where; where_hi = (int)(where >> 32);
+    pages = __builtin_amdgcn_ballot_w64(page >= 0);
+    f_base = f_at;
   };
-  segment_tiles(a.w, fet.g, kUnitShift, f_at, f_end);
-  settle();
-  unsigned bad = 0;                                // four bits a buffer: groups of keys whose page is none
+  auto enter = [&]() __attribute__((always_inline)) {
+    segment_tiles(args_again<PagedArgs>().w, fet.g, kTileShift, f_at, f_end);
+    f_first = f_at;
+    look_up();
+  };
+  enter();
+  unsigned gone = 0;                               // four bits a buffer: groups of keys without a page
+  bool more = true;                                // fet.g is the segment of the tile that was asked for last
   auto fetch = [&](int buf) __attribute__((always_inline)) {
-    if (!f_more) return;
-    unsigned none = 0;
-    int mine = -1;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int ok = checked_page(page[i], a.pages);
-      if (ok < 0) none |= 1u << i;
-      if (i == w) mine = ok;
+    if (f_at == f_end) {
+      if (!more || !fet.next(args_again<PagedArgs>().w)) { more = false; return; }
+      enter();
+    } else if (f_at - f_base == 16) {
+      look_up();
     }
-    const int key0 = (f_at << kUnitShift) + 16 * w, kvhead = fet.g.part / a.parts_each;
-    const int rows = mine >= 0 ? __builtin_amdgcn_readfirstlane(max(0, min(16, fet.g.q.len - key0))) : 0;
-    const long long at = (long long)max(mine, 0) * a.p_page + (long long)kvhead * a.p_head + (long long)(key0 & ((1 << a.page_shift) - 1)) * a.p_row;
+    const int t = 4 * (f_at - f_base);
+    const unsigned four = (unsigned)(pages >> t) & 15u;
+    const int rows = (four >> w) & 1 ? __builtin_amdgcn_readfirstlane(min(16, fet.g.q.len - (f_at << kTileShift) - 16 * w)) : 0;
     const unsigned span = rows > 0 ? (unsigned)(rows - 1) * pitch + row_bytes : 0u;
-    const __amdgpu_buffer_rsrc_t krs = make_rsrc((const bf16*)a.K + at, span), vrs = make_rsrc((const bf16*)a.V + at, span);
-    const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)buf * TILE + (unsigned)(w * NL) * 1024u);
+    const long long at = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane(where_hi, t + w) << 32) |
+                                     (unsigned)__builtin_amdgcn_readlane(where_lo, t + w));
+    const __amdgpu_buffer_rsrc_t krs = make_rsrc((const void*)at, span), vrs = make_rsrc((const void*)(at + v_off), span);
+    const unsigned to = lds0 + (unsigned)buf * TILE;
 #pragma unroll
     for (int i = 0; i < NL; i++) {
       dma_b128_to_lds(krs, to + i * 1024u, goff[i]);
       dma_b128_to_lds(vrs, to + 2 * TILE + i * 1024u, goff[i]);
     }
-    bad = (bad & ~(15u << (4 * buf))) | (none << (4 * buf));
+    gone = (gone & ~(15u << (4 * buf))) | ((four ^ 15u) << (4 * buf));
     f_at++;
-    settle();
   };
   fetch(0);
 
@@ -451,13 +495,17 @@ paged_chunk_kernel(PagedArgs a) {
     }
   const float c = a.scale * kLog2e;
   int buf = 0;
+#pragma unroll 1
   do {
-    const PagedSegment& s = cur.g;
-    const ItemRow x = item_row(a, s, 32 * w + lr);
-    const KeyRange see = seen_keys(a.w, s.q, x.token);
+    const PagedSegment s = fet.g;
+    const int seg_s = fet.s, end = f_end;
+    int at = f_first;
+    const PagedArgs& b = args_again<PagedArgs>();
+    const ItemRow x = item_row(b, s, 32 * w + lr);
+    const KeyRange see = seen_keys(b.w, s.q, x.token);
     bf16x8 q[KS];
     {
-      const bf16* const qr = (const bf16*)a.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * a.q_row + (size_t)(x.there ? x.head : 0) * a.q_head;
+      const bf16* const qr = (const bf16*)b.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * b.q_row + (size_t)(x.there ? x.head : 0) * b.q_head;
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) {
         const int col = 16 * ks + 8 * h;
@@ -472,21 +520,19 @@ paged_chunk_kernel(PagedArgs a) {
       for (int r = 0; r < 16; r++) o[db][r] = 0.f;
     float m = BURST_NEG_INF, l = 0.f;              // reference (log2 units); the row's sum over this lane's keys
     // tokens of the wavefront's rows: what all of them see, and what any of them does
-    const int most = min(a.w.tokens, s.q.n - s.block * a.w.tokens) - 1;
-    const int t0 = s.block * a.w.tokens + 32 * w / a.part_heads, t1 = s.block * a.w.tokens + min((32 * w + 31) / a.part_heads, most);
-    const bool rows_here = 32 * w / a.part_heads <= most;
-    const KeyRange first = seen_keys(a.w, s.q, t0), last = seen_keys(a.w, s.q, t1);
-    int at, end;
-    segment_tiles(a.w, s, kUnitShift, at, end);
+    const int most = min(b.w.tokens, s.q.n - s.block * b.w.tokens) - 1;
+    const int t0 = s.block * b.w.tokens + 32 * w / b.part_heads, t1 = s.block * b.w.tokens + min((32 * w + 31) / b.part_heads, most);
+    const bool rows_here = 32 * w / b.part_heads <= most;
+    const KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
 #pragma unroll 1
     for (; at < end; at++, buf ^= 1) {
       __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      const unsigned gone = (bad >> (4 * buf)) & 15u;
+      const unsigned none = (gone >> (4 * buf)) & 15u;
       fetch(buf ^ 1);
-      const int key0 = at << kUnitShift;
-      if (!rows_here || key0 > last.hi || key0 + kUnit - 1 < first.lo) continue;   // none of the wavefront's rows sees the tile
+      const int key0 = at << kTileShift;
+      if (!rows_here || key0 > last.hi || key0 + kTile - 1 < first.lo) continue;   // none of the wavefront's rows sees the tile
       const char* const kl = smem + buf * TILE;
       const char* const vl = smem + (2 + buf) * TILE;
       f32x16 sc[2];
@@ -498,14 +544,14 @@ paged_chunk_kernel(PagedArgs a) {
       for (int ks = 0; ks < KS; ks++)
 #pragma unroll
         for (int kb = 0; kb < 2; kb++) sc[kb] = mfma32(lds_read_b128(kl, kb * 32 * ROWB + kaddr[ks]), q[ks], sc[kb]);
-      if (gone != 0 || key0 < last.lo || key0 + kUnit - 1 > first.hi) {   // register r of block kb: key 32 kb + 8 (r / 4) + 4 h + r % 4
+      if (none != 0 || key0 < last.lo || key0 + kTile - 1 > first.hi) {   // register r of block kb: key 32 kb + 8 (r / 4) + 4 h + r % 4
         const int lo = see.lo - key0 - 4 * h, hi = see.hi - key0 - 4 * h;
 #pragma unroll
         for (int kb = 0; kb < 2; kb++)
 #pragma unroll
           for (int r = 0; r < 16; r++) {
             const int k = kb * 32 + 8 * (r >> 2) + (r & 3);
-            if (k < lo || k > hi || ((gone >> (2 * kb + (r >> 3))) & 1)) sc[kb][r] = BURST_NEG_INF;
+            if (k < lo || k > hi || ((none >> (2 * kb + (r >> 3))) & 1)) sc[kb][r] = BURST_NEG_INF;
           }
       }
       float mx = sc[0][0];
@@ -550,7 +596,7 @@ paged_chunk_kernel(PagedArgs a) {
     const unsigned long long bal = __builtin_amdgcn_ballot_w64(x.there && big >= kInfBits);
     unsigned redo = (unsigned)(bal | (bal >> 32));
     if (x.there && !((redo >> lr) & 1)) {
-      const RowPlace to = row_place(a, s, run, kChunkRows, 32 * w + lr, x);
+      const RowPlace to = row_place(b, s, run, kChunkRows, 32 * w + lr, x);
       const float inv = is_zero(l) ? 0.f : 1.f / l;
 #pragma unroll
       for (int db = 0; db < DB; db++)
@@ -559,66 +605,94 @@ paged_chunk_kernel(PagedArgs a) {
           const int col = db * 32 + 8 * q4 + 4 * h;
           if (col >= d) continue;
           const f32x4 v = {o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
-          if (to.whole) store4(a, to.o + col, v * inv);
+          if (to.whole) store4(b, to.o + col, v * inv);
           else *reinterpret_cast<f32x4*>(to.part + col) = v;
         }
       if (h == 0) {
         const float mn = m * kLn2;
-        if (to.whole) a.lse[to.lse] = row_lse(mn, l);
+        if (to.whole) b.lse[to.lse] = row_lse(mn, l);
         else { to.ml[0] = mn; to.ml[kChunkRows] = l; }
       }
     }
-    for (; redo != 0; redo &= redo - 1) row_again<bf16>(a, s, run, kChunkRows, 32 * w + __builtin_ctz(redo), lane);
-  } while (cur.next(a.w));
+    for (; redo != 0; redo &= redo - 1) row_again<bf16>(b, s, seg_s, run, kChunkRows, 32 * w + __builtin_ctz(redo), lane);
+  } while (more);
 }
 
 // ------------------------------------------------------------------------------- merge
-// Joins the partial results of the items that more than one run has worked on: a workgroup for every run whose start is the
-// first one inside an item.  A wavefront takes a row; the item's first part is in slot 1 of its run, the others in slot 0 of theirs.
+// Joins the partial results of the items that more than one run has worked on: four rows of the item that the start of a run is the first
+// one to cut.  16 lanes take a row's columns of one part, eight each, and the lane groups every fourth part, or, where there are
+// many parts, every 16th with the whole workgroup on one row after the other.
+struct Joined { float m, l; f32x4 o[2]; };
+__device__ __forceinline__ void join_in(Joined& x, float m, float l, const f32x4 (&o)[2]) {
+  const float top = fmaxf(x.m, m), ref = top == BURST_NEG_INF ? 0.f : top;
+  const float f = fast_exp2((x.m - ref) * kLog2e), g = fast_exp2((m - ref) * kLog2e);
+  x.m = top;
+  x.l = (is_zero(f) ? 0.f : x.l * f) + (is_zero(g) ? 0.f : l * g);
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int k = 0; k < 4; k++) x.o[i][k] = (is_zero(f) ? 0.f : x.o[i][k] * f) + (is_zero(g) ? 0.f : o[i][k] * g);
+}
 __global__ void __launch_bounds__(256)
 paged_merge_kernel(PagedArgs a, int rows_of_item) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int run = blockIdx.x + 1;
-  DeviceCursor cur;
-  if (!locate_run(a, run, lane, cur)) return;
-  const PagedSegment& g = cur.g;
-  const int n = parts_to_join(g, cur.run), first = run - 1, d = a.d;
-  if (n == 0) return;
+  __shared__ __attribute__((aligned(16))) float side[4][160];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (lane & 15) * 4;
+  const int run = blockIdx.x + 1, d = a.d;
+  const PagedJoin join = a.join[run];
+  if (join.n == 0) return;
+  const bool together = join.n > 16;               // all wavefronts on one row
   const size_t slot = (size_t)rows_of_item * (d + 2);
-  for (int r = blockIdx.y * 4 + wave; r < rows_of_item; r += 4 * gridDim.y) {
-    const ItemRow x = item_row(a, g, r);
-    if (!x.there) continue;
-    auto part = [&](int i) { return a.part + (2 * (size_t)(first + i) + (i == 0 ? 1 : 0)) * slot; };
-    float top = BURST_NEG_INF;
-    for (int i = lane; i < n; i += 64) top = fmaxf(top, part(i)[(size_t)rows_of_item * d + r]);
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-    const float ref = top == BURST_NEG_INF ? 0.f : top;
-    float l = 0.f, o0 = 0.f, o1 = 0.f;
-    const bool c0 = lane < d, c1 = lane + 64 < d;
-    for (int base = 0; base < n; base += 64) {
-      const int i = base + lane;
-      float f = 0.f;
-      if (i < n) {
-        const float* const ml = part(i) + (size_t)rows_of_item * d + r;
-        f = fast_exp2((ml[0] - ref) * kLog2e);
-        l += is_zero(f) ? 0.f : f * ml[rows_of_item];
+  const float* const base = a.part + 2 * (size_t)(run - 1) * slot;
+  const int step = together ? 16 : 4, begin = (together ? 4 * wave : 0) + (lane >> 4);
+  for (int k = together ? 0 : wave; k < (together ? 4 : wave + 1); k++) {
+    const int r = blockIdx.y * 4 + k;
+    const ItemRow x = item_row(a, join.part, join.block, join.count, r);
+    if (!x.there) continue;                        // (the same for all lanes that share a row)
+    Joined sum = {BURST_NEG_INF, 0.f, {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+    for (int i0 = begin; i0 < join.n; i0 += 4 * step) {
+      float m[4], l[4];
+      f32x4 o[4][2];
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const int i = i0 + j * step;
+        const float* const p = base + (2 * (size_t)(i < join.n ? i : begin) + ((i < join.n ? i : begin) == 0 ? 1 : 0)) * slot;
+        m[j] = i < join.n ? p[(size_t)rows_of_item * d + r] : BURST_NEG_INF;
+        l[j] = p[(size_t)rows_of_item * (d + 1) + r];
+#pragma unroll
+        for (int h = 0; h < 2; h++) o[j][h] = c + 64 * h < d ? *reinterpret_cast<const f32x4*>(p + (size_t)r * d + c + 64 * h) : f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      const int here = min(64, n - base);
-#pragma unroll 4
-      for (int k = 0; k < here; k++) {
-        const float fk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k));
-        const float* const o = part(base + k) + (size_t)r * d;
-        const float v0 = c0 ? o[lane] : 0.f, v1 = c1 ? o[lane + 64] : 0.f;
-        o0 += is_zero(fk) ? 0.f : fk * v0;
-        o1 += is_zero(fk) ? 0.f : fk * v1;
+#pragma unroll
+      for (int j = 0; j < 4; j++) join_in(sum, m[j], l[j], o[j]);
+    }
+    for (int off = 16; off < 64; off <<= 1) {      // the lane groups
+      f32x4 o[2];
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[h][e] = __shfl_xor(sum.o[h][e], off);
+      join_in(sum, __shfl_xor(sum.m, off), __shfl_xor(sum.l, off), o);
+    }
+    if (together) {
+      __syncthreads();
+      if (lane < 16) {
+        *reinterpret_cast<f32x4*>(&side[wave][c]) = sum.o[0];
+        *reinterpret_cast<f32x4*>(&side[wave][c + 64]) = sum.o[1];
+        if (lane == 0) { side[wave][128] = sum.m; side[wave][129] = sum.l; }
+      }
+      __syncthreads();
+      if (wave != 0) continue;
+      for (int w = 1; w < 4; w++) {
+        const f32x4 o[2] = {*reinterpret_cast<const f32x4*>(&side[w][c]), *reinterpret_cast<const f32x4*>(&side[w][c + 64])};
+        join_in(sum, side[w][128], side[w][129], o);
       }
     }
-    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
-    const size_t at = (size_t)(g.q.first + x.token) * a.o_row + (size_t)x.head * a.o_head;
-    const float inv = is_zero(l) ? 0.f : 1.f / l;
-    if (c0) store1(a, at + lane, is_zero(l) ? 0.f : o0 * inv);
-    if (c1) store1(a, at + lane + 64, is_zero(l) ? 0.f : o1 * inv);
-    if (lane == 0) a.lse[(size_t)(g.q.first + x.token) * a.heads + x.head] = row_lse(top, l);
+    if (lane >= 16) continue;
+    const size_t row = (size_t)(join.first + x.token), at = row * a.o_row + (size_t)x.head * a.o_head;
+    const float inv = is_zero(sum.l) ? 0.f : 1.f / sum.l;
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+      if (c + 64 * h < d) store4(a, at + c + 64 * h, is_zero(sum.l) ? f32x4{0.f, 0.f, 0.f, 0.f} : sum.o[h] * inv);
+    if (lane == 0) a.lse[row * a.heads + x.head] = row_lse(sum.m, sum.l);
   }
 }
 
@@ -642,7 +716,7 @@ int launch_paged_chunk(const PagedArgs& a, hipStream_t s) {
 }
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {
   if (a.runs < 2) return BURST_OK;
-  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item / 16), dim3(256), 0, s, a, rows_of_item);
+  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item / 4), dim3(256), 0, s, a, rows_of_item);
   return launch_status();
 }
 

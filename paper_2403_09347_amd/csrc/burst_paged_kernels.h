@@ -14,14 +14,18 @@ struct PagedArgs {
   long long q_row, q_head, o_row, o_head;          // element strides
   long long p_page, p_head, p_row;
   float* part;                       // partial results: [2 runs][rows_of_item][d] columns, m, l
+  struct PagedJoin* join;            // [runs]
   PagedWork w;
   int heads, group, d, pages, page_shift;
   int parts_each, part_heads;        // parts of a key/value head, query heads of a part
-  int runs, o_f32;
+  int runs, slack, o_f32;            // slack: see paged_deal
   float scale;
 };
+// What a run tells the merging launch: the item that is joined from the parts of n runs, from the run before it on (n = 0: none)
+struct PagedJoin { int n, first, count, part, block, pad[3]; };   // first, count: the sequence's rows
+static_assert(sizeof(PagedJoin) == 32, "one load");
 constexpr int kShortRows = 16, kChunkRows = 128;   // rows of an item
-constexpr int kShortLds = 32768;                   // bytes of a wavefront's ring
+constexpr int kShortLds = 32768;                   // bytes of a wavefront's ring of tiles
 
 int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s);
 int launch_paged_chunk(const PagedArgs& a, hipStream_t s);
@@ -34,55 +38,77 @@ __device__ __forceinline__ int scalar_at(const int* p, I i) {
   return ((const int __attribute__((address_space(4)))*)p)[i];
 }
 struct ScalarRead { static __device__ __forceinline__ int at(const int* p, int i) { return scalar_at(p, __builtin_amdgcn_readfirstlane(i)); } };
-struct DeviceCursor : PagedCursor<ScalarRead> { long long run; };
+typedef PagedCursor<ScalarRead> DeviceCursor;
 
 // Workgroup -> run: an XCD (ids go to the eight in turn) gets neighbouring runs, which share keys.
 __device__ __forceinline__ int run_of(int bid, int runs) {
   return runs % 8 == 0 ? (bid & 7) * (runs / 8) + (bid >> 3) : bid;
 }
-__device__ __forceinline__ long long wave_scan(long long x, int lane) {   // inclusive
-  for (int off = 1; off < 64; off <<= 1) {
-    const long long y = __shfl_up(x, off);
-    if (lane >= off) x += y;
-  }
+__device__ __forceinline__ int wave_scan(int x) {  // inclusive
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // row_bcast:15 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // row_bcast:31 to rows 2 and 3
   return x;
 }
-__device__ __forceinline__ long long lane_value64(long long x, int lane) {
-  return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
-                     (unsigned)__builtin_amdgcn_readlane((int)x, lane));
+__device__ __forceinline__ int wave_most(int x) {  // of numbers that are not negative; in every lane
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
 }
-// The start of run `run`, by a wavefront: every lane adds up the units of a sequence.  False: the run has none.
-__device__ __forceinline__ bool locate_run(const PagedArgs& a, int run, int lane, DeviceCursor& cur) {
+// The start of run `run`, by a wavefront: every lane adds up a sequence.  False: the run has nothing to do.  The merging launch is told
+// what the run's start has cut (`tell`).
+__device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane, bool tell, DeviceCursor& cur) {
   const PagedWork& w = a.w;
-  auto units = [&](int s) -> long long {
-    if (s >= w.sequences) return 0;
-    return w.cost(paged_seq(w.starts[s], w.starts[s + 1], w.lengths[s], w.rows, w.cap)) * w.parts;
-  };
-  long long total = 0, mine = 0, scan = 0;
-  for (int base = 0; base < w.sequences; base += 64) {
-    mine = units(base + lane);
-    scan = wave_scan(mine, lane);
-    total += lane_value64(scan, 63);
-  }
-  cur.run = run_length(total, a.runs);
-  const long long begin = cur.run * run;
-  if (begin >= total) return false;
-  long long before = 0;
-  int base = 0;
-  for (;; base += 64) {
-    if (w.sequences > 64) {
-      mine = units(base + lane);
-      scan = wave_scan(mine, lane);
+  PagedSeq q;
+  PagedTotals mine = {0, 0, 0}, all = {0, 0, 0};
+  auto totals = [&](int s) __attribute__((always_inline)) {
+    mine = PagedTotals{0, 0, 0};
+    if (s < w.sequences) {
+      q = paged_seq(w.starts[s], w.starts[s + 1], w.lengths[s], w.rows, w.cap);
+      mine = w.totals(q);
     }
-    const long long all = lane_value64(scan, 63);
-    if (begin < before + all) break;
-    before += all;
+  };
+#pragma unroll 1
+  for (int base = 0; base < w.sequences; base += 64) {
+    totals(base + lane);
+    all.units += __builtin_amdgcn_readlane(wave_scan(mine.units), 63) * w.parts;
+    all.items += __builtin_amdgcn_readlane(wave_scan(mine.items), 63) * w.parts;
+    all.most = max(all.most, wave_most(mine.most));
   }
-  const unsigned long long bal = __builtin_amdgcn_ballot_w64(begin < before + scan);
-  const int at = __builtin_ctzll(bal);
-  const long long rem = begin - (before + lane_value64(scan - mine, at));
-  cur.place(w, base + at, rem, min(cur.run, total - begin));
-  return true;
+  const PagedDeal deal = paged_deal(all, a.runs, a.slack);
+  const int total = deal.by_items ? all.items : all.units;
+  const long long from = (long long)deal.each * run;
+  const bool some = from < total;
+  if (some) {
+    const int begin = (int)from;
+    int before = 0, scan = 0, own = 0, base = 0;
+#pragma unroll 1
+    for (;; base += 64) {
+      if (w.sequences > 64) totals(base + lane);
+      own = (deal.by_items ? mine.items : mine.units) * w.parts;
+      scan = wave_scan(own);
+      const int here = __builtin_amdgcn_readlane(scan, 63);
+      if (begin < before + here) break;
+      before += here;
+    }
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(begin < before + scan));
+    const PagedSeq there = {__builtin_amdgcn_readlane(q.first, at), __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at)};
+    const int one = __builtin_amdgcn_readlane(deal.by_items ? mine.items : mine.units, at);
+    cur.place(w, base + at, there, one, begin - (before + __builtin_amdgcn_readlane(scan - own, at)), deal, min(deal.each, total - begin));
+  }
+  if (tell && a.join != nullptr) {
+    PagedJoin j = {0, 0, 0, 0, 0, {0, 0, 0}};
+    if (some && !deal.by_items) j = PagedJoin{parts_to_join(cur.g, deal.each), cur.g.q.first, cur.g.q.n, cur.g.part, cur.g.block, {0, 0, 0}};
+    a.join[run] = j;
+  }
+  return some;
 }
 #endif
 

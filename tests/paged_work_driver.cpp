@@ -14,6 +14,7 @@ using namespace burst;
 static int bad = 0;
 #define CHECK(x) do { if (!(x)) { if (bad++ < 10) std::printf("line %d: %s (case %d)\n", __LINE__, #x, g_case); } } while (0)
 static int g_case = 0;
+static long long by_items = 0, by_units = 0;
 
 static std::vector<int> g_starts, g_lengths;
 struct HostRead {
@@ -32,20 +33,23 @@ static int rnd(int n) {
 static int wild() { const int w[] = {-1, 0, 1, 0x7fffffff, -0x7fffffff - 1, 1 << 30, -5, 64}; return rnd(2) ? w[rnd(8)] : rnd(3000) - 100; }
 
 // as locate_run does it on the device
-static bool locate(const PagedWork& w, int runs, int run, Cursor& cur, long long& each) {
-  long long total = 0;
-  std::vector<long long> units;
+static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur, PagedDeal& deal) {
+  PagedTotals all = {0, 0, 0};
+  std::vector<PagedTotals> each;
   for (int s = 0; s < w.sequences; s++) {
-    units.push_back(w.cost(cur.load(w, s)) * w.parts);
-    total += units.back();
+    each.push_back(w.totals(Cursor::load(w, s)));
+    all.units += each[s].units * w.parts;
+    all.items += each[s].items * w.parts;
+    if (each[s].most > all.most) all.most = each[s].most;
   }
-  each = run_length(total, runs);
-  const long long begin = each * run;
+  deal = paged_deal(all, runs, slack);
+  const int total = deal.by_items ? all.items : all.units;
+  const long long begin = (long long)deal.each * run;
   if (begin >= total) return false;
-  long long before = 0;
-  int s = 0;
-  while (begin >= before + units[s]) before += units[s++];
-  cur.place(w, s, begin - before, each < total - begin ? each : total - begin);
+  auto one = [&](int s) { return deal.by_items ? each[s].items : each[s].units; };
+  int before = 0, s = 0;
+  while (begin >= before + one(s) * w.parts) before += one(s++) * w.parts;
+  cur.place(w, s, Cursor::load(w, s), one(s), (int)begin - before, deal, deal.each < total - begin ? deal.each : total - (int)begin);
   return true;
 }
 
@@ -71,8 +75,9 @@ static void batch(bool anything) {
   w.least = 1; w.most = 0x7fffffff;
   if (rnd(3) == 0) { w.least = 1 + rnd(5); w.most = w.least + rnd(50); }
   w.causal = rnd(3) != 0;
-  w.window = rnd(3) ? 0 : rnd(2) ? 1 + rnd(100) : 1LL << 40;
-  const int runs = 1 + rnd(40);
+  w.window = rnd(3) ? 0 : rnd(2) ? 1 + rnd(100) : 1 << 30;
+  w.unit_shift = rnd(4) ? 6 : 7 + rnd(3);
+  const int runs = 1 + rnd(40), slack = rnd(3) ? rnd(10) : rnd(2) * 100000;
 
   typedef std::tuple<int, int, int> Item;          // sequence, part, block
   std::map<Item, std::vector<int>> covered;
@@ -81,41 +86,49 @@ static void batch(bool anything) {
   std::map<Item, int> joins;
   for (int run = 0; run < runs; run++) {
     Cursor cur;
-    long long each;
-    if (!locate(w, runs, run, cur, each)) continue;
+    PagedDeal deal;
+    if (!locate(w, runs, slack, run, cur, deal)) continue;
     bool first = true;
     do {
       const PagedSegment& g = cur.g;
-      const Item item(g.s, g.part, g.block);
-      CHECK(g.s >= 0 && g.s < S && g.part >= 0 && g.part < w.parts && g.block >= 0 && g.block < w.blocks(g.q));
+      const Item item(cur.s, g.part, g.block);
+      CHECK(cur.s >= 0 && cur.s < S && g.part >= 0 && g.part < w.parts && g.block >= 0 && g.block < w.blocks(g.q));
       CHECK(g.lo <= g.from && g.from < g.to && g.to <= g.hi);
       CHECK(g.q.first >= 0 && g.q.n > 0 && g.q.first + g.q.n <= rows && g.q.len >= 0 && g.q.len <= cap);
       std::vector<int>& c = covered[item];
       c.resize(g.hi - g.lo);
       for (int u = g.from; u < g.to; u++) c[u - g.lo]++;
+      by_items += deal.by_items;
+      by_units += !deal.by_items;
       if (!g.whole()) {
+        CHECK(!deal.by_items);
         CHECK(used.insert(partial_slot(g, run)).second);
         CHECK(partial_slot(g, run) < 2 * runs);
         slots[item].push_back(partial_slot(g, run));
       }
-      for (int shift = 4; shift <= kUnitShift; shift += 2) {   // what the kernels fetch: 16 keys at a time, in one page
+      int k0, k1;
+      w.keys(g.q, g.block, k0, k1);
+      for (int shift = 4; shift <= kTileShift; shift += 2) {   // what the kernels fetch: 16 keys at a time, in one page
         int t, end;
         segment_tiles(w, g, shift, t, end);
+        CHECK(t < end);
+        const int lo = g.from << w.unit_shift, hi = g.to << w.unit_shift;
+        for (int key = lo > k0 ? lo : k0; key < (hi < k1 ? hi : k1); key++) CHECK(key >= t << shift && key < end << shift);
         for (; t < end; t++)
           for (int key = t << shift; key < (t + 1) << shift; key += 16) {
-            const int there = key < g.q.len - 1 ? key : g.q.len - 1;
-            CHECK(there >= 0 && (there >> page_shift) < width);
-            const int page = checked_page(table.at((size_t)g.s * width + (there >> page_shift)), pages);
+            const int entry = table_entry(key, g.q.len, page_shift);
+            CHECK(entry >= -1 && entry < width);
+            if (entry < 0) continue;
+            const int page = checked_page(table.at((size_t)cur.s * width + entry), pages);
             CHECK(page >= -1 && page < pages);
             CHECK((key & ((1 << page_shift) - 1)) + 16 <= 1 << page_shift);
-            if (shift == 4) CHECK(key < g.q.len);
           }
       }
       if (first && run > 0) {
-        const int n = parts_to_join(g, each);
+        const int n = parts_to_join(g, deal.each);
         if (n > 0) {
           joins[item]++;
-          for (int i = 0; i < n; i++) slots[Item(-1 - g.s, g.part, g.block)].push_back(2 * (run - 1 + i) + (i == 0 ? 1 : 0));
+          for (int i = 0; i < n; i++) slots[Item(-1 - cur.s, g.part, g.block)].push_back(2 * (run - 1 + i) + (i == 0 ? 1 : 0));
         }
       }
       first = false;
@@ -123,8 +136,7 @@ static void batch(bool anything) {
     CHECK(cur.left == 0);
   }
   for (int s = 0; s < S; s++) {
-    Cursor cur;
-    const PagedSeq q = cur.load(w, s);
+    const PagedSeq q = Cursor::load(w, s);
     if (!w.mine(q)) continue;
     for (int part = 0; part < w.parts; part++)
       for (int b = 0; b < w.blocks(q); b++) {
@@ -142,8 +154,7 @@ static void batch(bool anything) {
   for (auto& x : covered) items += !x.second.empty();
   size_t want = 0;
   for (int s = 0; s < S; s++) {
-    Cursor cur;
-    const PagedSeq q = cur.load(w, s);
+    const PagedSeq q = Cursor::load(w, s);
     if (w.mine(q)) want += (size_t)w.parts * w.blocks(q);
   }
   CHECK(items == want);
@@ -151,6 +162,7 @@ static void batch(bool anything) {
 
 int main() {
   for (g_case = 0; g_case < 6000; g_case++) batch(g_case % 3 == 2);
+  if (by_items < 1000 || by_units < 1000) bad++;   // both ways of dealing have been seen
   std::printf("work checks failed: %d\n", bad);
   return bad != 0;
 }
