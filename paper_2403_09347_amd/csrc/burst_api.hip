@@ -739,9 +739,10 @@ bool plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) { 
     w.most = i == 0 && plan.chunks ? fit : 0x7fffffff;
     w.causal = p->causal != 0;
     w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
+    w.item_cost = 1;
     double units;                                  // at most so many: 32 bits hold them
     for (w.unit_shift = burst::kTileShift;; w.unit_shift++) {
-      units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2);
+      units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2 + w.item_cost);
       if (units < 2e9 || w.unit_shift == 20) break;
     }
     if (units >= 2e9) return false;

@@ -35,6 +35,7 @@ struct PagedWork {
   int least, most;                   // sequences of fewer or more new tokens are another launch's
   int causal, window;                // window: 0 = none
   int unit_shift;
+  int item_cost;                     // what the beginning of an item costs, in units: it counts in a run's length
   BURST_HD bool mine(const PagedSeq& q) const { return q.n > 0 && q.n >= least && q.n <= most; }
   BURST_HD int blocks(const PagedSeq& q) const { return (q.n + tokens - 1) / tokens; }
   // keys [lo, hi) that the rows of a block see between them
@@ -63,15 +64,15 @@ struct PagedWork {
     for (int b = 0; b < n; b++) {
       int lo, hi;
       units(q, b, lo, hi);
-      t.units += hi - lo;
-      if (hi - lo > t.most) t.most = hi - lo;
+      t.units += hi - lo + item_cost;
+      if (hi - lo + item_cost > t.most) t.most = hi - lo + item_cost;
     }
     return t;
   }
 };
 
 // How the parts, blocks and units of all sequences (sequence, part, block, unit, the last one fastest) are dealt out to runs: `each` units a
-// run, the same number wherever it begins, or, where that costs less, `each` whole items, of which nothing has to be joined.
+// run (the items' beginnings among them: a run that ends within one leaves the item to the next), or, where that costs less, `each` whole items, of which nothing has to be joined.
 // `slack`: the units that a run may have more for that.
 struct PagedDeal { int each, by_items; };
 BURST_HD PagedDeal paged_deal(const PagedTotals& t, int runs, int slack) {
@@ -95,13 +96,14 @@ template <typename Read>
 struct PagedCursor {
   PagedSegment g;
   int s;                             // sequence
-  int left;                          // units (items) of the run behind the segment
+  int left;                          // units (items) from the beginning of the item behind the segment to the end of the run
   int by_items;
   static BURST_HD PagedSeq load(const PagedWork& w, int s) {
     return paged_seq(Read::at(w.starts, s), Read::at(w.starts, s + 1), Read::at(w.lengths, s), w.rows, w.cap);
   }
-  // the place `rem` units (items) into sequence s, which has more of them (`one` for each part of a head)
-  BURST_HD void place(const PagedWork& w, int at, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run) {
+  // the place `rem` units (items) into sequence s, which has more of them (`one` for each part of a head); false: the run, of `run`
+  // units, ends within the beginning of an item
+  BURST_HD bool place(const PagedWork& w, int at, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run) {
     by_items = d.by_items;
     s = at;
     g.q = q;
@@ -110,17 +112,20 @@ struct PagedCursor {
     g.block = by_items ? rem : 0;
     for (;;) {
       w.units(g.q, g.block, g.lo, g.hi);
-      if (by_items || rem < g.hi - g.lo) break;
-      rem -= g.hi - g.lo;
+      if (by_items || rem < g.hi - g.lo + w.item_cost) break;
+      rem -= g.hi - g.lo + w.item_cost;
       g.block++;
     }
-    left = run;
-    cut(by_items ? 0 : rem);
+    left = by_items ? run : rem + run;
+    return cut(w, by_items || rem < w.item_cost ? 0 : rem - w.item_cost);
   }
-  BURST_HD void cut(int skip) {
+  // the segment of the item that `left` reaches into; false: not as far as its first unit
+  BURST_HD bool cut(const PagedWork& w, int skip) {
     g.from = g.lo + skip;
-    g.to = !by_items && left < g.hi - g.from ? g.from + left : g.hi;
-    left -= by_items ? 1 : g.to - g.from;
+    g.to = g.hi;
+    if (!by_items && left - w.item_cost < g.hi - g.lo) g.to = g.lo + left - w.item_cost;
+    left -= by_items ? 1 : g.hi - g.lo + w.item_cost;
+    return g.to > g.from;
   }
   // the run's next segment; false: there is none
   BURST_HD bool next(const PagedWork& w) {
@@ -136,8 +141,7 @@ struct PagedCursor {
       }
     }
     w.units(g.q, g.block, g.lo, g.hi);
-    cut(0);
-    return true;
+    return cut(w, 0);
   }
 };
 // The tiles of 1 << shift keys (shift <= unit_shift) of a segment that hold a key which some row of its item sees: [first, end).  A segment

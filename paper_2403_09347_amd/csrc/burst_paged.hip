@@ -288,6 +288,10 @@ paged_short_kernel(PagedArgs a) {
         const int c = (4 * ks + g) * (16 / (int)sizeof(T));
         q[ks] = x.there && c < d ? *reinterpret_cast<const i32x4*>(qr + c) : i32x4{0, 0, 0, 0};
       }
+      // (Waited for here, once a segment: the compiler, which does not know of the loads in flight, would wait for all of them
+      // before the first product of every stage.)
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) asm volatile("" : "+v"(q[ks]));
 #pragma unroll
       for (int b = 0; b < OB; b++) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
       m = BURST_NEG_INF; l = 0.f;
@@ -619,9 +623,9 @@ paged_chunk_kernel(PagedArgs a) {
 }
 
 // ------------------------------------------------------------------------------- merge
-// Joins the partial results of the items that more than one run has worked on: four rows of the item that the start of a run is the first
-// one to cut.  16 lanes take a row's columns of one part, eight each, and the lane groups every fourth part, or, where there are
-// many parts, every 16th with the whole workgroup on one row after the other.
+// Joins the partial results of the items that more than one run has worked on: rows of the item that the start of a run is the first
+// one to cut.  16 lanes take a row's columns of one part, eight each, and the lane groups every fourth part, a row a wavefront; where there
+// are many parts, every 16th, a row a workgroup.
 struct Joined { float m, l; f32x4 o[2]; };
 __device__ __forceinline__ void join_in(Joined& x, float m, float l, const f32x4 (&o)[2]) {
   const float top = fmaxf(x.m, m), ref = top == BURST_NEG_INF ? 0.f : top;
@@ -644,16 +648,15 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
   const size_t slot = (size_t)rows_of_item * (d + 2);
   const float* const base = a.part + 2 * (size_t)(run - 1) * slot;
   const int step = together ? 16 : 4, begin = (together ? 4 * wave : 0) + (lane >> 4);
-  for (int k = together ? 0 : wave; k < (together ? 4 : wave + 1); k++) {
-    const int r = blockIdx.y * 4 + k;
+  for (int r = together ? blockIdx.y : blockIdx.y * 4 + wave; r < rows_of_item; r += (together ? 1 : 4) * gridDim.y) {
     const ItemRow x = item_row(a, join.part, join.block, join.count, r);
     if (!x.there) continue;                        // (the same for all lanes that share a row)
     Joined sum = {BURST_NEG_INF, 0.f, {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
-    for (int i0 = begin; i0 < join.n; i0 += 4 * step) {
-      float m[4], l[4];
-      f32x4 o[4][2];
+    for (int i0 = begin; i0 < join.n; i0 += 8 * step) {
+      float m[8], l[8];
+      f32x4 o[8][2];                                // (all of them asked for at once: every wait is for memory)
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
+      for (int j = 0; j < 8; j++) {
         const int i = i0 + j * step;
         const float* const p = base + (2 * (size_t)(i < join.n ? i : begin) + ((i < join.n ? i : begin) == 0 ? 1 : 0)) * slot;
         m[j] = i < join.n ? p[(size_t)rows_of_item * d + r] : BURST_NEG_INF;
@@ -662,7 +665,7 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
         for (int h = 0; h < 2; h++) o[j][h] = c + 64 * h < d ? *reinterpret_cast<const f32x4*>(p + (size_t)r * d + c + 64 * h) : f32x4{0.f, 0.f, 0.f, 0.f};
       }
 #pragma unroll
-      for (int j = 0; j < 4; j++) join_in(sum, m[j], l[j], o[j]);
+      for (int j = 0; j < 8; j++) join_in(sum, m[j], l[j], o[j]);
     }
     for (int off = 16; off < 64; off <<= 1) {      // the lane groups
       f32x4 o[2];
@@ -716,7 +719,7 @@ int launch_paged_chunk(const PagedArgs& a, hipStream_t s) {
 }
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {
   if (a.runs < 2) return BURST_OK;
-  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item / 4), dim3(256), 0, s, a, rows_of_item);
+  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item <= 64 ? 4 : rows_of_item / 8), dim3(256), 0, s, a, rows_of_item);
   return launch_status();
 }
 

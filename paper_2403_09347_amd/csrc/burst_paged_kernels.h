@@ -85,7 +85,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
   const PagedDeal deal = paged_deal(all, a.runs, a.slack);
   const int total = deal.by_items ? all.items : all.units;
   const long long from = (long long)deal.each * run;
-  const bool some = from < total;
+  bool some = from < total;
   if (some) {
     const int begin = (int)from;
     int before = 0, scan = 0, own = 0, base = 0;
@@ -101,7 +101,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(begin < before + scan));
     const PagedSeq there = {__builtin_amdgcn_readlane(q.first, at), __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at)};
     const int one = __builtin_amdgcn_readlane(deal.by_items ? mine.items : mine.units, at);
-    cur.place(w, base + at, there, one, begin - (before + __builtin_amdgcn_readlane(scan - own, at)), deal, min(deal.each, total - begin));
+    some = cur.place(w, base + at, there, one, begin - (before + __builtin_amdgcn_readlane(scan - own, at)), deal, min(deal.each, total - begin));
   }
   if (tell && a.join != nullptr) {
     PagedJoin j = {0, 0, 0, 0, 0, {0, 0, 0}};
