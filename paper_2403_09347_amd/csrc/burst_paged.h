@@ -27,7 +27,7 @@ BURST_HD PagedSeq paged_seq(int start, int end, int length, int rows, int cap) {
 // A unit: 1 << unit_shift keys of an item (64, more only where a call could have 2^31 units).  An item has the units that some
 // row of it sees, and at least one, so that rows that see nothing are written too.
 constexpr int kTileShift = 6;                      // tiles of the chunk kernel; units are not smaller
-struct PagedTotals { int units, items, most; };    // most: units of the largest item
+struct PagedTotals { int units, items, most, pair; };   // units of the largest item, and of two that follow one another
 struct PagedWork {
   const int* starts; const int* lengths;
   int sequences, rows, cap;          // rows of the packed tensors; keys that a row of the table has pages for
@@ -49,6 +49,10 @@ struct PagedWork {
     }
     if (hi < lo) hi = lo;
   }
+  // Under a causal mask blocks see more the later they are: they are taken from both ends in turn, so that every two that follow one another
+  // see about the same.
+  BURST_HD bool in_turn() const { return causal && window == 0; }
+  BURST_HD int block_at(int place, int n) const { return !in_turn() ? place : place & 1 ? n - 1 - (place >> 1) : place >> 1; }
   BURST_HD void units(const PagedSeq& q, int block, int& lo, int& hi) const {
     int k0, k1;
     keys(q, block, k0, k1);
@@ -57,28 +61,32 @@ struct PagedWork {
   }
   // all blocks of a sequence, for one part of a head
   BURST_HD PagedTotals totals(const PagedSeq& q) const {
-    PagedTotals t = {0, 0, 0};
+    PagedTotals t = {0, 0, 0, 0};
     if (!mine(q)) return t;
     const int n = blocks(q);
     t.items = n;
+    int first = 0, last = 0;
     for (int b = 0; b < n; b++) {
       int lo, hi;
       units(q, b, lo, hi);
-      t.units += hi - lo + item_cost;
-      if (hi - lo + item_cost > t.most) t.most = hi - lo + item_cost;
+      last = hi - lo + item_cost;
+      if (b == 0) first = last;
+      t.units += last;
+      if (last > t.most) t.most = last;
     }
+    t.pair = in_turn() && n > 1 ? first + last + (tokens >> unit_shift) + 2 : 2 * t.most;   // (rounded up)
     return t;
   }
 };
 
-// How the parts, blocks and units of all sequences (sequence, part, block, unit, the last one fastest) are dealt out to runs: `each` units a
+// How the parts, blocks and units of all sequences (sequence, part, place of the block, unit, the last one fastest) are dealt out to runs: `each` units a
 // run (the items' beginnings among them: a run that ends within one leaves the item to the next), or, where that costs less, `each` whole items, of which nothing has to be joined.
 // `slack`: the units that a run may have more for that.
 struct PagedDeal { int each, by_items; };
 BURST_HD PagedDeal paged_deal(const PagedTotals& t, int runs, int slack) {
   PagedDeal d;
   const int each = (int)(((unsigned)t.units + runs - 1) / (unsigned)runs), per = (int)(((unsigned)t.items + runs - 1) / (unsigned)runs);
-  d.by_items = (long long)per * t.most <= each + each / 16 + slack;
+  d.by_items = (long long)(per >> 1) * t.pair + (per & 1) * t.most <= each + each / 16 + slack;
   d.each = d.by_items ? per : each;
   if (d.each < 1) d.each = 1;
   return d;
@@ -95,7 +103,7 @@ struct PagedSegment {
 template <typename Read>
 struct PagedCursor {
   PagedSegment g;
-  int s;                             // sequence
+  int s, at;                         // sequence; place of the block
   int left;                          // units (items) from the beginning of the item behind the segment to the end of the run
   int by_items;
   static BURST_HD PagedSeq load(const PagedWork& w, int s) {
@@ -103,18 +111,18 @@ struct PagedCursor {
   }
   // the place `rem` units (items) into sequence s, which has more of them (`one` for each part of a head); false: the run, of `run`
   // units, ends within the beginning of an item
-  BURST_HD bool place(const PagedWork& w, int at, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run) {
+  BURST_HD bool place(const PagedWork& w, int seq, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run) {
     by_items = d.by_items;
-    s = at;
+    s = seq;
     g.q = q;
     g.part = (int)((unsigned)rem / (unsigned)one);
     rem -= g.part * one;
-    g.block = by_items ? rem : 0;
-    for (;;) {
+    const int n = w.blocks(g.q);
+    for (at = by_items ? rem : 0;; at++) {
+      g.block = w.block_at(at, n);
       w.units(g.q, g.block, g.lo, g.hi);
       if (by_items || rem < g.hi - g.lo + w.item_cost) break;
       rem -= g.hi - g.lo + w.item_cost;
-      g.block++;
     }
     left = by_items ? run : rem + run;
     return cut(w, by_items || rem < w.item_cost ? 0 : rem - w.item_cost);
@@ -130,8 +138,8 @@ struct PagedCursor {
   // the run's next segment; false: there is none
   BURST_HD bool next(const PagedWork& w) {
     if (left <= 0) return false;
-    if (++g.block >= w.blocks(g.q)) {
-      g.block = 0;
+    if (++at >= w.blocks(g.q)) {
+      at = 0;
       if (++g.part >= w.parts) {
         g.part = 0;
         do {
@@ -140,6 +148,7 @@ struct PagedCursor {
         } while (!w.mine(g.q));
       }
     }
+    g.block = w.block_at(at, w.blocks(g.q));
     w.units(g.q, g.block, g.lo, g.hi);
     return cut(w, 0);
   }

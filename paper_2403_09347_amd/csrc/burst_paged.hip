@@ -145,6 +145,15 @@ __device__ __forceinline__ void row_again(const PagedArgs& a, const PagedSegment
   }
 }
 
+// Operands from LDS byte addresses (see lds_read_b128 and lds_read_tr).
+__device__ __forceinline__ bf16x8 lds_b128(unsigned at) { return *(const bf16x8 __attribute__((address_space(3)))*)(size_t)at; }
+__device__ __forceinline__ bf16x4 lds_tr(unsigned at) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(size_t)at));
+}
+// Keeps the compiler's scheduler from moving anything across.
+#define BURST_FENCE() __builtin_amdgcn_sched_barrier(0)
+
 // vmcnt(N), the other counters untouched; nothing moves across it
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -420,7 +429,7 @@ template <int D>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_kernel(PagedArgs a) {
   constexpr int ROWB = 2 * D, GR = ROWB / 16, RPL = 1024 / ROWB, NL = 16 / RPL, TILE = kTile * ROWB;
-  constexpr int KS = D / 16, DB = D / 32;
+  constexpr int KS = D / 16, DB = D / 32, AHEAD = 4;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
   const int lane = threadIdx.x & 63, lr = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -487,15 +496,16 @@ paged_chunk_kernel(PagedArgs a) {
   };
   fetch(0);
 
-  int kaddr[KS], taddr[DB][2];
+  const unsigned base = lds_addr(smem);
+  unsigned kaddr[KS], taddr[DB][2];                // of buffer 0
 #pragma unroll
-  for (int ks = 0; ks < KS; ks++) kaddr[ks] = lr * ROWB + (((2 * ks + h) ^ chunk_code<D>(lr)) << 4);
+  for (int ks = 0; ks < KS; ks++) kaddr[ks] = base + lr * ROWB + (((2 * ks + h) ^ chunk_code<D>(lr)) << 4);
 #pragma unroll
   for (int db = 0; db < DB; db++)
 #pragma unroll
     for (int sx = 0; sx < 2; sx++) {
       const int j16 = lane & 15, row = 8 * sx + 4 * h + (j16 >> 2), granule = db * 4 + 2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1);
-      taddr[db][sx] = row * ROWB + ((granule ^ chunk_code<D>(row)) << 4) + (j16 & 1) * 8;
+      taddr[db][sx] = base + 2 * TILE + row * ROWB + ((granule ^ chunk_code<D>(row)) << 4) + (j16 & 1) * 8;
     }
   const float c = a.scale * kLog2e;
   int buf = 0;
@@ -537,17 +547,27 @@ paged_chunk_kernel(PagedArgs a) {
       fetch(buf ^ 1);
       const int key0 = at << kTileShift;
       if (!rows_here || key0 > last.hi || key0 + kTile - 1 < first.lo) continue;   // none of the wavefront's rows sees the tile
-      const char* const kl = smem + buf * TILE;
-      const char* const vl = smem + (2 + buf) * TILE;
+      const unsigned tile = (unsigned)buf * TILE;
       f32x16 sc[2];
 #pragma unroll
       for (int kb = 0; kb < 2; kb++)
 #pragma unroll
         for (int r = 0; r < 16; r++) sc[kb][r] = 0.f;
+      // Operands are read AHEAD products before their own.  (Left alone the compiler reads each of them right before its product and
+      // waits for it.)
+      {
+        bf16x8 k[2 * KS];
+        auto read = [&](int i) __attribute__((always_inline)) { k[i] = lds_b128(kaddr[i >> 1] + tile + (i & 1) * 32 * ROWB); };
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++)
+        for (int i = 0; i < AHEAD; i++) read(i);
+        BURST_FENCE();
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++) sc[kb] = mfma32(lds_read_b128(kl, kb * 32 * ROWB + kaddr[ks]), q[ks], sc[kb]);
+        for (int i = 0; i < 2 * KS; i++) {
+          sc[i & 1] = mfma32(k[i], q[i >> 1], sc[i & 1]);
+          if (i + AHEAD < 2 * KS) read(i + AHEAD);
+          BURST_FENCE();
+        }
+      }
       if (none != 0 || key0 < last.lo || key0 + kTile - 1 > first.hi) {   // register r of block kb: key 32 kb + 8 (r / 4) + 4 h + r % 4
         const int lo = see.lo - key0 - 4 * h, hi = see.hi - key0 - 4 * h;
 #pragma unroll
@@ -574,22 +594,32 @@ paged_chunk_kernel(PagedArgs a) {
           for (int r = 0; r < 16; r++) o[db][r] *= alpha;
       }
       const float nref = m == BURST_NEG_INF ? 0.f : -m;
-      bf16x8 p[4];
+      // P of the next 16 keys is computed between the products of these.
+      bf16x8 p[4], v[4 * DB];
+      auto read = [&](int i) __attribute__((always_inline)) {
+        const unsigned at = tile + (i / DB) * 16 * ROWB;
+        v[i] = __builtin_shufflevector(lds_tr(taddr[i % DB][0] + at), lds_tr(taddr[i % DB][1] + at), 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      auto prob = [&](int kg, int t) __attribute__((always_inline)) {
+        const float x = fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t], c, nref));
+        p[kg][t] = (bf16)x;
+        l += x;                                    // (unrounded: lse has 24 bits)
+      };
 #pragma unroll
-      for (int kg = 0; kg < 4; kg++)
+      for (int i = 0; i < AHEAD; i++) read(i);
 #pragma unroll
-        for (int t = 0; t < 8; t++) {
-          const float v = fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t], c, nref));
-          p[kg][t] = (bf16)v;
-          l += v;                                  // (unrounded: lse has 24 bits)
-        }
+      for (int t = 0; t < 8; t++) prob(0, t);
+      BURST_FENCE();
 #pragma unroll
-      for (int kg = 0; kg < 4; kg++)
+      for (int i = 0; i < 4 * DB; i++) {
+        const int kg = i / DB, db = i % DB;
+        o[db] = mfma32(v[i], p[kg], o[db]);
+        if (i + AHEAD < 4 * DB) read(i + AHEAD);
+        if (kg < 3)
 #pragma unroll
-        for (int db = 0; db < DB; db++) {
-          const bf16x4 va = lds_read_tr(vl, kg * 16 * ROWB + taddr[db][0]), vb = lds_read_tr(vl, kg * 16 * ROWB + taddr[db][1]);
-          o[db] = mfma32(__builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7), p[kg], o[db]);
-        }
+          for (int t = 0; t < 8 / DB; t++) prob(kg + 1, db * (8 / DB) + t);
+        BURST_FENCE();
+      }
     }
     l = sum_both_halves(l);
     unsigned big = larger_of(0, l);
@@ -624,8 +654,9 @@ paged_chunk_kernel(PagedArgs a) {
 
 // ------------------------------------------------------------------------------- merge
 // Joins the partial results of the items that more than one run has worked on: rows of the item that the start of a run is the first
-// one to cut.  16 lanes take a row's columns of one part, eight each, and the lane groups every fourth part, a row a wavefront; where there
-// are many parts, every 16th, a row a workgroup.
+// one to cut.  16 lanes take a row's columns of one part, eight each: all parts of a row one after the other where they are few, every fourth
+// one with a wavefront on a row, or every 16th with a workgroup on a row.  (Bound by latency: 2048 tokens at the end of 4096, 512 items cut
+// once, 65 thousand rows of two or three parts: 69 us with a wavefront a row, 21 so.)
 struct Joined { float m, l; f32x4 o[2]; };
 __device__ __forceinline__ void join_in(Joined& x, float m, float l, const f32x4 (&o)[2]) {
   const float top = fmaxf(x.m, m), ref = top == BURST_NEG_INF ? 0.f : top;
@@ -644,11 +675,12 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
   const int run = blockIdx.x + 1, d = a.d;
   const PagedJoin join = a.join[run];
   if (join.n == 0) return;
-  const bool together = join.n > 16;               // all wavefronts on one row
+  const bool alone = join.n <= 8, together = join.n > 32;   // a lane group on a row; all wavefronts on a row
   const size_t slot = (size_t)rows_of_item * (d + 2);
   const float* const base = a.part + 2 * (size_t)(run - 1) * slot;
-  const int step = together ? 16 : 4, begin = (together ? 4 * wave : 0) + (lane >> 4);
-  for (int r = together ? blockIdx.y : blockIdx.y * 4 + wave; r < rows_of_item; r += (together ? 1 : 4) * gridDim.y) {
+  const int step = alone ? 1 : together ? 16 : 4, begin = alone ? 0 : (together ? 4 * wave : 0) + (lane >> 4);
+  const int rows = 16 / step;                      // of a workgroup at a time
+  for (int r = blockIdx.y * rows + (alone ? 4 * wave + (lane >> 4) : together ? 0 : wave); r < rows_of_item; r += rows * gridDim.y) {
     const ItemRow x = item_row(a, join.part, join.block, join.count, r);
     if (!x.there) continue;                        // (the same for all lanes that share a row)
     Joined sum = {BURST_NEG_INF, 0.f, {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
@@ -658,16 +690,20 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
 #pragma unroll
       for (int j = 0; j < 8; j++) {
         const int i = i0 + j * step;
-        const float* const p = base + (2 * (size_t)(i < join.n ? i : begin) + ((i < join.n ? i : begin) == 0 ? 1 : 0)) * slot;
-        m[j] = i < join.n ? p[(size_t)rows_of_item * d + r] : BURST_NEG_INF;
+        const float* const p = base + (2 * (size_t)i + (i == 0 ? 1 : 0)) * slot;
+        m[j] = BURST_NEG_INF; l[j] = 0.f;
+        o[j][0] = o[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (i >= join.n) continue;
+        m[j] = p[(size_t)rows_of_item * d + r];
         l[j] = p[(size_t)rows_of_item * (d + 1) + r];
 #pragma unroll
-        for (int h = 0; h < 2; h++) o[j][h] = c + 64 * h < d ? *reinterpret_cast<const f32x4*>(p + (size_t)r * d + c + 64 * h) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; h++)
+          if (c + 64 * h < d) o[j][h] = *reinterpret_cast<const f32x4*>(p + (size_t)r * d + c + 64 * h);
       }
 #pragma unroll
       for (int j = 0; j < 8; j++) join_in(sum, m[j], l[j], o[j]);
     }
-    for (int off = 16; off < 64; off <<= 1) {      // the lane groups
+    for (int off = alone ? 64 : 16; off < 64; off <<= 1) {   // the lane groups
       f32x4 o[2];
 #pragma unroll
       for (int h = 0; h < 2; h++)
@@ -689,13 +725,13 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
         join_in(sum, side[w][128], side[w][129], o);
       }
     }
-    if (lane >= 16) continue;
+    if (!alone && lane >= 16) continue;
     const size_t row = (size_t)(join.first + x.token), at = row * a.o_row + (size_t)x.head * a.o_head;
     const float inv = is_zero(sum.l) ? 0.f : 1.f / sum.l;
 #pragma unroll
     for (int h = 0; h < 2; h++)
       if (c + 64 * h < d) store4(a, at + c + 64 * h, is_zero(sum.l) ? f32x4{0.f, 0.f, 0.f, 0.f} : sum.o[h] * inv);
-    if (lane == 0) a.lse[row * a.heads + x.head] = row_lse(sum.m, sum.l);
+    if (c == 0) a.lse[row * a.heads + x.head] = row_lse(sum.m, sum.l);
   }
 }
 
@@ -719,7 +755,7 @@ int launch_paged_chunk(const PagedArgs& a, hipStream_t s) {
 }
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {
   if (a.runs < 2) return BURST_OK;
-  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item <= 64 ? 4 : rows_of_item / 8), dim3(256), 0, s, a, rows_of_item);
+  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item <= 64 ? 4 : rows_of_item / 16), dim3(256), 0, s, a, rows_of_item);
   return launch_status();
 }
 

@@ -67,9 +67,9 @@ __device__ __forceinline__ int wave_most(int x) {  // of numbers that are not ne
 __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane, bool tell, DeviceCursor& cur) {
   const PagedWork& w = a.w;
   PagedSeq q;
-  PagedTotals mine = {0, 0, 0}, all = {0, 0, 0};
+  PagedTotals mine = {0, 0, 0, 0}, all = {0, 0, 0, 0};
   auto totals = [&](int s) __attribute__((always_inline)) {
-    mine = PagedTotals{0, 0, 0};
+    mine = PagedTotals{0, 0, 0, 0};
     if (s < w.sequences) {
       q = paged_seq(w.starts[s], w.starts[s + 1], w.lengths[s], w.rows, w.cap);
       mine = w.totals(q);
@@ -81,6 +81,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
     all.units += __builtin_amdgcn_readlane(wave_scan(mine.units), 63) * w.parts;
     all.items += __builtin_amdgcn_readlane(wave_scan(mine.items), 63) * w.parts;
     all.most = max(all.most, wave_most(mine.most));
+    all.pair = max(all.pair, wave_most(mine.pair));
   }
   const PagedDeal deal = paged_deal(all, a.runs, a.slack);
   const int total = deal.by_items ? all.items : all.units;

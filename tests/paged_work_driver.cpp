@@ -33,16 +33,20 @@ static int rnd(int n) {
 static int wild() { const int w[] = {-1, 0, 1, 0x7fffffff, -0x7fffffff - 1, 1 << 30, -5, 64}; return rnd(2) ? w[rnd(8)] : rnd(3000) - 100; }
 
 // as locate_run does it on the device
-static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur, PagedDeal& deal) {
-  PagedTotals all = {0, 0, 0};
+static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur, PagedDeal& deal, long long& bound) {
+  PagedTotals all = {0, 0, 0, 0};
   std::vector<PagedTotals> each;
   for (int s = 0; s < w.sequences; s++) {
     each.push_back(w.totals(Cursor::load(w, s)));
     all.units += each[s].units * w.parts;
     all.items += each[s].items * w.parts;
     if (each[s].most > all.most) all.most = each[s].most;
+    if (each[s].pair > all.pair) all.pair = each[s].pair;
   }
   deal = paged_deal(all, runs, slack);
+  const long long per = deal.each, even = (all.units + runs - 1) / runs;
+  bound = (per >> 1) * all.pair + (per & 1) * all.most;
+  if (deal.by_items) CHECK(bound <= even + even / 16 + slack);
   const int total = deal.by_items ? all.items : all.units;
   const long long begin = (long long)deal.each * run;
   if (begin >= total) return false;
@@ -87,8 +91,10 @@ static void batch(bool anything) {
   for (int run = 0; run < runs; run++) {
     Cursor cur;
     PagedDeal deal;
-    if (!locate(w, runs, slack, run, cur, deal)) continue;
+    long long bound = 0;
+    if (!locate(w, runs, slack, run, cur, deal, bound)) continue;
     bool first = true;
+    long long length = 0;                          // no run of whole items is longer than the deal's bound on it
     do {
       const PagedSegment& g = cur.g;
       const Item item(cur.s, g.part, g.block);
@@ -132,8 +138,10 @@ static void batch(bool anything) {
         }
       }
       first = false;
+      length += g.hi - g.lo + w.item_cost;
     } while (cur.next(w));
     CHECK(cur.left <= w.item_cost);
+    if (deal.by_items) CHECK(length <= bound);
   }
   for (int s = 0; s < S; s++) {
     const PagedSeq q = Cursor::load(w, s);
