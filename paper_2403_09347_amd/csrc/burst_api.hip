@@ -709,52 +709,47 @@ int check_paged(const burst_paged_params* p, Paged& g, bool attend) {
   if (g.page[2] < d || g.page[2] >= 1LL << 25) return BURST_ERR_SHAPE;
   return BURST_OK;
 }
-// The launches of burst_paged_fwd: what each takes, and its runs (as many as the chip holds, or as many units as there can be).
-struct PagedPlan { bool shorts, chunks; int least; burst::PagedArgs a[2]; size_t bytes; };
-bool plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {   // false: more units than 32 bits count
+// The kernel of a burst_paged_fwd call and its runs: as many as the chip holds at once, or as there can be units.
+struct PagedPlan { bool chunk; burst::PagedArgs a; size_t bytes; };
+int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   const int group = p->H / p->kv_heads, cap = p->width * p->page;
   const int most = p->max_new > 0 && p->max_new < p->rows ? p->max_new : p->rows;
-  // A sequence whose rows fill 16 rows of an item at most is the short kernel's; longer ones the chunk kernel's (bf16).
-  const int fit = group <= burst::kShortRows ? burst::kShortRows / group : 0;
-  plan.chunks = p->dtype == BURST_BF16 && most > fit;
-  plan.shorts = !plan.chunks || (p->sequences > 1 && fit > 0);
-  plan.bytes = 0;
-  for (int i = 0; i < 2; i++) {
-    burst::PagedArgs& a = plan.a[i];
-    a = burst::PagedArgs{};
-    const int rows = i == 0 ? burst::kShortRows : burst::kChunkRows;
-    a.group = group; a.heads = p->H; a.d = p->d; a.pages = p->pages; a.page_shift = g.page_shift;
-    a.part_heads = group < rows ? group : rows;
-    a.parts_each = (group + rows - 1) / rows;
-    a.table = p->table; a.table_stride = g.table_stride;
-    a.q_row = g.q[0]; a.q_head = g.q[1]; a.o_row = g.o[0]; a.o_head = g.o[1];
-    a.p_page = g.page[0]; a.p_head = g.page[1]; a.p_row = g.page[2];
-    a.o_f32 = p->out_f32 != 0 || p->dtype == BURST_F32;
-    a.scale = p->scale;
-    burst::PagedWork& w = a.w;
-    w.starts = p->starts; w.lengths = p->lengths; w.sequences = p->sequences; w.rows = p->rows; w.cap = cap;
-    w.tokens = group <= rows ? rows / group : 1;
-    w.parts = p->kv_heads * a.parts_each;
-    w.least = i == 0 || !plan.shorts ? 1 : fit + 1;
-    w.most = i == 0 && plan.chunks ? fit : 0x7fffffff;
-    w.causal = p->causal != 0;
-    w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
-    w.item_cost = 1;
-    double units;                                  // at most so many: 32 bits hold them
-    for (w.unit_shift = burst::kTileShift;; w.unit_shift++) {
-      units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2 + w.item_cost);
-      if (units < 2e9 || w.unit_shift == 20) break;
-    }
-    if (units >= 2e9) return false;
-    const int slots = i == 0 ? 1024 : 512;
-    a.runs = units < slots ? (int)units : slots;
-    if (a.runs < 1) a.runs = 1;
-    if (a.runs > 8) a.runs &= ~7;
-    a.slack = i == 0 ? 2 : 8;
-    const size_t bytes = a.runs < 2 ? 0 : (size_t)a.runs * (2 * rows * (p->d + 2) * sizeof(float) + sizeof(burst::PagedJoin));
-    if ((i == 0 ? plan.shorts : plan.chunks) && bytes > plan.bytes) plan.bytes = bytes;
+  // bf16 calls whose sequences may have more rows than an item of the short kernel are the chunk kernel's, the sequences that have fewer
+  // among them.  (Two launches for a call's short and long sequences, each with its join, took longer.  us, two kernels / this one: 12
+  // sequences of 1 to 512 new tokens over 600 to 8000 keys, 32 heads, 176 / 165; 64 of 1 to 40 over 4096 to 16384, 32 over 8 heads, 487 / 472;
+  // 4 with a window of 1024, d = 64, 42 / 37.)
+  plan.chunk = p->dtype == BURST_BF16 && (long long)most * group > burst::kShortRows;
+  const int rows = plan.chunk ? burst::kChunkRows : burst::kShortRows;
+  burst::PagedArgs& a = plan.a;
+  a = burst::PagedArgs{};
+  a.group = group; a.heads = p->H; a.d = p->d; a.pages = p->pages; a.page_shift = g.page_shift;
+  a.part_heads = group < rows ? group : rows;
+  a.parts_each = (group + rows - 1) / rows;
+  a.table = p->table; a.table_stride = g.table_stride;
+  a.q_row = g.q[0]; a.q_head = g.q[1]; a.o_row = g.o[0]; a.o_head = g.o[1];
+  a.p_page = g.page[0]; a.p_head = g.page[1]; a.p_row = g.page[2];
+  a.o_f32 = p->out_f32 != 0 || p->dtype == BURST_F32;
+  a.scale = p->scale;
+  burst::PagedWork& w = a.w;
+  w.starts = p->starts; w.lengths = p->lengths; w.sequences = p->sequences; w.rows = p->rows; w.cap = cap;
+  w.tokens = group <= rows ? rows / group : 1;
+  w.parts = p->kv_heads * a.parts_each;
+  w.causal = p->causal != 0;
+  w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
+  w.item_cost = 1;
+  double units;                                    // at most so many: 32 bits hold them
+  for (w.unit_shift = burst::kTileShift;; w.unit_shift++) {
+    units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2 + w.item_cost);
+    if (units < 2e9) break;
+    if (w.unit_shift == 20) return BURST_ERR_SHAPE;
   }
-  return true;
+  const int slots = plan.chunk ? 512 : 1024;
+  a.runs = units < slots ? (int)units : slots;
+  if (a.runs < 1) a.runs = 1;
+  if (a.runs > 8) a.runs &= ~7;
+  a.slack = plan.chunk ? 8 : 2;
+  plan.bytes = a.runs < 2 ? 0 : (size_t)a.runs * (2 * rows * (p->d + 2) * sizeof(float) + sizeof(burst::PagedJoin));
+  return BURST_OK;
 }
 
 }  // namespace
@@ -1224,7 +1219,7 @@ size_t burst_paged_workspace_bytes(const burst_paged_params* p) {
   Paged g;
   if (check_paged(p, g, true) != BURST_OK) return 0;
   PagedPlan plan;
-  return plan_paged(p, g, plan) ? plan.bytes : 0;
+  return plan_paged(p, g, plan) == BURST_OK ? plan.bytes : 0;
 }
 
 int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,
@@ -1238,28 +1233,20 @@ int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, voi
   REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4);
   if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
   PagedPlan plan;
-  if (!plan_paged(p, g, plan)) return BURST_ERR_SHAPE;
+  if ((st = plan_paged(p, g, plan)) != BURST_OK) return st;
   if (plan.bytes > 0) {
     REQUIRE_PTR(workspace);
     if (workspace_bytes < plan.bytes) return BURST_ERR_SHAPE;
   }
   if ((st = check_arch()) != BURST_OK) return st;
-  for (burst::PagedArgs& a : plan.a) {
-    a.Q = Q; a.O = O; a.lse = lse; a.K = K_pages; a.V = V_pages; a.part = (float*)workspace;
-    a.join = a.runs < 2 ? nullptr : (burst::PagedJoin*)(a.part + (size_t)2 * a.runs * (&a == plan.a ? burst::kShortRows : burst::kChunkRows) * (p->d + 2));
-  }
+  burst::PagedArgs& a = plan.a;
+  const int rows = plan.chunk ? burst::kChunkRows : burst::kShortRows;
+  a.Q = Q; a.O = O; a.lse = lse; a.K = K_pages; a.V = V_pages; a.part = (float*)workspace;
+  a.join = a.runs < 2 ? nullptr : (burst::PagedJoin*)(a.part + (size_t)2 * a.runs * rows * (p->d + 2));
   hipStream_t s = (hipStream_t)stream;
   return validated([&] {
-    int e = BURST_OK;
-    if (plan.chunks) {
-      if ((e = burst::launch_paged_chunk(plan.a[1], s)) != BURST_OK) return e;
-      if ((e = burst::launch_paged_merge(plan.a[1], burst::kChunkRows, s)) != BURST_OK) return e;
-    }
-    if (plan.shorts) {
-      if ((e = burst::launch_paged_short(plan.a[0], p->dtype, s)) != BURST_OK) return e;
-      e = burst::launch_paged_merge(plan.a[0], burst::kShortRows, s);
-    }
-    return e;
+    const int e = plan.chunk ? burst::launch_paged_chunk(a, s) : burst::launch_paged_short(a, p->dtype, s);
+    return e != BURST_OK ? e : burst::launch_paged_merge(a, rows, s);
   });
 }
 

@@ -32,11 +32,9 @@ struct PagedWork {
   const int* starts; const int* lengths;
   int sequences, rows, cap;          // rows of the packed tensors; keys that a row of the table has pages for
   int tokens, parts;                 // of an item; parts of all key/value heads
-  int least, most;                   // sequences of fewer or more new tokens are another launch's
   int causal, window;                // window: 0 = none
   int unit_shift;
   int item_cost;                     // what the beginning of an item costs, in units: it counts in a run's length
-  BURST_HD bool mine(const PagedSeq& q) const { return q.n > 0 && q.n >= least && q.n <= most; }
   BURST_HD int blocks(const PagedSeq& q) const { return (q.n + tokens - 1) / tokens; }
   // keys [lo, hi) that the rows of a block see between them
   BURST_HD void keys(const PagedSeq& q, int block, int& lo, int& hi) const {
@@ -62,7 +60,7 @@ struct PagedWork {
   // all blocks of a sequence, for one part of a head
   BURST_HD PagedTotals totals(const PagedSeq& q) const {
     PagedTotals t = {0, 0, 0, 0};
-    if (!mine(q)) return t;
+    if (q.n <= 0) return t;
     const int n = blocks(q);
     t.items = n;
     int first = 0, last = 0;
@@ -145,7 +143,7 @@ struct PagedCursor {
         do {
           if (++s >= w.sequences) return false;
           g.q = load(w, s);
-        } while (!w.mine(g.q));
+        } while (g.q.n <= 0);
       }
     }
     g.block = w.block_at(at, w.blocks(g.q));

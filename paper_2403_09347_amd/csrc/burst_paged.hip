@@ -2,9 +2,9 @@
 // position and window leave, K and V in pages, with the running maximum and sum of burst_local_fwd and nothing but
 // O and lse stored.
 //
-// Two kernels.  paged_short_kernel: one wavefront and 16 rows (tokens x the heads of a group) at a time, every wavefront
+// Two kernels, one of them a call.  paged_short_kernel: one wavefront and 16 rows (tokens x the heads of a group) at a time, every wavefront
 // with a stream of K and V tiles of its own through LDS: single tokens, where reading the cache is the work (HBM), and fp32.
-// paged_chunk_kernel (bf16): 128 rows and four wavefronts that share the tiles, bound by the matrix and vector units.
+// paged_chunk_kernel (bf16, calls with longer sequences): 128 rows and four wavefronts that share the tiles, bound by the matrix and vector units.
 // Either way the work is a sequence of units (64 keys of 16 or 128 rows, see burst_paged.h) that is cut into runs of equal length,
 // as many as the chip holds at once, whatever the lengths of the sequences are: the arrays that say so are on the device, and a
 // captured call is replayed with others.  Where a run ends inside an item, the item's partial results go to the workspace

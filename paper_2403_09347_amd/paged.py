@@ -26,8 +26,8 @@ def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=Non
     """Attention of the new tokens q [rows, H, d] (H a multiple of kv_heads) over the keys of their sequences up to their own positions (causal =
     False: all of them), the last `window` of them if that is not 0.  Returns (O [rows, H, d], lse [rows, H] fp32): new tensors, or out
     (of q's type or float32) and lse; rows behind the last sequence are not written, tokens that see no key get 0 and -inf.
-    max_new: the most new tokens of any sequence, if the caller knows it (chooses kernels only: 1 spares single tokens the launches
-    for prompts).  O as float32, lse and a sum of 1 are a state that binding.burst_merge_state joins with those of
+    max_new: the most new tokens of any sequence, if the caller knows it (chooses the kernel only: 1 gives single tokens the one that is
+    made for them).  O as float32, lse and a sum of 1 are a state that binding.burst_merge_state joins with those of
     the ring's other devices.  No gradient."""
     scale = float(scale) if scale is not None else q.shape[-1] ** -0.5
     try:
