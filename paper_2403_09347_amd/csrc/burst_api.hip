@@ -714,11 +714,11 @@ struct PagedPlan { bool chunk; burst::PagedArgs a; size_t bytes; };
 int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   const int group = p->H / p->kv_heads, cap = p->width * p->page;
   const int most = p->max_new > 0 && p->max_new < p->rows ? p->max_new : p->rows;
-  // bf16 calls whose sequences may have more rows than an item of the short kernel are the chunk kernel's, the sequences that have fewer
+  // Calls whose sequences may have more rows than an item of the short kernel are the chunk kernel's, the sequences that have fewer
   // among them.  (Two launches for a call's short and long sequences, each with its join, took longer.  us, two kernels / this one: 12
   // sequences of 1 to 512 new tokens over 600 to 8000 keys, 32 heads, 176 / 165; 64 of 1 to 40 over 4096 to 16384, 32 over 8 heads, 487 / 472;
   // 4 with a window of 1024, d = 64, 42 / 37.)
-  plan.chunk = p->dtype == BURST_BF16 && (long long)most * group > burst::kShortRows;
+  plan.chunk = (long long)most * group > burst::kShortRows;
   const int rows = plan.chunk ? burst::kChunkRows : burst::kShortRows;
   burst::PagedArgs& a = plan.a;
   a = burst::PagedArgs{};
@@ -738,7 +738,7 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
   w.item_cost = 1;
   double units;                                    // at most so many: 32 bits hold them
-  for (w.unit_shift = burst::kTileShift;; w.unit_shift++) {
+  for (w.unit_shift = plan.chunk && p->dtype == BURST_F32 ? burst::kTileShiftF32 : burst::kTileShift;; w.unit_shift++) {
     units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2 + w.item_cost);
     if (units < 2e9) break;
     if (w.unit_shift == 20) return BURST_ERR_SHAPE;
@@ -1245,7 +1245,7 @@ int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, voi
   a.join = a.runs < 2 ? nullptr : (burst::PagedJoin*)(a.part + (size_t)2 * a.runs * rows * (p->d + 2));
   hipStream_t s = (hipStream_t)stream;
   return validated([&] {
-    const int e = plan.chunk ? burst::launch_paged_chunk(a, s) : burst::launch_paged_short(a, p->dtype, s);
+    const int e = plan.chunk ? burst::launch_paged_chunk(a, p->dtype, s) : burst::launch_paged_short(a, p->dtype, s);
     return e != BURST_OK ? e : burst::launch_paged_merge(a, rows, s);
   });
 }

@@ -417,73 +417,76 @@ paged_short_kernel(PagedArgs a) {
 }
 
 // ------------------------------------------------------------------------------- chunk
-// Four wavefronts of 32 rows each share K and V tiles of 64 keys, double-buffered in LDS (DMA, one barrier a tile); operand
-// orientation and LDS layout as in burst_plain_mfma.h: S^T = K Q^T with a row per lane, whose P is the operand of
-// O^T += V^T P^T as it stands.  A wavefront fetches 16 keys of every tile, which lie in one page.  Two workgroups a CU, so that one's
+// Four wavefronts of 32 rows each share K and V tiles, double-buffered in LDS (DMA, one barrier a tile).  Two workgroups a CU, so that one's
 // vector work overlaps the other's matrix work.
-// Scores and references are in log2 units (one fma an exponent), as in the d = 64 and d = 128 kernels of the walks.
-constexpr int kTile = 1 << kTileShift;             // keys
-template <int D>
-__device__ __forceinline__ int chunk_code(int row) { return D == 64 ? (row >> 1) & 7 : row_code(row); }
-template <int D>
-__global__ void __launch_bounds__(256, 2)
-paged_chunk_kernel(PagedArgs a) {
-  constexpr int ROWB = 2 * D, GR = ROWB / 16, RPL = 1024 / ROWB, NL = 16 / RPL, TILE = kTile * ROWB;
-  constexpr int KS = D / 16, DB = D / 32, AHEAD = 4;
-  __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
-  const int lane = threadIdx.x & 63, lr = lane & 31, h = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int run = run_of(blockIdx.x, a.runs);
+// The fetching side, a tile of 1 << SHIFT keys ahead: tiles [f_at, f_end) of fet.g are still to be asked for.  A wavefront fetches a quarter of
+// every tile, whose keys lie in one page; the lanes hold the places of the 64 groups of 16 keys from tile f_base on.
+template <typename T, int D, int SHIFT>
+struct TileFeed {
+  static constexpr int ROWB = D * (int)sizeof(T), GR = ROWB / 16, TILE = ROWB << SHIFT;   // LDS bytes and granules of a row; bytes of a tile
+  static constexpr int GROUPS = (1 << SHIFT) / 16, ROWS = (1 << SHIFT) / 4;               // of 16 keys in a tile; keys of a wavefront's quarter
+  static constexpr int RPL = 1024 / ROWB, NL = ROWS / RPL;                                // rows of a load; loads
+  static __device__ __forceinline__ int code(int row) { return short_code<GR>(row); }
   DeviceCursor fet;
-  if (!start_run(a, run, lane, threadIdx.x == 0, fet)) return;
-  const unsigned lds0 = lds_addr(smem) + (unsigned)(w * NL) * 1024u;
-  const int d = a.d;
-  const unsigned pitch = (unsigned)(a.p_row * 2), row_bytes = (unsigned)(d * 2);
-  const long long v_off = (const char*)a.V - (const char*)a.K;
-  int goff[NL];
+  int w, lane;
+  int f_first, f_at, f_end, f_base, where_lo, where_hi, goff[NL];
+  unsigned long long pages;          // those of the 64 groups that have a page
+  long long v_off;
+  unsigned lds0, pitch, row_bytes;
+  unsigned gone;                     // GROUPS bits a buffer: groups without a page
+  bool more;                         // fet.g is the segment of the tile that was asked for last
+  __device__ __forceinline__ int group() const { return w * ROWS / 16; }
+  __device__ __forceinline__ int first_row() const { return w * ROWS % 16; }
+  __device__ __forceinline__ bool start(const PagedArgs& a, int run, const char* smem) {
+    lane = threadIdx.x & 63;
+    w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!start_run(a, run, lane, threadIdx.x == 0, fet)) return false;
+    lds0 = lds_addr(smem) + (unsigned)(w * NL) * 1024u;
+    pitch = (unsigned)(a.p_row * (int)sizeof(T)); row_bytes = (unsigned)(a.d * (int)sizeof(T));
+    v_off = (const char*)a.V - (const char*)a.K;
 #pragma unroll
-  for (int i = 0; i < NL; i++) {
-    const int row = i * RPL + lane / GR, granule = (lane % GR) ^ chunk_code<D>(row);
-    goff[i] = granule * 8 < d ? row * (int)pitch + granule * 16 : (int)0x80000000u;
+    for (int i = 0; i < NL; i++) {
+      const int row = i * RPL + lane / GR, granule = (lane % GR) ^ code(first_row() + row);
+      goff[i] = granule * (16 / (int)sizeof(T)) < a.d ? row * (int)pitch + granule * 16 : (int)0x80000000u;
+    }
+    gone = 0;
+    more = true;
+    enter();
+    fetch(0);
+    return true;
   }
-  // The fetching side, a tile ahead: tiles [f_at, f_end) of fet.g are still to be asked for; the lanes hold the places of the 64 groups of
-  // 16 keys of the 16 tiles from f_base on.
-  int f_first, f_at, f_end, f_base;
-  int where_lo, where_hi;
-  unsigned long long pages = 0;                    // those of the 64 groups that have a page
-  auto look_up = [&]() __attribute__((always_inline)) {
+  __device__ __forceinline__ void look_up() {
     const PagedArgs& b = args_again<PagedArgs>();
-    const int key = (f_at << kTileShift) + 16 * lane, entry = table_entry(key, fet.g.q.len, b.page_shift);
+    const int key = (f_at << SHIFT) + 16 * lane, entry = table_entry(key, fet.g.q.len, b.page_shift);
     int page = -1;
     if (entry >= 0) page = checked_page(b.table[(long long)fet.s * b.table_stride + entry], b.pages);
     const long long at = (long long)max(page, 0) * b.p_page + (long long)((unsigned)fet.g.part / (unsigned)b.parts_each) * b.p_head +
-                         (long long)(key & ((1 << b.page_shift) - 1)) * b.p_row;
-    const long long where = (long long)(size_t)b.K + at * 2;
+                         (long long)((key & ((1 << b.page_shift) - 1)) + first_row()) * b.p_row;
+    const long long where = (long long)(size_t)b.K + at * (long long)sizeof(T);
     where_lo = (int)where; where_hi = (int)(where >> 32);
     pages = __builtin_amdgcn_ballot_w64(page >= 0);
     f_base = f_at;
-  };
-  auto enter = [&]() __attribute__((always_inline)) {
-    segment_tiles(args_again<PagedArgs>().w, fet.g, kTileShift, f_at, f_end);
+  }
+  __device__ __forceinline__ void enter() {
+    segment_tiles(args_again<PagedArgs>().w, fet.g, SHIFT, f_at, f_end);
     f_first = f_at;
     look_up();
-  };
-  enter();
-  unsigned gone = 0;                               // four bits a buffer: groups of keys without a page
-  bool more = true;                                // fet.g is the segment of the tile that was asked for last
-  auto fetch = [&](int buf) __attribute__((always_inline)) {
+  }
+  // asks for the next tile, if the run has one (`more`); K goes to buffer buf, V two tiles behind it
+  __device__ __forceinline__ void fetch(int buf) {
     if (f_at == f_end) {
       if (!more || !fet.next(args_again<PagedArgs>().w)) { more = false; return; }
       enter();
-    } else if (f_at - f_base == 16) {
+    } else if (f_at - f_base == 64 / GROUPS) {
       look_up();
     }
-    const int t = 4 * (f_at - f_base);
-    const unsigned four = (unsigned)(pages >> t) & 15u;
-    const int rows = (four >> w) & 1 ? __builtin_amdgcn_readfirstlane(min(16, fet.g.q.len - (f_at << kTileShift) - 16 * w)) : 0;
+    constexpr unsigned ALL = (1u << GROUPS) - 1;
+    const int t = GROUPS * (f_at - f_base);
+    const unsigned here = (unsigned)(pages >> t) & ALL;
+    const int rows = (here >> group()) & 1 ? __builtin_amdgcn_readfirstlane(min(ROWS, fet.g.q.len - (f_at << SHIFT) - w * ROWS)) : 0;
     const unsigned span = rows > 0 ? (unsigned)(rows - 1) * pitch + row_bytes : 0u;
-    const long long at = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane(where_hi, t + w) << 32) |
-                                     (unsigned)__builtin_amdgcn_readlane(where_lo, t + w));
+    const long long at = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane(where_hi, t + group()) << 32) |
+                                     (unsigned)__builtin_amdgcn_readlane(where_lo, t + group()));
     const __amdgpu_buffer_rsrc_t krs = make_rsrc((const void*)at, span), vrs = make_rsrc((const void*)(at + v_off), span);
     const unsigned to = lds0 + (unsigned)buf * TILE;
 #pragma unroll
@@ -491,29 +494,46 @@ paged_chunk_kernel(PagedArgs a) {
       dma_b128_to_lds(krs, to + i * 1024u, goff[i]);
       dma_b128_to_lds(vrs, to + 2 * TILE + i * 1024u, goff[i]);
     }
-    gone = (gone & ~(15u << (4 * buf))) | ((four ^ 15u) << (4 * buf));
+    gone = (gone & ~(ALL << (GROUPS * buf))) | ((here ^ ALL) << (GROUPS * buf));
     f_at++;
-  };
-  fetch(0);
+  }
+  __device__ __forceinline__ unsigned missing(int buf) const { return (gone >> (GROUPS * buf)) & ((1u << GROUPS) - 1); }
+};
+
+// bf16: tiles of 64 keys, operand orientation and LDS layout as in burst_plain_mfma.h: S^T = K Q^T with a row per lane, whose P is the operand
+// of O^T += V^T P^T as it stands.
+// Scores and references are in log2 units (one fma an exponent), as in the d = 64 and d = 128 kernels of the walks.
+constexpr int kTile = 1 << kTileShift;             // keys
+// C: columns that are computed, of the D that a row of LDS has.
+template <int D, int C>
+__global__ void __launch_bounds__(256, 2)
+paged_chunk_kernel(PagedArgs a) {
+  typedef TileFeed<bf16, D, kTileShift> Feed;
+  constexpr int ROWB = Feed::ROWB, TILE = Feed::TILE, KS = C / 16, DB = C / 32, AHEAD = 4;
+  __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
+  const int run = run_of(blockIdx.x, a.runs);
+  Feed f;
+  if (!f.start(a, run, smem)) return;
+  const int lane = f.lane, lr = lane & 31, h = lane >> 5, w = f.w, d = a.d;
 
   const unsigned base = lds_addr(smem);
   unsigned kaddr[KS], taddr[DB][2];                // of buffer 0
 #pragma unroll
-  for (int ks = 0; ks < KS; ks++) kaddr[ks] = base + lr * ROWB + (((2 * ks + h) ^ chunk_code<D>(lr)) << 4);
+  for (int ks = 0; ks < KS; ks++) kaddr[ks] = base + lr * ROWB + (((2 * ks + h) ^ Feed::code(lr)) << 4);
 #pragma unroll
   for (int db = 0; db < DB; db++)
 #pragma unroll
     for (int sx = 0; sx < 2; sx++) {
       const int j16 = lane & 15, row = 8 * sx + 4 * h + (j16 >> 2), granule = db * 4 + 2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1);
-      taddr[db][sx] = base + 2 * TILE + row * ROWB + ((granule ^ chunk_code<D>(row)) << 4) + (j16 & 1) * 8;
+      taddr[db][sx] = base + 2 * TILE + row * ROWB + ((granule ^ Feed::code(row)) << 4) + (j16 & 1) * 8;
     }
   const float c = a.scale * kLog2e;
   int buf = 0;
 #pragma unroll 1
   do {
-    const PagedSegment s = fet.g;
-    const int seg_s = fet.s, end = f_end;
-    int at = f_first;
+    const PagedSegment s = f.fet.g;
+    const int seg_s = f.fet.s, end = f.f_end;
+    int at = f.f_first;
     const PagedArgs& b = args_again<PagedArgs>();
     const ItemRow x = item_row(b, s, 32 * w + lr);
     const KeyRange see = seen_keys(b.w, s.q, x.token);
@@ -543,8 +563,8 @@ paged_chunk_kernel(PagedArgs a) {
       __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      const unsigned none = (gone >> (4 * buf)) & 15u;
-      fetch(buf ^ 1);
+      const unsigned none = f.missing(buf);
+      f.fetch(buf ^ 1);
       const int key0 = at << kTileShift;
       if (!rows_here || key0 > last.hi || key0 + kTile - 1 < first.lo) continue;   // none of the wavefront's rows sees the tile
       const unsigned tile = (unsigned)buf * TILE;
@@ -617,7 +637,8 @@ paged_chunk_kernel(PagedArgs a) {
         if (i + AHEAD < 4 * DB) read(i + AHEAD);
         if (kg < 3)
 #pragma unroll
-          for (int t = 0; t < 8 / DB; t++) prob(kg + 1, db * (8 / DB) + t);
+          for (int t = 0; t < 8; t++)
+            if (t * DB / 8 == db) prob(kg + 1, t);
         BURST_FENCE();
       }
     }
@@ -649,7 +670,166 @@ paged_chunk_kernel(PagedArgs a) {
       }
     }
     for (; redo != 0; redo &= redo - 1) row_again<bf16>(b, s, seg_s, run, kChunkRows, 32 * w + __builtin_ctz(redo), lane);
-  } while (more);
+  } while (f.more);
+}
+
+// fp32: tiles of 32 keys, products as in the short kernel, two blocks of 16 rows a wavefront (each operand of K and V read from LDS serves
+// both).  Bound by the fp32 matrix rate.
+template <int D, int C>
+__global__ void __launch_bounds__(256, 2)
+paged_chunk_f32_kernel(PagedArgs a) {
+  typedef TileFeed<float, D, kTileShiftF32> Feed;
+  constexpr int ROWB = Feed::ROWB, TILE = Feed::TILE, GR = Feed::GR, KEYS = 1 << kTileShiftF32;
+  constexpr int KS = C / 16, HV = GR / 16, OB = D / 16;   // granule steps of a product over d; 64-column parts; 16-column blocks of O^T
+  __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
+  const int run = run_of(blockIdx.x, a.runs);
+  Feed f;
+  if (!f.start(a, run, smem)) return;
+  const int lane = f.lane, r = lane & 15, g = lane >> 4, w = f.w, d = a.d;
+
+  int kaddr[KS], vaddr[4][HV];                     // in a 16-key block of a tile
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) kaddr[ks] = r * ROWB + (((4 * ks + g) ^ Feed::code(r)) << 4);
+#pragma unroll
+  for (int j = 0; j < 4; j++)
+#pragma unroll
+    for (int half = 0; half < HV; half++) vaddr[j][half] = (4 * g + j) * ROWB + (((r + 16 * half) ^ Feed::code(4 * g + j)) << 4);
+  int buf = 0;
+#pragma unroll 1
+  do {
+    const PagedSegment s = f.fet.g;
+    const int seg_s = f.fet.s, end = f.f_end;
+    int at = f.f_first;
+    const PagedArgs& b = args_again<PagedArgs>();
+    ItemRow x[2];
+    KeyRange see[2];
+    f32x4 q[2][KS], o[2][OB];
+    float m[2], l[2];                              // references (natural units); sums over this lane's keys
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      x[i] = item_row(b, s, 32 * w + 16 * i + r);
+      see[i] = seen_keys(b.w, s.q, x[i].token);
+      const float* const qr = (const float*)b.Q + (size_t)(s.q.first + (x[i].there ? x[i].token : 0)) * b.q_row + (size_t)(x[i].there ? x[i].head : 0) * b.q_head;
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) {
+        const int c = (4 * ks + g) * 4;
+        q[i][ks] = x[i].there && c < d ? *reinterpret_cast<const f32x4*>(qr + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int k = 0; k < OB; k++) o[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[i] = BURST_NEG_INF; l[i] = 0.f;
+    }
+    const int most = min(b.w.tokens, s.q.n - s.block * b.w.tokens) - 1;
+    const int t0 = s.block * b.w.tokens + 32 * w / b.part_heads, t1 = s.block * b.w.tokens + min((32 * w + 31) / b.part_heads, most);
+    const bool rows_here = 32 * w / b.part_heads <= most;
+    const KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+#pragma unroll 1
+    for (; at < end; at++, buf ^= 1) {
+      __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      const unsigned none = f.missing(buf);
+      f.fetch(buf ^ 1);
+      const int key0 = at * KEYS;
+      if (!rows_here || key0 > last.hi || key0 + KEYS - 1 < first.lo) continue;
+      const char* const kl = smem + buf * TILE;
+      const char* const vl = smem + (2 + buf) * TILE;
+      f32x4 sc[2][2];                              // [rows][keys]
+#pragma unroll
+      for (int i = 0; i < 2; i++) sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) {
+        const f32x4 k0 = *reinterpret_cast<const f32x4*>(kl + kaddr[ks]), k1 = *reinterpret_cast<const f32x4*>(kl + 16 * ROWB + kaddr[ks]);
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+          for (int i = 0; i < 2; i++) {
+            sc[i][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k0[j], q[i][ks][j], sc[i][0], 0, 0, 0);
+            sc[i][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k1[j], q[i][ks][j], sc[i][1], 0, 0, 0);
+          }
+      }
+      const bool masked = none != 0 || key0 < last.lo || key0 + KEYS - 1 > first.hi;
+      bool raise = false;
+      float mx[2];
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        mx[i] = BURST_NEG_INF;
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            float v = product(sc[i][kb][j], a.scale);
+            const int key = key0 + 16 * kb + 4 * g + j;
+            if (masked && (((none >> kb) & 1) != 0 || key < see[i].lo || key > see[i].hi)) v = BURST_NEG_INF;
+            sc[i][kb][j] = v;
+            mx[i] = fmaxf(mx[i], v);
+          }
+        raise |= mx[i] > m[i] + 8.f;
+      }
+      if (__builtin_amdgcn_ballot_w64(raise) != 0)  // see the short kernel
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          const float to = fmaxf(m[i], max_over_groups(mx[i])), alpha = fast_exp2((m[i] - (to == BURST_NEG_INF ? 0.f : to)) * kLog2e);
+          m[i] = to;
+          l[i] *= alpha;
+#pragma unroll
+          for (int k = 0; k < OB; k++) o[i][k] *= alpha;
+        }
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const float ref = m[i] == BURST_NEG_INF ? 0.f : m[i];
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            sc[i][kb][j] = fast_exp2((sc[i][kb][j] - ref) * kLog2e);
+            l[i] += sc[i][kb][j];
+          }
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+          for (int half = 0; half < HV; half++) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(vl + kb * 16 * ROWB + vaddr[j][half]);
+#pragma unroll
+            for (int c = 0; c < 4; c++)
+#pragma unroll
+              for (int i = 0; i < 2; i++) o[i][4 * half + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[c], sc[i][kb][j], o[i][4 * half + c], 0, 0, 0);
+          }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      l[i] = sum_over_groups(l[i]);
+      unsigned big = larger_of(0, l[i]);
+#pragma unroll
+      for (int k = 0; k < OB; k++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) big = larger_of(big, o[i][k][j]);
+      const unsigned long long bal = __builtin_amdgcn_ballot_w64(x[i].there && big >= kInfBits);
+      unsigned redo = (unsigned)(bal | (bal >> 16) | (bal >> 32) | (bal >> 48)) & 0xffffu;
+      if (x[i].there && !((redo >> r) & 1)) {
+        const RowPlace to = row_place(b, s, run, kChunkRows, 32 * w + 16 * i + r, x[i]);
+        const float inv = is_zero(l[i]) ? 0.f : 1.f / l[i];
+#pragma unroll
+        for (int half = 0; half < HV; half++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {            // row 4g + j of block 4 half + c holds column 64 half + 16 g + 4 j + c
+            const int col = 64 * half + 16 * g + 4 * j;
+            if (col >= d) continue;
+            const f32x4 v = {o[i][4 * half][j], o[i][4 * half + 1][j], o[i][4 * half + 2][j], o[i][4 * half + 3][j]};
+            if (to.whole) store4(b, to.o + col, v * inv);
+            else *reinterpret_cast<f32x4*>(to.part + col) = v;
+          }
+        if (g == 0) {
+          if (to.whole) b.lse[to.lse] = row_lse(m[i], l[i]);
+          else { to.ml[0] = m[i]; to.ml[kChunkRows] = l[i]; }
+        }
+      }
+      for (; redo != 0; redo &= redo - 1) row_again<float>(b, s, seg_s, run, kChunkRows, 32 * w + 16 * i + __builtin_ctz(redo), lane);
+    }
+  } while (f.more);
 }
 
 // ------------------------------------------------------------------------------- merge
@@ -747,15 +927,23 @@ int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s) {
   }
   return launch_status();
 }
-int launch_paged_chunk(const PagedArgs& a, hipStream_t s) {
+int launch_paged_chunk(const PagedArgs& a, int dtype, hipStream_t s) {
   const dim3 grid((unsigned)a.runs), block(256);
-  if (a.d <= 64) BURST_LAUNCH(paged_chunk_kernel<64>, grid, block, 0, s, a);
-  else BURST_LAUNCH(paged_chunk_kernel<128>, grid, block, 0, s, a);
+  if (dtype == BURST_BF16) {
+    if (a.d <= 32) BURST_LAUNCH((paged_chunk_kernel<64, 32>), grid, block, 0, s, a);
+    else if (a.d <= 64) BURST_LAUNCH((paged_chunk_kernel<64, 64>), grid, block, 0, s, a);
+    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_kernel<128, 96>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_chunk_kernel<128, 128>), grid, block, 0, s, a);
+  } else {
+    if (a.d <= 64) BURST_LAUNCH((paged_chunk_f32_kernel<64, 64>), grid, block, 0, s, a);
+    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_f32_kernel<128, 96>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_chunk_f32_kernel<128, 128>), grid, block, 0, s, a);
+  }
   return launch_status();
 }
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {
   if (a.runs < 2) return BURST_OK;
-  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item <= 64 ? 4 : rows_of_item / 16), dim3(256), 0, s, a, rows_of_item);
+  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item / 4), dim3(256), 0, s, a, rows_of_item);
   return launch_status();
 }
 

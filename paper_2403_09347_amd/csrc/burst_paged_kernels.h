@@ -28,7 +28,7 @@ constexpr int kShortRows = 16, kChunkRows = 128;   // rows of an item
 constexpr int kShortLds = 32768;                   // bytes of a wavefront's ring of tiles
 
 int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s);
-int launch_paged_chunk(const PagedArgs& a, hipStream_t s);
+int launch_paged_chunk(const PagedArgs& a, int dtype, hipStream_t s);
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s);
 
 #ifdef __HIPCC__

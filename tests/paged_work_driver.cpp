@@ -78,7 +78,7 @@ static void batch(bool anything) {
   w.causal = rnd(3) != 0;
   w.window = rnd(3) ? 0 : rnd(2) ? 1 + rnd(100) : 1 << 30;
   w.item_cost = rnd(4);
-  w.unit_shift = rnd(4) ? 6 : 7 + rnd(3);
+  w.unit_shift = rnd(4) ? 5 + rnd(2) : 7 + rnd(3);
   const int runs = 1 + rnd(40), slack = rnd(3) ? rnd(10) : rnd(2) * 100000;
 
   typedef std::tuple<int, int, int> Item;          // sequence, part, block
@@ -112,7 +112,7 @@ static void batch(bool anything) {
       }
       int k0, k1;
       w.keys(g.q, g.block, k0, k1);
-      for (int shift = 4; shift <= kTileShift; shift += 2) {   // what the kernels fetch: 16 keys at a time, in one page
+      for (int shift = 4; shift <= kTileShift && shift <= w.unit_shift; shift++) {   // what the kernels fetch: 16 keys at a time, in one page
         int t, end;
         segment_tiles(w, g, shift, t, end);
         CHECK(t < end);
