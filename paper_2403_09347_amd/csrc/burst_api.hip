@@ -736,9 +736,13 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   w.parts = p->kv_heads * a.parts_each;
   w.causal = p->causal != 0;
   w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
-  w.item_cost = 1;
+  // Units of 32 keys (bf16 chunks: of 64), and what an item's beginning and a join are worth of them.  us a call of the short kernel, units of
+  // 64 keys, beginning 1, slack 2 / so: one token over 32768 keys 38.2 / 37.7, over 4000 18.5 / 16.7, 64 ragged sequences 126.3 / 125.2,
+  // 256 of 16 to 300 keys 39.1 / 35.5 (beginning 1: 137 and 38.5).  The chunk kernel, slack 4 / 8: 4 sequences with a window of 1024, d = 64,
+  // 46 / 37; the others that were tried take the same time with a beginning of 0 to 3 and a slack of 4 to 16.
+  w.item_cost = plan.chunk ? 1 : 2;
   double units;                                    // at most so many: 32 bits hold them
-  for (w.unit_shift = plan.chunk && p->dtype == BURST_F32 ? burst::kTileShiftF32 : burst::kTileShift;; w.unit_shift++) {
+  for (w.unit_shift = plan.chunk && p->dtype == BURST_BF16 ? burst::kTileShift : burst::kTileShiftF32;; w.unit_shift++) {
     units = ((double)p->rows / w.tokens + p->sequences) * w.parts * ((cap >> w.unit_shift) + 2 + w.item_cost);
     if (units < 2e9) break;
     if (w.unit_shift == 20) return BURST_ERR_SHAPE;

@@ -24,7 +24,7 @@ BURST_HD PagedSeq paged_seq(int start, int end, int length, int rows, int cap) {
 
 // An item: a block of `tokens` tokens of a sequence with the query heads of one part of a key/value head's group.  Groups of more
 // heads than a block has rows are cut into parts of so many heads (and then a block has one token).
-// A unit: 1 << unit_shift keys of an item (64, fp32 chunks 32, more only where a call could have 2^31 units).  An item has the units that
+// A unit: 1 << unit_shift keys of an item (32, bf16 chunks 64, more only where a call could have 2^31 units).  An item has the units that
 // some row of it sees, and at least one, so that rows that see nothing are written too.
 constexpr int kTileShift = 6, kTileShiftF32 = 5;   // tiles of the chunk kernels; units are not smaller
 struct PagedTotals { int units, items, most, pair; };   // units of the largest item, and of two that follow one another

@@ -367,12 +367,13 @@ paged_short_kernel(PagedArgs a) {
         p0[j] = (bf16)p[j];
         p1[j] = (bf16)(p[j] - (float)p0[j]);
       }
+      s16x4 v[OB];
 #pragma unroll
-      for (int b = 0; b < OB; b++) {
-        const s16x4 v = __builtin_bit_cast(s16x4, lds_read_tr(vl, vaddr[b]));
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(s16x4, p1), o[b], 0, 0, 0);
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(s16x4, p0), o[b], 0, 0, 0);
-      }
+      for (int b = 0; b < OB; b++) v[b] = __builtin_bit_cast(s16x4, lds_read_tr(vl, vaddr[b]));
+#pragma unroll
+      for (int b = 0; b < OB; b++) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[b], __builtin_bit_cast(s16x4, p1), o[b], 0, 0, 0);
+#pragma unroll
+      for (int b = 0; b < OB; b++) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[b], __builtin_bit_cast(s16x4, p0), o[b], 0, 0, 0);
     }
     wait_lds();                                    // (the tile has been read: its slot is filled again)
     ahead--;
