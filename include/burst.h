@@ -321,13 +321,14 @@ int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d,
 /* The new tokens of several sequences and the pages of their caches.  New tokens lie packed, sequence after sequence:
  * sequence s has rows starts[s] .. starts[s + 1] - 1 of the token tensors, which are indexed [row, head, d].  lengths[s] counts
  * the tokens of the sequence, the new ones among them: new token t of n is at position lengths[s] - n + t, and position p
- * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to width * page and to >= 0, starts to 0 .. rows
- * and to ascending order; a page that is not in 0 .. pages - 1 holds no keys. */
+ * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to 0 .. width * page and starts to 0 .. rows, a
+ * sequence that ends before it starts has no tokens, and a page that is not in 0 .. pages - 1 holds no keys.  The arrays are not to
+ * change while a call that reads them runs. */
 typedef struct burst_paged_params {
   int32_t sequences, rows;           /* >= 0, < 2^30; rows: of the token tensors, those behind the last sequence among them */
   int32_t H, kv_heads, d, dtype;     /* H a multiple of kv_heads; d a multiple of 8 (bf16) or 4 (fp32), at most 128 */
   int32_t pages, page, width;        /* pages; rows of a page: a power of two, 16 or more; pages of a table row; width * page < 2^30 */
-  int32_t max_new;                   /* most new tokens of any sequence as far as the caller knows it, 0 = not known: chooses kernels only */
+  int32_t max_new;                   /* most new tokens of any sequence as far as the caller knows it, 0 = not known: chooses the kernel only */
   int32_t causal;                    /* burst_paged_fwd: 0 = every key of the sequence is visible, 1 = those up to the token's position */
   int32_t out_f32;                   /* burst_paged_fwd: 1 = O is fp32 whatever the dtype */
   float   scale;                     /* burst_paged_fwd: as in burst_params */
@@ -337,7 +338,7 @@ typedef struct burst_paged_params {
   int64_t table_stride;              /* entries from one sequence's pages to the next's; 0 = width */
   int64_t page_strides[3];           /* elements {page, head, row} of K_pages and V_pages; all zero = dense [pages, kv_heads, page, d] */
   int64_t q_strides[2], kv_strides[2], o_strides[2];   /* elements {row, head} of Q; of K and V (new tokens); of O or Q_out; both zero = dense.
-                                      * Strides of 16 bytes' multiples (burst_cache_append: any), none negative */
+                                      * Strides in multiples of 16 bytes (burst_cache_append: any), none negative */
 } burst_paged_params;
 /* Writes the new tokens' keys and values (K, V [rows, kv_heads, d]) to their places in K_pages and V_pages, the keys rotated by their
  * positions + offsets[s] (int64 DEVICE [sequences], NULL: 0; what the ring keeps before this device's share).  r = NULL: nothing is rotated.

@@ -704,7 +704,8 @@ int check_paged(const burst_paged_params* p, Paged& g, bool attend) {
   const long long q[2] = {p->H * d, d}, kv[2] = {p->kv_heads * d, d}, page[3] = {p->kv_heads * p->page * d, p->page * d, d};
   // (the attention reads and writes 16 bytes at a time; rows of a page must not overlap, and 16 of them lie within 2 GiB)
   const long long u = attend ? unit : 1;
-  if (!set_strides(g.q, p->q_strides, q, u) || !set_strides(g.kv, p->kv_strides, kv, u) || !set_strides(g.o, p->o_strides, q, u) ||
+  if (!set_strides(g.q, p->q_strides, q, u) || !set_strides(g.kv, p->kv_strides, kv, u) ||
+      !set_strides(g.o, p->o_strides, q, attend && p->out_f32 != 0 ? 4 : u) ||
       !set_strides(g.page, p->page_strides, page, u)) return BURST_ERR_SHAPE;
   if (g.page[2] < d || g.page[2] >= 1LL << 25) return BURST_ERR_SHAPE;
   return BURST_OK;

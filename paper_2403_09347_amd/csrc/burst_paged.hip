@@ -559,6 +559,10 @@ paged_chunk_kernel(PagedArgs a) {
     const int t0 = s.block * b.w.tokens + 32 * w / b.part_heads, t1 = s.block * b.w.tokens + min((32 * w + 31) / b.part_heads, most);
     const bool rows_here = 32 * w / b.part_heads <= most;
     const KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+    // Rows of few keys have P in two terms, 16 bits of it: their outputs are not small against V, and what rounding P to 8 bits does to them
+    // would be seen beside the rounding of O.  (5 tokens of 23 keys: O is 2.7e-3 of its norm off 64 bits with one term, 1.7e-3 with two, as with an exact P;
+    // 64 tokens of 500 keys, one term, 2.3e-3.)
+    const bool few = last.hi - first.lo < 256;
 #pragma unroll 1
     for (; at < end; at++, buf ^= 1) {
       __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
@@ -641,6 +645,19 @@ paged_chunk_kernel(PagedArgs a) {
           for (int t = 0; t < 8; t++)
             if (t * DB / 8 == db) prob(kg + 1, t);
         BURST_FENCE();
+      }
+      if (few) {
+#pragma unroll
+        for (int kg = 0; kg < 4; kg++) {
+          bf16x8 rest;
+#pragma unroll
+          for (int t = 0; t < 8; t++) rest[t] = (bf16)(fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t], c, nref)) - (float)p[kg][t]);
+#pragma unroll
+          for (int db = 0; db < DB; db++) {
+            const unsigned at = tile + kg * 16 * ROWB;
+            o[db] = mfma32(__builtin_shufflevector(lds_tr(taddr[db][0] + at), lds_tr(taddr[db][1] + at), 0, 1, 2, 3, 4, 5, 6, 7), rest, o[db]);
+          }
+        }
       }
     }
     l = sum_both_halves(l);
@@ -854,16 +871,18 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
   __shared__ __attribute__((aligned(16))) float side[4][160];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (lane & 15) * 4;
   const int run = blockIdx.x + 1, d = a.d;
-  const PagedJoin join = a.join[run];
-  if (join.n == 0) return;
-  const bool alone = join.n <= 8, together = join.n > 32;   // a lane group on a row; all wavefronts on a row
+  PagedJoin join = a.join[run];
+  if (join.n <= 0) return;
+  join.n = min(join.n, a.runs - run + 1);          // (as they are; no access outside the workspace and the outputs if another call has written there)
+  const bool few = rows_of_item <= kShortRows;
+  const bool alone = join.n <= (few ? 8 : 32), together = join.n > (few ? 32 : 128);   // a lane group on a row; all wavefronts on a row
   const size_t slot = (size_t)rows_of_item * (d + 2);
   const float* const base = a.part + 2 * (size_t)(run - 1) * slot;
   const int step = alone ? 1 : together ? 16 : 4, begin = alone ? 0 : (together ? 4 * wave : 0) + (lane >> 4);
   const int rows = 16 / step;                      // of a workgroup at a time
   for (int r = blockIdx.y * rows + (alone ? 4 * wave + (lane >> 4) : together ? 0 : wave); r < rows_of_item; r += rows * gridDim.y) {
     const ItemRow x = item_row(a, join.part, join.block, join.count, r);
-    if (!x.there) continue;                        // (the same for all lanes that share a row)
+    if (!x.there || (unsigned)(join.first + x.token) >= (unsigned)a.w.rows || (unsigned)x.head >= (unsigned)a.heads) continue;   // (lanes that share a row alike)
     Joined sum = {BURST_NEG_INF, 0.f, {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
     for (int i0 = begin; i0 < join.n; i0 += 8 * step) {
       float m[8], l[8];
@@ -944,7 +963,7 @@ int launch_paged_chunk(const PagedArgs& a, int dtype, hipStream_t s) {
 }
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {
   if (a.runs < 2) return BURST_OK;
-  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item / 4), dim3(256), 0, s, a, rows_of_item);
+  BURST_LAUNCH(paged_merge_kernel, dim3((unsigned)a.runs - 1, rows_of_item <= kShortRows ? 4 : 16), dim3(256), 0, s, a, rows_of_item);
   return launch_status();
 }
 

@@ -308,7 +308,7 @@ class Rotate : public torch::autograd::Function<Rotate> {
  public:
   // xp: n tensors, then the positions of those that have some (position_of)
   static variable_list forward(AutogradContext* ctx, const Tensor& turns, at::TensorList xp, int64_t n, const std::vector<int64_t>& position_of,
-                               const std::vector<int64_t>& offsets, bool interleaved, double amplitude) {
+                               const std::vector<int64_t>& offsets, bool interleaved, double amplitude, bool inverse) {
     const variable_list xs(xp.begin(), xp.begin() + n), positions(xp.begin() + n, xp.end());
     variable_list saved = {turns};
     saved.insert(saved.end(), positions.begin(), positions.end());
@@ -317,24 +317,36 @@ class Rotate : public torch::autograd::Function<Rotate> {
     ctx->saved_data["offsets"] = offsets;
     ctx->saved_data["interleaved"] = interleaved;
     ctx->saved_data["amplitude"] = amplitude;
+    ctx->saved_data["inverse"] = inverse;
     ctx->saved_data["type"] = (int64_t)xs[0].scalar_type();
     ctx->set_materialize_grads(false);
-    return rotate_all(xs, turns, positions, position_of, offsets, interleaved, amplitude, false);
+    return rotate_all(xs, turns, positions, position_of, offsets, interleaved, amplitude, inverse);
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
     const variable_list s = ctx->get_saved_variables();
     const variable_list positions(s.begin() + 1, s.end());
     const auto position_of = ctx->saved_data["position_of"].toIntVector(), offsets = ctx->saved_data["offsets"].toIntVector();
-    variable_list out(1 + grads.size() + positions.size() + 5), some;
+    variable_list out(1 + grads.size() + positions.size() + 6), some;
     std::vector<int64_t> at, off;
+    variable_list where;                          // positions of the gradients that there are
     for (size_t i = 0; i < grads.size(); i++)
       if (grads[i].defined()) {
         some.push_back(grads[i].to((c10::ScalarType)ctx->saved_data["type"].toInt()));
-        at.push_back(position_of[i]);
+        at.push_back(position_of[i] >= 0 ? (int64_t)where.size() : -1);
+        if (position_of[i] >= 0) where.push_back(positions[position_of[i]]);
         off.push_back(offsets[i]);
       }
     if (some.empty()) return out;
-    const variable_list g = rotate_all(some, s[0], positions, at, off, ctx->saved_data["interleaved"].toBool(), ctx->saved_data["amplitude"].toDouble(), true);
+    const bool interleaved = ctx->saved_data["interleaved"].toBool(), inverse = !ctx->saved_data["inverse"].toBool();
+    const double amplitude = ctx->saved_data["amplitude"].toDouble();
+    variable_list g;
+    if (at::GradMode::is_enabled()) {              // (create_graph: the gradient is a rotation again)
+      variable_list gp(some);
+      gp.insert(gp.end(), where.begin(), where.end());
+      g = Rotate::apply(s[0], at::TensorList(gp), (int64_t)some.size(), at, off, interleaved, amplitude, inverse);
+    } else {
+      g = rotate_all(some, s[0], where, at, off, interleaved, amplitude, inverse);
+    }
     for (size_t i = 0, k = 0; i < grads.size(); i++)
       if (grads[i].defined()) out[1 + i] = g[k++];
     return out;
@@ -343,6 +355,7 @@ class Rotate : public torch::autograd::Function<Rotate> {
 void check_turns(const Tensor& turns, int64_t d, const Tensor& like) {
   TORCH_CHECK_VALUE(turns.scalar_type() == torch::kDouble && turns.dim() == 1 && turns.is_contiguous() && turns.device() == like.device(),
                     "turns: contiguous float64 tensor [pairs] on the tensors' device expected");
+  TORCH_CHECK_VALUE(!turns.requires_grad(), "turns: a tensor that needs no gradient expected");
   TORCH_CHECK_VALUE(turns.numel() >= 1 && 2 * turns.numel() <= d, "turns: between one pair and all of the head's columns expected");
 }
 std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, const std::vector<int64_t>& offsets,
@@ -363,7 +376,7 @@ std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, c
                       p->size(-1) == xs[i].size(2), "positions: int64 [rows] or [B, rows] on the tensors' device expected");
     xp.push_back(p->size(-1) <= 1 || p->stride(-1) == 1 ? *p : p->contiguous());
   }
-  return Rotate::apply(turns, at::TensorList(xp), (int64_t)xs.size(), position_of, offsets, interleaved, amplitude);
+  return Rotate::apply(turns, at::TensorList(xp), (int64_t)xs.size(), position_of, offsets, interleaved, amplitude, false);
 }
 
 // ---- paged: new tokens [rows, heads, d], pages [pages, kv_heads, page, d]

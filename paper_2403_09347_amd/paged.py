@@ -6,8 +6,8 @@ Several sequences at once: token tensors [rows, heads, d] hold the new tokens of
 (views of a packed projection are read in place); lengths[s] counts all tokens of the sequence, the new ones among them; position p of
 it is row p % page of page table[s, p // page] of k_pages and v_pages [pages, kv_heads, page, d] (any strides with a contiguous last
 dimension; page: a power of two, 16 or more).  table, lengths and starts are int32 tensors on the device and are read there, so
-that a captured call can be replayed with other contents; values outside their ranges are cut to them, and a page that is
-not one of the pages holds no keys."""
+that a captured call can be replayed with other contents (they are not to change while a call runs); values outside their
+ranges are cut to them, and a page that is not one of the pages holds no keys."""
 from . import binding as B
 
 

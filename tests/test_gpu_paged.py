@@ -37,6 +37,34 @@ def test_groups(dtype, H, KV, new):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+def test_groups_of_more_heads_than_a_block_has_rows(dtype):
+    b = Batch([90, 300], [2, 1], 150, 1, 32, dtype=dtype, seed=1)
+    for max_new in (0, 2):
+        O, lse = attend(b, max_new=max_new)
+        b.check(O, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_new_tokens_than_the_caller_said(dtype):
+    """max_new chooses the kernel: one that is too small changes no result beyond rounding."""
+    b = Batch([300, 70, 5], [45, 1, 5], 4, 2, 64, dtype=dtype)
+    O, lse = attend(b, max_new=1)
+    b.check(O, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 40])
+def test_a_cache_without_pages(dtype, new):
+    b = Batch([100], [new], 4, 2, 64, dtype=dtype)
+    none = b.k_pages[:0].contiguous()
+    O, lse = burst_paged_attention(b.q, none, none, b.table, b.lengths, b.starts)
+    assert (O == 0).all() and torch.isneginf(lse).all()
+    O, lse = burst_paged_attention(b.q, b.k_pages, b.v_pages, b.table[:, :0], b.lengths, b.starts)
+    assert (O == 0).all() and torch.isneginf(lse).all()
+    burst_cache_append(b.k, b.v, none, none.clone(), b.table, b.lengths, b.starts)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("page,pool,packed", [(16, "head", False), (16, "seq", True), (32, "seq", False), (64, "head", True), (128, "seq", True), (1024, "head", False)])
 @pytest.mark.parametrize("d", [128, 64])
 def test_chunks_and_layouts(dtype, page, pool, packed, d):

@@ -100,11 +100,32 @@ def test_gradient_against_differences():
     assert abs((quotient * f64(g)).sum() - (f64(dx) * f64(u)).sum()) <= 1728 * 10 * 2.0 ** -22
 
 
+def test_gradients_of_gradients():
+    """The gradient is linear in what it is given: its gradient turns forward again."""
+    x, g, u = (rand(1, 2, 11, 32, seed=i).requires_grad_(i < 2) for i in range(3))
+    pos = torch.randint(0, 1 << 20, (11,), generator=torch.Generator().manual_seed(3)).to(DEV)
+    y = burst_rotary([x, x.detach()], default_turns(32), 5, positions=[pos, None], interleaved=True)
+    (dx,) = torch.autograd.grad(y[0], x, g, create_graph=True)
+    check_rotation("dx", dx, g, 5 + f64(pos)[None, None], f64(default_turns(32)), True, inverse=True)
+    (dg,) = torch.autograd.grad(dx, g, u)
+    check_rotation("dg", dg, u, 5 + f64(pos)[None, None], f64(default_turns(32)), True)
+
+
 def test_a_gradient_of_a_sum():
     """Its gradient is one value seen everywhere, with strides of 0."""
     x = rand(1, 2, 9, 16).requires_grad_(True)
     burst_rotary(x, default_turns(16)).sum().backward()
     check_rotation("dx", x.grad, torch.ones_like(x), np.arange(9)[None, None], f64(default_turns(16)), inverse=True)
+
+
+def test_refusals():
+    x, t = rand(1, 2, 3, 64), default_turns(64)
+    for bad in (dict(x=x.half()), dict(x=x[0]), dict(x=[x, x.to(BF16)]), dict(x=[x, x[..., :32]]), dict(turns=t.float()), dict(turns=t.cpu()),
+                dict(turns=default_turns(66)), dict(turns=t[:0]), dict(turns=t[::2]), dict(turns=t.clone().requires_grad_(True)),
+                dict(positions=torch.arange(4, device=DEV)), dict(positions=torch.arange(3)), dict(positions=torch.arange(3, device=DEV).int()),
+                dict(positions=torch.zeros(2, 3, dtype=torch.int64, device=DEV)), dict(offset=[1, 2]), dict(amplitude=float("nan"))):
+        with pytest.raises((ValueError, RuntimeError)):
+            burst_rotary(**dict(dict(x=x, turns=t), **bad))
 
 
 @pytest.mark.parametrize("scaling,factor", [("linear", 4.0), ("ntk", 8.0), ("yarn", 16.0)])
