@@ -8,6 +8,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/functions/utils.h>
 
 #include <cmath>
 #include <optional>
@@ -304,54 +305,61 @@ variable_list rotate_all(const variable_list& xs, const Tensor& turns, const var
                      stream_of(like)), "burst_rotate");
   return out;
 }
-class Rotate : public torch::autograd::Function<Rotate> {
- public:
-  // xp: n tensors, then the positions of those that have some (position_of)
-  static variable_list forward(AutogradContext* ctx, const Tensor& turns, at::TensorList xp, int64_t n, const std::vector<int64_t>& position_of,
-                               const std::vector<int64_t>& offsets, bool interleaved, double amplitude, bool inverse) {
-    const variable_list xs(xp.begin(), xp.begin() + n), positions(xp.begin() + n, xp.end());
-    variable_list saved = {turns};
-    saved.insert(saved.end(), positions.begin(), positions.end());
-    ctx->save_for_backward(saved);
-    ctx->saved_data["position_of"] = position_of;
-    ctx->saved_data["offsets"] = offsets;
-    ctx->saved_data["interleaved"] = interleaved;
-    ctx->saved_data["amplitude"] = amplitude;
-    ctx->saved_data["inverse"] = inverse;
-    ctx->saved_data["type"] = (int64_t)xs[0].scalar_type();
-    ctx->set_materialize_grads(false);
-    return rotate_all(xs, turns, positions, position_of, offsets, interleaved, amplitude, inverse);
-  }
-  static variable_list backward(AutogradContext* ctx, variable_list grads) {
-    const variable_list s = ctx->get_saved_variables();
-    const variable_list positions(s.begin() + 1, s.end());
-    const auto position_of = ctx->saved_data["position_of"].toIntVector(), offsets = ctx->saved_data["offsets"].toIntVector();
-    variable_list out(1 + grads.size() + positions.size() + 6), some;
-    std::vector<int64_t> at, off;
-    variable_list where;                          // positions of the gradients that there are
-    for (size_t i = 0; i < grads.size(); i++)
-      if (grads[i].defined()) {
-        some.push_back(grads[i].to((c10::ScalarType)ctx->saved_data["type"].toInt()));
-        at.push_back(position_of[i] >= 0 ? (int64_t)where.size() : -1);
-        if (position_of[i] >= 0) where.push_back(positions[position_of[i]]);
-        off.push_back(offsets[i]);
-      }
-    if (some.empty()) return out;
-    const bool interleaved = ctx->saved_data["interleaved"].toBool(), inverse = !ctx->saved_data["inverse"].toBool();
-    const double amplitude = ctx->saved_data["amplitude"].toDouble();
-    variable_list g;
-    if (at::GradMode::is_enabled()) {              // (create_graph: the gradient is a rotation again)
-      variable_list gp(some);
-      gp.insert(gp.end(), where.begin(), where.end());
-      g = Rotate::apply(s[0], at::TensorList(gp), (int64_t)some.size(), at, off, interleaved, amplitude, inverse);
-    } else {
-      g = rotate_all(some, s[0], where, at, off, interleaved, amplitude, inverse);
+// What a rotation is, but for its tensors; position_of: for each tensor the place of its positions, -1 = none.
+struct Turning {
+  std::vector<int64_t> position_of, offsets;
+  bool interleaved;
+  double amplitude;
+  bool inverse;
+};
+variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns, const variable_list& positions, const Turning& how);
+// (A node of its own instead of a torch::autograd::Function, whose saved values go through a dictionary: host us of a call on two tensors with
+// its gradients 73 so, 69 here, of which two views with theirs take 54.)
+struct RotateBackward : public torch::autograd::Node {
+  torch::autograd::SavedVariable turns;
+  std::vector<torch::autograd::SavedVariable> positions;
+  Turning how;
+  at::ScalarType type;
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(grads.size()), some, where;
+    Turning back{{}, {}, how.interleaved, how.amplitude, !how.inverse};
+    for (size_t i = 0; i < grads.size(); i++) {
+      if (!grads[i].defined()) continue;
+      some.push_back(grads[i].scalar_type() == type ? grads[i] : grads[i].to(type));
+      back.position_of.push_back(how.position_of[i] >= 0 ? (int64_t)where.size() : -1);
+      if (how.position_of[i] >= 0) where.push_back(positions[how.position_of[i]].unpack());
+      back.offsets.push_back(how.offsets[i]);
     }
+    if (some.empty()) return out;
+    const variable_list g = rotate_differentiably(some, turns.unpack(), where, back);   // (create_graph: a rotation again)
     for (size_t i = 0, k = 0; i < grads.size(); i++)
-      if (grads[i].defined()) out[1 + i] = g[k++];
+      if (grads[i].defined()) out[i] = g[k++];
     return out;
   }
+  void release_variables() override {
+    turns.reset_data();
+    for (auto& p : positions) p.reset_data();
+  }
+  std::string name() const override { return "BurstRotaryBackward"; }
 };
+variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns, const variable_list& positions, const Turning& how) {
+  std::shared_ptr<RotateBackward> node;
+  if (at::GradMode::is_enabled() && torch::autograd::any_variable_requires_grad(xs)) {
+    node = std::shared_ptr<RotateBackward>(new RotateBackward(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(xs));
+    node->turns = torch::autograd::SavedVariable(turns, false);
+    for (const Tensor& p : positions) node->positions.emplace_back(p, false);
+    node->how = how;
+    node->type = xs[0].scalar_type();
+  }
+  variable_list out;
+  {
+    const at::NoGradGuard no_grad;
+    out = rotate_all(xs, turns, positions, how.position_of, how.offsets, how.interleaved, how.amplitude, how.inverse);
+  }
+  if (node) torch::autograd::set_history(out, node);
+  return out;
+}
 void check_turns(const Tensor& turns, int64_t d, const Tensor& like) {
   TORCH_CHECK_VALUE(turns.scalar_type() == torch::kDouble && turns.dim() == 1 && turns.is_contiguous() && turns.device() == like.device(),
                     "turns: contiguous float64 tensor [pairs] on the tensors' device expected");
@@ -366,17 +374,17 @@ std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, c
                       (x.scalar_type() == torch::kBFloat16 || x.scalar_type() == torch::kFloat),
                       "[B, heads, rows, d] tensors of bfloat16 or float32, of one type, d and device, expected");
   check_turns(turns, xs[0].size(3), xs[0]);
-  variable_list xp(xs);
-  std::vector<int64_t> position_of;
+  Turning how{{}, offsets, interleaved, amplitude, false};
+  variable_list at;
   for (size_t i = 0; i < xs.size(); i++) {
     const auto& p = positions[i];
-    position_of.push_back(p.has_value() ? (int64_t)(xp.size() - xs.size()) : -1);
+    how.position_of.push_back(p.has_value() ? (int64_t)at.size() : -1);
     if (!p.has_value()) continue;
     TORCH_CHECK_VALUE(p->scalar_type() == torch::kLong && p->device() == xs[i].device() && (p->dim() == 1 || (p->dim() == 2 && p->size(0) == xs[i].size(0))) &&
                       p->size(-1) == xs[i].size(2), "positions: int64 [rows] or [B, rows] on the tensors' device expected");
-    xp.push_back(p->size(-1) <= 1 || p->stride(-1) == 1 ? *p : p->contiguous());
+    at.push_back(p->size(-1) <= 1 || p->stride(-1) == 1 ? *p : p->contiguous());
   }
-  return Rotate::apply(turns, at::TensorList(xp), (int64_t)xs.size(), position_of, offsets, interleaved, amplitude, false);
+  return rotate_differentiably(xs, turns, at, how);
 }
 
 // ---- paged: new tokens [rows, heads, d], pages [pages, kv_heads, page, d]

@@ -111,6 +111,50 @@ def test_gradients_of_gradients():
     check_rotation("dg", dg, u, 5 + f64(pos)[None, None], f64(default_turns(32)), True)
 
 
+def test_the_graph_is_freed_kept_and_guarded_as_torchs_own():
+    x, t = rand(1, 2, 9, 16).requires_grad_(True), default_turns(16)
+    pos = torch.arange(9, device=DEV)
+    y = burst_rotary(x, t, positions=pos)
+    one, two = (torch.autograd.grad(y, x, torch.ones_like(y), retain_graph=True)[0] for _ in range(2))
+    assert torch.equal(one, two)
+    torch.autograd.grad(y, x, torch.ones_like(y))
+    with pytest.raises(RuntimeError):                         # freed
+        torch.autograd.grad(y, x, torch.ones_like(y))
+    y = burst_rotary(x, t, positions=pos)
+    pos.add_(1)
+    with pytest.raises(RuntimeError):                         # changed in place
+        torch.autograd.grad(y, x, torch.ones_like(y))
+    with torch.no_grad():
+        assert not burst_rotary(x, t).requires_grad
+    assert not burst_rotary(x.detach(), t).requires_grad
+    a, b = burst_rotary([x, x.detach()], t)
+    a.sum().backward()                                        # one of two outputs used
+    assert x.grad is not None
+
+
+def test_captured_gradients():
+    """Forward and backward recorded together, replayed with other inputs and eager work in between."""
+    x, g, t = rand(1, 4, 200, 64, dtype=BF16).requires_grad_(True), rand(1, 4, 200, 64, dtype=BF16, seed=2), default_turns(64)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(burst_rotary(x, t, 9), x, g)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = burst_rotary(x, t, 9)
+        (dx,) = torch.autograd.grad(y, x, g)
+    for seed in (3, 4, 5):
+        with torch.no_grad():
+            x.copy_(rand(1, 4, 200, 64, dtype=BF16, seed=seed))
+        g.copy_(rand(1, 4, 200, 64, dtype=BF16, seed=seed + 10))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_rotation("y", y, x, 9 + np.arange(200)[None, None], f64(t))
+        check_rotation("dx", dx, g, 9 + np.arange(200)[None, None], f64(t), inverse=True)
+
+
 def test_a_gradient_of_a_sum():
     """Its gradient is one value seen everywhere, with strides of 0."""
     x = rand(1, 2, 9, 16).requires_grad_(True)
