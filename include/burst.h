@@ -321,8 +321,9 @@ int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d,
 /* The new tokens of several sequences and the pages of their caches.  New tokens lie packed, sequence after sequence:
  * sequence s has rows starts[s] .. starts[s + 1] - 1 of the token tensors, which are indexed [row, head, d].  lengths[s] counts
  * the tokens of the sequence, the new ones among them: new token t of n is at position lengths[s] - n + t, and position p
- * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to 0 .. width * page and starts to 0 .. rows, a
- * sequence that ends before it starts has no tokens, and a page that is not in 0 .. pages - 1 holds no keys.  The arrays are not to
+ * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to 0 .. width * page and starts to 0 .. rows, and a
+ * page that is not in 0 .. pages - 1 holds no keys.  Starts do not decrease: where they do, burst_paged_fwd writes nothing, and which tokens
+ * burst_cache_append takes for whose is not defined.  The arrays are not to
  * change while a call that reads them runs. */
 typedef struct burst_paged_params {
   int32_t sequences, rows;           /* >= 0, < 2^30; rows: of the token tensors, those behind the last sequence among them */

@@ -701,7 +701,7 @@ int check_paged(const burst_paged_params* p, Paged& g, bool attend) {
   if (p->table_stride != 0 && p->table_stride < p->width) return BURST_ERR_SHAPE;
   g.table_stride = p->table_stride != 0 ? p->table_stride : p->width;
   g.page_shift = __builtin_ctz((unsigned)p->page);
-  const long long q[2] = {p->H * d, d}, kv[2] = {p->kv_heads * d, d}, page[3] = {p->kv_heads * p->page * d, p->page * d, d};
+  const long long q[2] = {p->H * d, d}, kv[2] = {p->kv_heads * d, d}, page[3] = {d * p->kv_heads * p->page, d * p->page, d};
   // (the attention reads and writes 16 bytes at a time; rows of a page must not overlap, and 16 of them lie within 2 GiB)
   const long long u = attend ? unit : 1;
   if (!set_strides(g.q, p->q_strides, q, u) || !set_strides(g.kv, p->kv_strides, kv, u) ||

@@ -57,29 +57,33 @@ struct PagedWork {
     lo = k0 >> unit_shift;
     hi = k1 > k0 ? ((k1 - 1) >> unit_shift) + 1 : lo + 1;
   }
-  // all blocks of a sequence, for one part of a head
-  BURST_HD PagedTotals totals(const PagedSeq& q) const {
-    PagedTotals t = {0, 0, 0, 0};
-    if (q.n <= 0) return t;
-    const int n = blocks(q);
-    t.items = n;
-    int first = 0, last = 0;
-    for (int b = 0; b < n; b++) {
-      int lo, hi;
-      units(q, b, lo, hi);
-      last = hi - lo + item_cost;
-      if (b == 0) first = last;
-      t.units += last;
-      if (last > t.most) t.most = last;
+  BURST_HD int cost(const PagedSeq& q, int block) const {   // units, an item's beginning among them
+    int lo, hi;
+    units(q, block, lo, hi);
+    return hi - lo + item_cost;
+  }
+  // blocks from, from + step .. of the n of a sequence, for one part of a head: all blocks' number, these ones' units, and those of the largest
+  BURST_HD PagedTotals totals(const PagedSeq& q, int n, int from, int step) const {
+    PagedTotals t = {0, n, 0, 0};
+    for (int b = from; b < n; b += step) {
+      const int c = cost(q, b);
+      t.units += c;
+      if (c > t.most) t.most = c;
     }
-    t.pair = in_turn() && n > 1 ? first + last + (tokens >> unit_shift) + 2 : 2 * t.most;   // (rounded up)
     return t;
   }
+  // units of two blocks that follow one another, at most; most: of the largest block
+  BURST_HD int pair(const PagedSeq& q, int n, int most) const {
+    return in_turn() && n > 1 ? cost(q, 0) + cost(q, n - 1) + (tokens >> unit_shift) + 2 : 2 * most;   // (rounded up)
+  }
+  // Whether a sequence ends behind its start.  Where one does not, rows could belong to several sequences, and there could be more units than
+  // 32 bits hold: such a call does nothing.
+  static BURST_HD bool in_order(int start, int end) { return start <= end; }
 };
 
-// How the parts, blocks and units of all sequences (sequence, part, place of the block, unit, the last one fastest) are dealt out to runs: `each` units a
-// run (the items' beginnings among them: a run that ends within one leaves the item to the next), or, where that costs less, `each` whole items, of which nothing has to be joined.
-// `slack`: the units that a run may have more for that.
+// How the parts, blocks and units of all sequences (sequence, part, place of the block, unit, the last one fastest) are dealt out to runs:
+// `each` units a run (the items' beginnings among them: a run that ends within one leaves the item to the next), or, where that costs
+// less, `each` whole items, of which nothing has to be joined.  `slack`: the units that a run may have more for that.
 struct PagedDeal { int each, by_items; };
 BURST_HD PagedDeal paged_deal(const PagedTotals& t, int runs, int slack) {
   PagedDeal d;
@@ -108,15 +112,17 @@ struct PagedCursor {
     return paged_seq(Read::at(w.starts, s), Read::at(w.starts, s + 1), Read::at(w.lengths, s), w.rows, w.cap);
   }
   // the place `rem` units (items) into sequence s, which has more of them (`one` for each part of a head); false: the run, of `run`
-  // units, ends within the beginning of an item
-  BURST_HD bool place(const PagedWork& w, int seq, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run) {
+  // units, ends within the beginning of an item.  Skip: (part's units, blocks) -> the place of a block that is not behind the one sought, and
+  // takes the units before it away.
+  template <typename Skip>
+  BURST_HD bool place(const PagedWork& w, int seq, const PagedSeq& q, int one, int rem, const PagedDeal& d, int run, const Skip& skip) {
     by_items = d.by_items;
     s = seq;
     g.q = q;
     g.part = (int)((unsigned)rem / (unsigned)one);
     rem -= g.part * one;
     const int n = w.blocks(g.q);
-    for (at = by_items ? rem : 0;; at++) {
+    for (at = by_items ? rem : skip(rem, n);; at++) {
       g.block = w.block_at(at, n);
       w.units(g.q, g.block, g.lo, g.hi);
       if (by_items || rem < g.hi - g.lo + w.item_cost) break;

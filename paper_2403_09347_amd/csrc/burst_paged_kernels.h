@@ -64,16 +64,40 @@ __device__ __forceinline__ int wave_most(int x) {  // of numbers that are not ne
 }
 // The start of run `run`, by a wavefront: every lane adds up a sequence.  False: the run has nothing to do.  The merging launch is told
 // what the run's start has cut (`tell`).
+// Of sequences with many blocks the lanes share the blocks where there are few such sequences: going through them takes as long as
+// the longest has blocks, sharing about four blocks' time for every 64.  (us a call, lanes by themselves / so: 131072 tokens with a window of
+// 1024, 8 heads over one, 1361 / 817; 16384 tokens causal 657 / 591; 4096, 32 heads over 8, 158 / 152; single tokens 0.1 more.)
 __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane, bool tell, DeviceCursor& cur) {
   const PagedWork& w = a.w;
   PagedSeq q;
   PagedTotals mine = {0, 0, 0, 0}, all = {0, 0, 0, 0};
+  unsigned long long disorder = 0;
   auto totals = [&](int s) __attribute__((always_inline)) {
-    mine = PagedTotals{0, 0, 0, 0};
+    q = PagedSeq{0, 0, 0};
+    bool bad = false;
     if (s < w.sequences) {
-      q = paged_seq(w.starts[s], w.starts[s + 1], w.lengths[s], w.rows, w.cap);
-      mine = w.totals(q);
+      const int start = w.starts[s], end = w.starts[s + 1];
+      bad = !PagedWork::in_order(start, end);
+      q = paged_seq(start, end, w.lengths[s], w.rows, w.cap);
     }
+    disorder |= __builtin_amdgcn_ballot_w64(bad);
+    const int n = w.blocks(q);
+    unsigned long long longer = __builtin_amdgcn_ballot_w64(n > 8);
+    if (longer != 0) {
+      const int most = wave_most(n);
+      if (4LL * __builtin_popcountll(longer) * ((most + 63) / 64) >= most) longer = 0;
+    }
+    if (((longer >> lane) & 1) == 0) mine = w.totals(q, n, 0, 1);
+#pragma unroll 1
+    for (; longer != 0; longer &= longer - 1) {
+      const int at = __builtin_ctzll(longer);
+      const PagedSeq there = {0, __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at)};
+      PagedTotals t = w.totals(there, __builtin_amdgcn_readlane(n, at), lane, 64);
+      t.units = __builtin_amdgcn_readlane(wave_scan(t.units), 63);
+      t.most = wave_most(t.most);
+      if (lane == at) mine = t;
+    }
+    mine.pair = w.pair(q, n, mine.most);
   };
 #pragma unroll 1
   for (int base = 0; base < w.sequences; base += 64) {
@@ -86,7 +110,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
   const PagedDeal deal = paged_deal(all, a.runs, a.slack);
   const int total = deal.by_items ? all.items : all.units;
   const long long from = (long long)deal.each * run;
-  bool some = from < total;
+  bool some = disorder == 0 && from < total;
   if (some) {
     const int begin = (int)from;
     int before = 0, scan = 0, own = 0, base = 0;
@@ -102,7 +126,21 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(begin < before + scan));
     const PagedSeq there = {__builtin_amdgcn_readlane(q.first, at), __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at)};
     const int one = __builtin_amdgcn_readlane(deal.by_items ? mine.items : mine.units, at);
-    some = cur.place(w, base + at, there, one, begin - (before + __builtin_amdgcn_readlane(scan - own, at)), deal, min(deal.each, total - begin));
+    some = cur.place(w, base + at, there, one, begin - (before + __builtin_amdgcn_readlane(scan - own, at)), deal, min(deal.each, total - begin),
+                     [&](int& rem, int n) __attribute__((always_inline)) {   // 64 blocks at a time
+                       int place = 0;
+#pragma unroll 1
+                       for (; n - place > 8; place += 64) {
+                         const int c = place + lane < n ? w.cost(there, w.block_at(place + lane, n)) : 0, sum = wave_scan(c);
+                         if (rem < __builtin_amdgcn_readlane(sum, 63)) {
+                           const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rem < sum));
+                           rem -= __builtin_amdgcn_readlane(sum - c, i);
+                           return place + i;
+                         }
+                         rem -= __builtin_amdgcn_readlane(sum, 63);
+                       }
+                       return place;
+                     });
   }
   if (tell && a.join != nullptr) {
     PagedJoin j = {0, 0, 0, 0, 0, {0, 0, 0}};

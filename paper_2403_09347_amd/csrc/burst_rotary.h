@@ -23,6 +23,7 @@ struct RotateArgs {
   int dims, interleaved, inverse;
   float amplitude;
   int rows_each;
+  int first;                                       // block that the launch begins with
   // packed tokens of sequences (starts != nullptr): rows behind the last sequence and at negative positions are left out
   const int* starts; const int* lengths; const int* table; const long long* offsets;
   long long table_stride;

@@ -34,10 +34,11 @@ rotate_kernel(RotateArgs a) {
   __shared__ float2 turn[kRotateRows * 64];
   __shared__ long long at[kRotateRows], to[kRotateRows];   // position; where the row goes (elements of y), -1: nowhere
   const int tid = threadIdx.x, lane = tid & 63;
+  const int bid = a.first + (int)blockIdx.x;
   int i = 0;
-  while (i + 1 < a.n && (int)blockIdx.x >= a.it[i + 1].first_block) i++;
+  while (i + 1 < a.n && bid >= a.it[i + 1].first_block) i++;
   const RotateItem& it = a.it[i];
-  int blk = blockIdx.x - it.first_block;
+  int blk = bid - it.first_block;
   const int ht = blk % it.head_tiles;
   blk /= it.head_tiles;
   const int rt = blk % it.row_tiles, b = blk / it.row_tiles;
@@ -145,7 +146,7 @@ static void enqueue(const RotateArgs& a, bool vec, long long blocks, hipStream_t
   else BURST_LAUNCH((rotate_kernel<T, false, false>), grid, block, 0, s, a);
 }
 
-// The items of `a` (all but their tiles, which are laid out here) in one launch.
+// The items of `a` (all but their tiles, which are laid out here) in one launch (more only of more than 8 million blocks).
 int launch_rotate(RotateArgs& a, int dtype, hipStream_t s) {
   const int E = dtype == BURST_BF16 ? 8 : 4;
   // 16-byte accesses: every granule of a row starts on 16 bytes, and no pair is cut by one
@@ -179,10 +180,16 @@ int launch_rotate(RotateArgs& a, int dtype, hipStream_t s) {
     blocks += (long long)it.B * it.row_tiles * it.head_tiles;
     if (blocks > 0x7fffffffLL) return BURST_ERR_SHAPE;
   }
-  if (blocks == 0) return BURST_OK;
-  if (dtype == BURST_BF16) enqueue<bf16>(a, vec, blocks, s);
-  else enqueue<float>(a, vec, blocks, s);
-  return launch_status();
+  constexpr long long kMost = 1 << 23;             // blocks of a launch: it can have 2^32 threads
+  for (long long first = 0; first < blocks; first += kMost) {
+    a.first = (int)first;
+    const long long n = blocks - first < kMost ? blocks - first : kMost;
+    if (dtype == BURST_BF16) enqueue<bf16>(a, vec, n, s);
+    else enqueue<float>(a, vec, n, s);
+    const int e = launch_status();
+    if (e != BURST_OK) return e;
+  }
+  return BURST_OK;
 }
 
 }  // namespace burst

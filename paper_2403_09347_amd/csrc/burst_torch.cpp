@@ -270,6 +270,9 @@ std::tuple<int, Tensor, std::vector<Tensor>, std::vector<Tensor>> walk_backward(
   return {st, dQ, dK, dV};
 }
 
+void fits_int(const Tensor& t) {
+  for (const int64_t n : t.sizes()) TORCH_CHECK_VALUE(n <= 0x7fffffff, "sizes below 2^31 expected");
+}
 // ---- rotary.burst_rotary: several tensors rotated by one call, and their gradients brought back by another.
 bool rows_in_place(const Tensor& t) {              // strides that burst_rotate takes: all zero would mean dense ones
   if (t.size(3) != 1 && t.stride(3) != 1) return false;
@@ -373,6 +376,7 @@ std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, c
     TORCH_CHECK_VALUE(x.dim() == 4 && x.is_cuda() && x.device() == xs[0].device() && x.scalar_type() == xs[0].scalar_type() && x.size(3) == xs[0].size(3) &&
                       (x.scalar_type() == torch::kBFloat16 || x.scalar_type() == torch::kFloat),
                       "[B, heads, rows, d] tensors of bfloat16 or float32, of one type, d and device, expected");
+  for (const Tensor& x : xs) fits_int(x);
   check_turns(turns, xs[0].size(3), xs[0]);
   Turning how{{}, offsets, interleaved, amplitude, false};
   variable_list at;
@@ -391,6 +395,7 @@ std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, c
 void check_tokens(const Tensor& t, const Tensor& k_pages, const char* what) {
   TORCH_CHECK_VALUE(t.dim() == 3 && t.device() == k_pages.device() && t.scalar_type() == k_pages.scalar_type() && t.size(2) == k_pages.size(3), what,
                     ": [rows, heads, d] of the type, device and d of the pages expected");
+  fits_int(t);
   TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && t.requires_grad()), what, ": the paged calls have no gradient (call them under torch.no_grad)");
 }
 // A token tensor as it is where its strides can be handed on (unit: elements that they have to be multiples of), else a copy.
@@ -408,9 +413,13 @@ void set_token_strides(int64_t (&out)[2], const Tensor& t) {
 burst_paged_params describe_paged(const Tensor& k_pages, const Tensor& v_pages, const Tensor& table, const Tensor& lengths, const Tensor& starts) {
   TORCH_CHECK_VALUE(k_pages.dim() == 4 && k_pages.is_cuda() && (k_pages.scalar_type() == torch::kBFloat16 || k_pages.scalar_type() == torch::kFloat),
                     "k_pages: device tensor [pages, kv_heads, page, d] of bfloat16 or float32 expected");
+  fits_int(k_pages);
+  fits_int(table);
   TORCH_CHECK_VALUE(v_pages.scalar_type() == k_pages.scalar_type() && v_pages.device() == k_pages.device() && v_pages.sizes() == k_pages.sizes() &&
                     v_pages.strides() == k_pages.strides(), "v_pages: like k_pages in type, sizes and strides expected");
   TORCH_CHECK_VALUE(k_pages.size(3) == 1 || k_pages.stride(3) == 1, "pages: a contiguous last dimension expected");
+  for (int i = 0; i < 3; i++)                      // (an expanded dimension has no place for more than one row, and strides of zero mean dense ones)
+    TORCH_CHECK_VALUE(k_pages.size(i) <= 1 || k_pages.stride(i) >= k_pages.size(3), "pages: rows that lie in memory one after the other expected");
   for (const Tensor* t : {&table, &lengths, &starts})
     TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == k_pages.device(), "table, lengths, starts: int32 tensors on the pages' device expected");
   TORCH_CHECK_VALUE(lengths.dim() == 1 && starts.dim() == 1 && starts.size(0) == lengths.size(0) + 1 && table.dim() == 2 && table.size(0) == lengths.size(0),

@@ -2,6 +2,7 @@
 // ones, and arrays that hold anything.  Checks that every unit of every item belongs to exactly one run, that no key
 // outside the table or the pages is named, and that the parts of a cut item are joined once, from the slots that they were written
 // to.  Built with the address and undefined-behaviour sanitizers by tests/test_paged_work.py.
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <map>
@@ -14,7 +15,7 @@ using namespace burst;
 static int bad = 0;
 #define CHECK(x) do { if (!(x)) { if (bad++ < 10) std::printf("line %d: %s (case %d)\n", __LINE__, #x, g_case); } } while (0)
 static int g_case = 0;
-static long long by_items = 0, by_units = 0;
+static long long by_items = 0, by_units = 0, ordered = 0, disordered = 0;
 
 static std::vector<int> g_starts, g_lengths;
 struct HostRead {
@@ -32,12 +33,22 @@ static int rnd(int n) {
 }
 static int wild() { const int w[] = {-1, 0, 1, 0x7fffffff, -0x7fffffff - 1, 1 << 30, -5, 64}; return rnd(2) ? w[rnd(8)] : rnd(3000) - 100; }
 
-// as locate_run does it on the device
+// As the kernels' start_run does it, whose lanes share the blocks of a sequence, or go past them 64 at a time.
 static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur, PagedDeal& deal, long long& bound) {
   PagedTotals all = {0, 0, 0, 0};
   std::vector<PagedTotals> each;
   for (int s = 0; s < w.sequences; s++) {
-    each.push_back(w.totals(Cursor::load(w, s)));
+    const PagedSeq q = Cursor::load(w, s);
+    PagedTotals t = w.totals(q, w.blocks(q), 0, 1), shared = {0, 0, 0, 0};
+    for (int lane = 0; lane < 64; lane++) {
+      const PagedTotals x = w.totals(q, w.blocks(q), lane, 64);
+      shared.items = x.items; shared.units += x.units;
+      if (x.most > shared.most) shared.most = x.most;
+    }
+    CHECK(t.units == shared.units && t.items == shared.items && t.most == shared.most);
+    t.pair = w.pair(q, w.blocks(q), t.most);
+    each.push_back(t);
+    if (!PagedWork::in_order(g_starts[s], g_starts[s + 1])) return false;
     all.units += each[s].units * w.parts;
     all.items += each[s].items * w.parts;
     if (each[s].most > all.most) all.most = each[s].most;
@@ -53,7 +64,21 @@ static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur
   auto one = [&](int s) { return deal.by_items ? each[s].items : each[s].units; };
   int before = 0, s = 0;
   while (begin >= before + one(s) * w.parts) before += one(s++) * w.parts;
-  return cur.place(w, s, Cursor::load(w, s), one(s), (int)begin - before, deal, deal.each < total - begin ? deal.each : total - (int)begin);
+  return cur.place(w, s, Cursor::load(w, s), one(s), (int)begin - before, deal, deal.each < total - begin ? deal.each : total - (int)begin,
+                   [&](int& rem, int n) {
+                     int place = 0;
+                     const PagedSeq q = Cursor::load(w, s);
+                     for (; n - place > 8; place += 64) {
+                       int sum = 0;
+                       for (int i = 0; i < 64 && place + i < n; i++) {
+                         const int c = w.cost(q, w.block_at(place + i, n));
+                         if (rem < sum + c) { rem -= sum; return place + i; }
+                         sum += c;
+                       }
+                       rem -= sum;
+                     }
+                     return place;
+                   });
 }
 
 static void batch(bool anything) {
@@ -63,10 +88,16 @@ static void batch(bool anything) {
   g_lengths.assign(S, 0);
   for (int s = 0; s < S; s++) {
     g_lengths[s] = anything ? wild() : rnd(4) ? rnd(cap + 1) : rnd(2);
-    g_starts[s + 1] = g_starts[s] + (rnd(4) ? rnd(4) : rnd(200));
+    g_starts[s + 1] = g_starts[s] + (rnd(4) ? rnd(4) : rnd(rnd(20) ? 200 : 3000));
   }
   const int rows = g_starts[S] + rnd(3);
-  if (anything) for (int& x : g_starts) x = rnd(2) ? x : wild();
+  bool order = true;
+  if (anything) {
+    for (int& x : g_starts) x = rnd(2) ? x : wild();
+    if (rnd(4)) std::sort(g_starts.begin(), g_starts.end());
+    for (int s = 0; s < S; s++) order = order && g_starts[s] <= g_starts[s + 1];
+    (order ? ordered : disordered)++;
+  }
   std::vector<int> table((size_t)S * width);
   for (int& x : table) x = anything || rnd(20) == 0 ? wild() : rnd(pages);
   PagedWork w = {};
@@ -91,6 +122,7 @@ static void batch(bool anything) {
     PagedDeal deal;
     long long bound = 0;
     if (!locate(w, runs, slack, run, cur, deal, bound)) continue;
+    CHECK(order);
     bool first = true;
     long long length = 0;                          // no run of whole items is longer than the deal's bound on it
     do {
@@ -141,6 +173,7 @@ static void batch(bool anything) {
     CHECK(cur.left <= w.item_cost);
     if (deal.by_items) CHECK(length <= bound);
   }
+  if (!order) return;                              // (nothing is done)
   for (int s = 0; s < S; s++) {
     const PagedSeq q = Cursor::load(w, s);
     if (q.n <= 0) continue;
@@ -168,7 +201,7 @@ static void batch(bool anything) {
 
 int main() {
   for (g_case = 0; g_case < 6000; g_case++) batch(g_case % 3 == 2);
-  if (by_items < 1000 || by_units < 1000) bad++;   // both ways of dealing have been seen
+  if (by_items < 1000 || by_units < 1000 || ordered < 500 || disordered < 100) bad++;   // all of them have been seen
   std::printf("work checks failed: %d\n", bad);
   return bad != 0;
 }

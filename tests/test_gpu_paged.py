@@ -521,3 +521,37 @@ def test_tensors_that_do_not_fit_are_refused():
     refuses(burst_cache_append, k_pages=b.k_pages.clone().requires_grad_(True))
     with torch.no_grad():
         burst_cache_append(**dict(a, k=b.k.clone().requires_grad_(True)))
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 70), (False, 0)])
+def test_sequences_of_many_blocks(causal, window):
+    """More than 64 blocks of 16 tokens in one sequence, few in the next."""
+    b = Batch([1500, 40, 900], [1400, 40, 800], 8, 1, 32, seed=31)
+    O, lse = attend(b, causal=causal, window=window)
+    b.check(O, lse, causal, window)
+    b = Batch([1200, 40], [1100, 2], 8, 1, 32, dtype=F32, seed=32)
+    O, lse = attend(b, causal=causal, window=window)
+    b.check(O, lse, causal, window)
+
+
+@pytest.mark.parametrize("new", [1, 4096])
+def test_starts_that_decrease(new):
+    """The same rows in 32 sequences of 2^29 keys each would be more work than 32 bits count: nothing is done."""
+    q = torch.ones(4096, 2, 64, dtype=BF16, device=DEV)
+    none = torch.empty(0, 2, 1 << 26, 64, dtype=BF16, device=DEV)
+    table = torch.full((64, 8), -1, dtype=torch.int32, device=DEV)
+    lengths = torch.full((64,), 1 << 30, dtype=torch.int32, device=DEV)
+    starts = torch.tensor([0, 4096] * 32 + [0], dtype=torch.int32, device=DEV)
+    O, lse = torch.full_like(q, 5), torch.full((4096, 2), 5.0, device=DEV)
+    burst_paged_attention(q, none, none, table, lengths, starts, out=O, lse=lse, max_new=new)
+    assert (O == 5).all() and (lse == 5).all()
+
+
+def test_expanded_pages_are_refused():
+    b = Batch([20, 30], [2, 1], 4, 2, 64)
+    for shape in ((1, 1, 1, 64), (1, 2, 16, 64), (6, 1, 16, 64), (6, 2, 1, 64)):
+        p = torch.zeros(shape, dtype=BF16, device=DEV).expand(6, 2, 16, 64)
+        with pytest.raises(ValueError, match="rows that lie in memory"):
+            burst_paged_attention(b.q, p, p, b.table, b.lengths, b.starts)
+        with pytest.raises(ValueError, match="rows that lie in memory"):
+            burst_cache_append(b.k, b.v, p, p, b.table, b.lengths, b.starts)

@@ -248,3 +248,11 @@ def test_a_rotated_ring_is_the_rotated_sequence():
     whole, _ = burst_attention(q, [k], [v], causal=True, turns=turns)
     last, _ = burst_attention(q[:, :, 192:], list(k.split(64, 2)), list(v.split(64, 2)), causal=True, q_off=192, turns=turns)
     assert (whole[:, :, 192:].float() - last.float()).abs().max().item() <= 2e-2
+
+
+def test_more_rows_than_a_launch_has_blocks_for():
+    rows, t = (1 << 27) + 100, default_turns(2)
+    x = (torch.arange(2 * rows, device=DEV) % 251).to(BF16).view(1, 1, rows, 2)
+    y = burst_rotary(x, t)
+    for at in (0, (1 << 27) - 50, rows - 50):
+        check_rotation(at, y[:, :, at:at + 50], x[:, :, at:at + 50], at + np.arange(50)[None, None], f64(t))
