@@ -555,3 +555,12 @@ def test_expanded_pages_are_refused():
             burst_paged_attention(b.q, p, p, b.table, b.lengths, b.starts)
         with pytest.raises(ValueError, match="rows that lie in memory"):
             burst_cache_append(b.k, b.v, p, p, b.table, b.lengths, b.starts)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_sequences_that_share_pages(new):
+    """A common beginning lies in the same pages."""
+    b = Batch([400, 300, 270], [new] * 3, 4, 2, 64, seed=33)
+    b.table[1:, :10] = b.table[0, :10]
+    O, lse = attend(b)
+    b.check(O, lse)
