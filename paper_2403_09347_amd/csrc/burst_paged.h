@@ -167,6 +167,13 @@ BURST_HD void segment_tiles(const PagedWork& w, const PagedSegment& g, int shift
   end = e < g.to << u ? e : g.to << u;
   if (end <= first) end = first + 1;
 }
+// The run of a workgroup, -1: none.  Workgroup ids go to the eight XCDs in turn: the runs that have work (`active` of them) are spread over all
+// XCDs, and neighbouring ones, which share keys, lie on one.
+BURST_HD int run_of(int bid, int runs, int active) {
+  if (runs % 8 != 0) return bid < active ? bid : -1;
+  const int each = (active + 7) >> 3, run = (bid & 7) * each + (bid >> 3);
+  return bid >> 3 < each && run < active ? run : -1;
+}
 // Where a run leaves the partial results of an item that is not all its own: the first part of an item is its run's last segment, every
 // other part its run's first one.
 BURST_HD int partial_slot(const PagedSegment& g, int run) { return 2 * run + (g.from == g.lo ? 1 : 0); }

@@ -193,9 +193,9 @@ paged_short_kernel(PagedArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[NST * 2 * TILE];
   __shared__ i32x4 segs[NSEG][3];
   const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
-  const int run = run_of(blockIdx.x, a.runs);
+  int run;
   DeviceCursor fet;
-  if (!start_run(a, run, lane, lane == 0, fet)) return;
+  if (!start_run(a, blockIdx.x, lane, lane == 0, fet, run)) return;
   const unsigned lds0 = lds_addr(smem);
   const int d = a.d;
   const unsigned pitch = (unsigned)(a.p_row * sizeof(T)), row_bytes = (unsigned)(d * sizeof(T));
@@ -444,10 +444,10 @@ struct TileFeed {
   bool more;                         // fet.g is the segment of the tile that was asked for last
   __device__ __forceinline__ int group() const { return w * ROWS / 16; }
   __device__ __forceinline__ int first_row() const { return w * ROWS % 16; }
-  __device__ __forceinline__ bool start(const PagedArgs& a, int run, const char* smem) {
+  __device__ __forceinline__ bool start(const PagedArgs& a, int& run, const char* smem) {
     lane = threadIdx.x & 63;
     w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (!start_run(a, run, lane, threadIdx.x == 0, fet)) return false;
+    if (!start_run(a, blockIdx.x, lane, threadIdx.x == 0, fet, run)) return false;
     lds0 = lds_addr(smem) + (unsigned)(w * NL) * 1024u;
     pitch = (unsigned)(a.p_row * (int)sizeof(T)); row_bytes = (unsigned)(a.d * (int)sizeof(T));
     v_off = (const char*)a.V - (const char*)a.K;
@@ -521,7 +521,7 @@ paged_chunk_kernel(PagedArgs a) {
   typedef TileFeed<bf16, D, kTileShift> Feed;
   constexpr int ROWB = Feed::ROWB, TILE = Feed::TILE, KS = C / 16, DB = C / 32, AHEAD = 4;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
-  const int run = run_of(blockIdx.x, a.runs);
+  int run;
   Feed f;
   if (!f.start(a, run, smem)) return;
   const int lane = f.lane, lr = lane & 31, h = lane >> 5, w = f.w, d = a.d;
@@ -709,7 +709,7 @@ paged_chunk_f32_kernel(PagedArgs a) {
   constexpr int ROWB = Feed::ROWB, TILE = Feed::TILE, GR = Feed::GR, KEYS = 1 << kTileShiftF32;
   constexpr int KS = C / 16, HV = GR / 16, OB = D / 16;   // granule steps of a product over d; 64-column parts; 16-column blocks of O^T
   __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
-  const int run = run_of(blockIdx.x, a.runs);
+  int run;
   Feed f;
   if (!f.start(a, run, smem)) return;
   const int lane = f.lane, r = lane & 15, g = lane >> 4, w = f.w, d = a.d;
@@ -881,7 +881,7 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (lane & 15) * 4;
   const int run = blockIdx.x + 1, d = a.d;
   PagedJoin join = a.join[run];
-  if (join.n <= 0) return;
+  if (run >= a.join[0].n || join.n <= 0) return;
   join.n = min(join.n, a.runs - run + 1);          // (as they are; no access outside the workspace and the outputs if another call has written there)
   const bool few = rows_of_item <= kShortRows;
   const bool alone = join.n <= (few ? 8 : 32), together = join.n > (few ? 32 : 128);   // a lane group on a row; all wavefronts on a row

@@ -21,7 +21,8 @@ struct PagedArgs {
   int runs, slack, o_f32;            // slack: see paged_deal
   float scale;
 };
-// What a run tells the merging launch: the item that is joined from the parts of n runs, from the run before it on (n = 0: none)
+// What a run tells the merging launch: the item that is joined from the parts of n runs, from the run before it on (n = 0: none); run 0, which
+// cuts none: the number of runs that have work, in n.
 struct PagedJoin { int n, first, count, part, block, pad[3]; };   // first, count: the sequence's rows
 static_assert(sizeof(PagedJoin) == 32, "one load");
 constexpr int kShortRows = 16, kChunkRows = 128;   // rows of an item
@@ -40,10 +41,6 @@ __device__ __forceinline__ int scalar_at(const int* p, I i) {
 struct ScalarRead { static __device__ __forceinline__ int at(const int* p, int i) { return scalar_at(p, __builtin_amdgcn_readfirstlane(i)); } };
 typedef PagedCursor<ScalarRead> DeviceCursor;
 
-// Workgroup -> run: an XCD (ids go to the eight in turn) gets neighbouring runs, which share keys.
-__device__ __forceinline__ int run_of(int bid, int runs) {
-  return runs % 8 == 0 ? (bid & 7) * (runs / 8) + (bid >> 3) : bid;
-}
 __device__ __forceinline__ int wave_scan(int x) {  // inclusive
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr:1, 2, 4, 8
   x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
@@ -62,12 +59,12 @@ __device__ __forceinline__ int wave_most(int x) {  // of numbers that are not ne
   x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
   return __builtin_amdgcn_readlane(x, 63);
 }
-// The start of run `run`, by a wavefront: every lane adds up a sequence.  False: the run has nothing to do.  The merging launch is told
+// A workgroup's run and its start, by a wavefront: every lane adds up a sequence.  False: there is none for it.  The merging launch is told
 // what the run's start has cut (`tell`).
 // Of sequences with many blocks the lanes share the blocks where there are few such sequences: going through them takes as long as
 // the longest has blocks, sharing about four blocks' time for every 64.  (us a call, lanes by themselves / so: 131072 tokens with a window of
 // 1024, 8 heads over one, 1361 / 817; 16384 tokens causal 657 / 591; 4096, 32 heads over 8, 158 / 152; single tokens 0.1 more.)
-__device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane, bool tell, DeviceCursor& cur) {
+__device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane, bool tell, DeviceCursor& cur, int& run) {
   const PagedWork& w = a.w;
   PagedSeq q;
   PagedTotals mine = {0, 0, 0, 0}, all = {0, 0, 0, 0};
@@ -108,9 +105,11 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
     all.pair = max(all.pair, wave_most(mine.pair));
   }
   const PagedDeal deal = paged_deal(all, a.runs, a.slack);
-  const int total = deal.by_items ? all.items : all.units;
+  const int total = disorder != 0 ? 0 : deal.by_items ? all.items : all.units;
+  const int active = (int)(((unsigned)total + deal.each - 1) / (unsigned)deal.each);
+  run = run_of(bid, a.runs, active);
+  bool some = run >= 0;
   const long long from = (long long)deal.each * run;
-  bool some = disorder == 0 && from < total;
   if (some) {
     const int begin = (int)from;
     int before = 0, scan = 0, own = 0, base = 0;
@@ -142,10 +141,11 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int run, int lane,
                        return place;
                      });
   }
-  if (tell && a.join != nullptr) {
+  if (tell && a.join != nullptr && (run >= 0 || bid == 0)) {
     PagedJoin j = {0, 0, 0, 0, 0, {0, 0, 0}};
     if (some && !deal.by_items) j = PagedJoin{parts_to_join(cur.g, deal.each), cur.g.q.first, cur.g.q.n, cur.g.part, cur.g.block, {0, 0, 0}};
-    a.join[run] = j;
+    if (bid == 0) j.n = active;
+    a.join[bid == 0 ? 0 : run] = j;
   }
   return some;
 }

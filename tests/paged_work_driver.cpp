@@ -199,8 +199,25 @@ static void batch(bool anything) {
   CHECK(items == want);
 }
 
+// every run with work has one workgroup, run 0 the first one, and no XCD has more than its share
+static void placement() {
+  const int runs = rnd(3) ? 8 * (1 + rnd(128)) : 1 + rnd(8), active = rnd(runs + 1);
+  std::vector<int> seen(runs), xcd(8);
+  for (int bid = 0; bid < runs; bid++) {
+    const int run = run_of(bid, runs, active);
+    CHECK(run >= -1 && run < active);
+    if (run < 0) continue;
+    seen[run]++;
+    xcd[bid % 8]++;
+    CHECK((run == 0) == (bid == 0));
+  }
+  for (int run = 0; run < active; run++) CHECK(seen[run] == 1);
+  if (runs % 8 == 0)
+    for (int n : xcd) CHECK(n <= (active + 7) / 8);
+}
+
 int main() {
-  for (g_case = 0; g_case < 6000; g_case++) batch(g_case % 3 == 2);
+  for (g_case = 0; g_case < 6000; g_case++) { batch(g_case % 3 == 2); placement(); }
   if (by_items < 1000 || by_units < 1000 || ordered < 500 || disordered < 100) bad++;   // all of them have been seen
   std::printf("work checks failed: %d\n", bad);
   return bad != 0;
