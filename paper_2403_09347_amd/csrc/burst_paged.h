@@ -168,7 +168,8 @@ BURST_HD void segment_tiles(const PagedWork& w, const PagedSegment& g, int shift
   if (end <= first) end = first + 1;
 }
 // The run of a workgroup, -1: none.  Workgroup ids go to the eight XCDs in turn: the runs that have work (`active` of them) are spread over all
-// XCDs, and neighbouring ones, which share keys, lie on one.
+// XCDs, and neighbouring ones, which share keys, lie on one.  (us a call, laid out as if all had work / so: one token over 32768 keys 38.1 /
+// 37.0, 8 over 200 to 1500 17.8 / 16.5, a window of 1024 at d = 64, 300 runs of 512, 37.9 / 36.3; 8 x 8 tokens fp32 46.0 / 48.4.)
 BURST_HD int run_of(int bid, int runs, int active) {
   if (runs % 8 != 0) return bid < active ? bid : -1;
   const int each = (active + 7) >> 3, run = (bid & 7) * each + (bid >> 3);

@@ -174,8 +174,8 @@ __device__ __forceinline__ void wait_lds() {
 // zeros) in a ring of stages that runs on across the items of the run; a wavefront waits for its own loads alone, there are no barriers.
 // LDS rows of 8, 16 or 32 granules, permuted so that 16 rows of one granule column fall into different banks.
 // Measured (32 query heads over 8, d = 128, us and the cache's bytes a second): 64 single tokens over 16 to 16384 keys each, 645 MB, 126 (5.1
-// TB/s); one over 32768 keys, 134 MB, 38 (3.5 TB/s; 7 of them joining); 32 over 2000 keys, 32 heads of
-// their own, 1.05 GB, 187 (5.6 TB/s).  A device copy reads and writes 5.0 TB/s.
+// TB/s); one over 32768 keys, 134 MB, 37 (3.6 TB/s; 7 of them joining); 32 over 2000 keys, 32 heads of
+// their own, 1.05 GB, 184 (5.7 TB/s).  A device copy reads and writes 5.0 TB/s.
 template <int GR>
 __device__ __forceinline__ int short_code(int row) { return GR == 8 ? (row >> 1) & 7 : row_code(row & 15); }
 
@@ -510,8 +510,8 @@ struct TileFeed {
 // bf16: tiles of 64 keys, operand orientation and LDS layout as in burst_plain_mfma.h: S^T = K Q^T with a row per lane, whose P is the operand
 // of O^T += V^T P^T as it stands.
 // Scores and references are in log2 units (one fma an exponent), as in the d = 64 and d = 128 kernels of the walks.
-// Measured: 2048 tokens over 32768 keys, 32 heads over 8, d = 128, 1025 to 1070 us (1.00 to 1.04 PFLOP/s; a large library product 1.14);
-// 4096 tokens of 8192, d = 64, twice, 526 us (0.78).  At d = 64 a tile's products are 512 cycles of a wavefront and its vector instructions about
+// Measured: 2048 tokens over 32768 keys, 32 heads over 8, d = 128, 1025 to 1115 us (0.95 to 1.04 PFLOP/s, cards differ; a large library product 1.14);
+// 4096 tokens of 8192, d = 64, twice, 526 to 550 us (0.75 to 0.78).  At d = 64 a tile's products are 512 cycles of a wavefront and its vector instructions about
 // 900, which two wavefronts a SIMD overlap in part.  (Four buffers instead of two at d = 64: 535 / 526 at that size, the others within 1 %.)
 constexpr int kTile = 1 << kTileShift;             // keys
 // C: columns that are computed, of the D that a row of LDS has.
