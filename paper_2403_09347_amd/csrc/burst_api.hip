@@ -753,6 +753,10 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   if (a.runs < 1) a.runs = 1;
   if (a.runs > 8) a.runs &= ~7;
   a.slack = plan.chunk ? 8 : 2;
+  // Chunk runs of four units at most: half as many of twice the length, a workgroup a CU, fewer parts to join.  us a call, as many runs as the chip
+  // holds / so: 256 tokens over 4096 keys, 8 heads, 36.8 / 28.2, 2 x 40 over 2000, fp32, d = 64, 31.6 / 25.5, 3 of 30 to 300 over 400 to 1500, fp32,
+  // 47.1 / 43.1; 16 x 5 over 300 to 900, 32 heads over 8, 21.4 / 22.5.  Up to eight units: 8 x 8 over 4096, fp32, 48 / 56.
+  a.few = plan.chunk ? 4 : 0;
   plan.bytes = a.runs < 2 ? 0 : (size_t)a.runs * (2 * rows * (p->d + 2) * sizeof(float) + sizeof(burst::PagedJoin));
   return BURST_OK;
 }

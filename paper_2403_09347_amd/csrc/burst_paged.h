@@ -85,8 +85,10 @@ struct PagedWork {
 // `each` units a run (the items' beginnings among them: a run that ends within one leaves the item to the next), or, where that costs
 // less, `each` whole items, of which nothing has to be joined.  `slack`: the units that a run may have more for that.
 struct PagedDeal { int each, by_items; };
-BURST_HD PagedDeal paged_deal(const PagedTotals& t, int runs, int slack) {
+// few: where a run would have no more units than this, half as many runs have twice as many.
+BURST_HD PagedDeal paged_deal(const PagedTotals& t, int runs, int slack, int few) {
   PagedDeal d;
+  if (t.units <= (long long)few * runs) runs = (runs + 1) >> 1;
   const int each = (int)(((unsigned)t.units + runs - 1) / (unsigned)runs), per = (int)(((unsigned)t.items + runs - 1) / (unsigned)runs);
   d.by_items = (long long)(per >> 1) * t.pair + (per & 1) * t.most <= each + each / 16 + slack;
   d.each = d.by_items ? per : each;

@@ -18,7 +18,7 @@ struct PagedArgs {
   PagedWork w;
   int heads, group, d, pages, page_shift;
   int parts_each, part_heads;        // parts of a key/value head, query heads of a part
-  int runs, slack, o_f32;            // slack: see paged_deal
+  int runs, slack, few, o_f32;       // slack, few: see paged_deal
   float scale;
 };
 // What a run tells the merging launch: the item that is joined from the parts of n runs, from the run before it on (n = 0: none); run 0, which
@@ -104,7 +104,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane,
     all.most = max(all.most, wave_most(mine.most));
     all.pair = max(all.pair, wave_most(mine.pair));
   }
-  const PagedDeal deal = paged_deal(all, a.runs, a.slack);
+  const PagedDeal deal = paged_deal(all, a.runs, a.slack, a.few);
   const int total = disorder != 0 ? 0 : deal.by_items ? all.items : all.units;
   const int active = (int)(((unsigned)total + deal.each - 1) / (unsigned)deal.each);
   run = run_of(bid, a.runs, active);

@@ -34,7 +34,7 @@ static int rnd(int n) {
 static int wild() { const int w[] = {-1, 0, 1, 0x7fffffff, -0x7fffffff - 1, 1 << 30, -5, 64}; return rnd(2) ? w[rnd(8)] : rnd(3000) - 100; }
 
 // As the kernels' start_run does it, whose lanes share the blocks of a sequence, or go past them 64 at a time.
-static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur, PagedDeal& deal, long long& bound) {
+static bool locate(const PagedWork& w, int runs, int slack, int few, int run, Cursor& cur, PagedDeal& deal, long long& bound) {
   PagedTotals all = {0, 0, 0, 0};
   std::vector<PagedTotals> each;
   for (int s = 0; s < w.sequences; s++) {
@@ -54,7 +54,8 @@ static bool locate(const PagedWork& w, int runs, int slack, int run, Cursor& cur
     if (each[s].most > all.most) all.most = each[s].most;
     if (each[s].pair > all.pair) all.pair = each[s].pair;
   }
-  deal = paged_deal(all, runs, slack);
+  deal = paged_deal(all, runs, slack, few);
+  if (all.units <= (long long)few * runs) runs = (runs + 1) / 2;
   const long long per = deal.each, even = (all.units + runs - 1) / runs;
   bound = (per >> 1) * all.pair + (per & 1) * all.most;
   if (deal.by_items) CHECK(bound <= even + even / 16 + slack);
@@ -110,7 +111,7 @@ static void batch(bool anything) {
   w.window = rnd(3) ? 0 : rnd(2) ? 1 + rnd(100) : 1 << 30;
   w.item_cost = rnd(4);
   w.unit_shift = rnd(4) ? 5 + rnd(2) : 7 + rnd(3);
-  const int runs = 1 + rnd(40), slack = rnd(3) ? rnd(10) : rnd(2) * 100000;
+  const int runs = 1 + rnd(40), slack = rnd(3) ? rnd(10) : rnd(2) * 100000, few = rnd(2) * rnd(9);
 
   typedef std::tuple<int, int, int> Item;          // sequence, part, block
   std::map<Item, std::vector<int>> covered;
@@ -121,7 +122,7 @@ static void batch(bool anything) {
     Cursor cur;
     PagedDeal deal;
     long long bound = 0;
-    if (!locate(w, runs, slack, run, cur, deal, bound)) continue;
+    if (!locate(w, runs, slack, few, run, cur, deal, bound)) continue;
     CHECK(order);
     bool first = true;
     long long length = 0;                          // no run of whole items is longer than the deal's bound on it
