@@ -472,17 +472,23 @@ def rotary(turns, interleaved=False, amplitude=1.0, inverse=False):
 def burst_rotate(xs, ys, r, offsets=None, positions=None):
     """xs, ys: lists of [B, heads, rows, d] tensors with a contiguous last dimension, of one type and d; offsets: the position of row 0
     of each; positions: None, or for each None or an int64 device tensor [B, rows] with contiguous rows, to which its offset is added."""
-    items = (BurstRows * len(xs))()
-    for i, (x, y, c) in enumerate(zip(xs, ys, items)):
-        if x.shape != y.shape or x.dtype != y.dtype or not x.is_cuda or not y.is_cuda:
+    if len(ys) != len(xs) or any(more is not None and len(more) != len(xs) for more in (offsets, positions)):
+        raise ValueError("as many ys, offsets and positions as xs expected")
+    offsets, positions = offsets or [0] * len(xs), positions or [None] * len(xs)
+    for x, y, at in zip(xs, ys, positions):
+        if x.dtype not in (torch.bfloat16, torch.float32) or x.dtype != xs[0].dtype or x.dim() != 4 or x.shape[3] != xs[0].shape[3]:
+            raise ValueError("[B, heads, rows, d] tensors of bfloat16 or float32, of one type and d, expected")
+        if at is not None and (at.dtype != torch.int64 or tuple(at.shape) != (x.shape[0], x.shape[2]) or (at.shape[1] > 1 and at.stride(1) != 1)):
+            raise ValueError("positions: int64 device tensor [B, rows] with contiguous rows expected")
+        if x.shape != y.shape or x.dtype != y.dtype:
             raise ValueError("x, y: device tensors of the same sizes and type expected")
+    items = (BurstRows * len(xs))()
+    for x, y, at, offset, c in zip(xs, ys, positions, offsets, items):
+        if not all(t.is_cuda for t in (x, y, at) if t is not None):
+            raise ValueError("x, y, positions: device tensors expected")
         c.x_strides[:], c.y_strides[:] = strides_of(x) or (0, 0, 0), strides_of(y) or (0, 0, 0)
-        c.x, c.y, c.B, c.heads, c.rows = x.data_ptr(), y.data_ptr(), x.shape[0], x.shape[1], x.shape[2]
-        c.offset = 0 if offsets is None else offsets[i]
-        if positions is not None and positions[i] is not None:
-            at = positions[i]
-            if at.dtype != torch.int64 or not at.is_cuda or tuple(at.shape) != (x.shape[0], x.shape[2]) or at.stride(1) not in (0, 1):
-                raise ValueError("positions: int64 device tensor [B, rows] expected")
+        c.x, c.y, c.B, c.heads, c.rows, c.offset = x.data_ptr(), y.data_ptr(), x.shape[0], x.shape[1], x.shape[2], offset
+        if at is not None:
             c.positions, c.positions_stride = at.data_ptr(), at.stride(0)
     dtype = BURST_BF16 if not len(xs) or xs[0].dtype == torch.bfloat16 else BURST_F32
     _check(load().burst_rotate(items, len(xs), ctypes.byref(r), xs[0].shape[3] if len(xs) else 2, dtype, _stream()), "burst_rotate")
@@ -492,19 +498,63 @@ def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts,
     """k_pages: [pages, kv_heads, page, d] (its strides go into the block; V_pages lies likewise); table [sequences, width], lengths
     [sequences], starts [sequences + 1]: int32 device tensors.  Token tensors are dense unless their strides are set in the block."""
     code = {torch.bfloat16: BURST_BF16, torch.float32: BURST_F32, "bf16": BURST_BF16, "f32": BURST_F32}.get(dtype, dtype)
+    if any(t.dtype != torch.int32 for t in (table, lengths, starts)) or table.dim() != 2 or lengths.shape != table.shape[:1] or \
+            starts.shape != (table.shape[0] + 1,):
+        raise ValueError("table [sequences, width], lengths [sequences], starts [sequences + 1]: int32 tensors expected")
+    if not lengths.is_contiguous() or not starts.is_contiguous() or (table.shape[1] > 1 and table.stride(1) != 1) or \
+            (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
+        raise ValueError("lengths, starts and the table's rows: contiguous expected")
+    if k_pages.dim() != 4 or tuple(k_pages.shape[1::2]) != (kv_heads, d) or (d > 1 and k_pages.stride(3) != 1):
+        raise ValueError("k_pages: [pages, kv_heads, page, d] with a contiguous last dimension expected")
+    if any(k_pages.shape[i] > 1 and k_pages.stride(i) < d for i in range(3)):   # (strides of 0, as of an expanded tensor, mean dense ones)
+        raise ValueError("pages: rows that lie in memory one after the other expected")
     p = BurstPagedParams(sequences=lengths.shape[0], rows=q_rows, H=H, kv_heads=kv_heads, d=d, dtype=code, pages=k_pages.shape[0],
                          page=k_pages.shape[2], width=table.shape[1], max_new=max_new, causal=1 if causal else 0,
                          out_f32=1 if out_f32 else 0, scale=scale, window=window, starts=starts.data_ptr(), lengths=lengths.data_ptr(),
-                         table=table.data_ptr(), table_stride=table.stride(0))
-    if not k_pages.is_contiguous():
-        p.page_strides[:] = [k_pages.stride(i) for i in range(3)]
+                         table=table.data_ptr(), table_stride=table.stride(0) if table.shape[0] > 1 else 0)
+    p.page_strides[:] = strides_of(k_pages) or (0, 0, 0)
     return p
+
+
+_TYPES = {BURST_BF16: torch.bfloat16, BURST_F32: torch.float32}
+
+
+def _lying(t, shape, dtype, want, what):
+    """Pointer of a tensor that must have these sizes (the first one at least), this type and these strides of all dimensions but the last
+    (all 0: dense)."""
+    if t.dtype != dtype or t.dim() != len(shape) or t.shape[0] < shape[0] or tuple(t.shape[1:]) != tuple(shape[1:]):
+        raise ValueError(f"{what}: {dtype} tensor {list(shape)} expected")
+    want = tuple(want)
+    if any(want):
+        lies = (shape[-1] <= 1 or t.stride(-1) == 1) and all(n <= 1 or t.stride(i) == want[i] for i, n in enumerate(shape[:-1]))
+    else:
+        lies = t.is_contiguous()
+    if not lies:
+        raise ValueError(f"{what}: strides as the parameter block says expected")
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _pages(t, p, what):
+    return _lying(t, (p.pages, p.kv_heads, p.page, p.d), _TYPES.get(p.dtype), p.page_strides, what)
+
+
+def _tokens(t, heads, strides, p, what, dtype=None):
+    return _lying(t, (p.rows, heads, p.d), dtype or _TYPES.get(p.dtype), strides, what)
+
+
+def _offsets(t, p):
+    if t is not None and (t.dtype != torch.int64 or tuple(t.shape) != (p.sequences,)):
+        raise ValueError("offsets: int64 device tensor [sequences] expected")
+    return _ptr(t)
 
 
 def burst_cache_append(K, V, k_pages, v_pages, Q, Q_out, offsets, r, p):
     """Q, Q_out, offsets, r: None where there are none."""
-    at = lambda t: None if t is None else ctypes.c_void_p(t.data_ptr())      # noqa: E731  (strided: see the block)
-    _check(load().burst_cache_append(at(K), at(V), at(k_pages), at(v_pages), at(Q), at(Q_out), _ptr(offsets),
+    k, v = _tokens(K, p.kv_heads, p.kv_strides, p, "K"), _tokens(V, p.kv_heads, p.kv_strides, p, "V")
+    q, q_out = (None, None) if Q is None else (_tokens(Q, p.H, p.q_strides, p, "Q"), _tokens(Q_out, p.H, p.o_strides, p, "Q_out"))
+    _check(load().burst_cache_append(k, v, _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"), q, q_out, _offsets(offsets, p),
                                      None if r is None else ctypes.byref(r), ctypes.byref(p), _stream()), "burst_cache_append")
 
 
@@ -513,9 +563,11 @@ def burst_paged_workspace_bytes(p):
 
 
 def burst_paged_fwd(Q, k_pages, v_pages, O, lse, p, workspace=None):
-    at = lambda t: ctypes.c_void_p(t.data_ptr())                             # noqa: E731
-    _check(load().burst_paged_fwd(at(Q), at(k_pages), at(v_pages), at(O), _f32(lse), _ptr(workspace), _bytes(workspace),
-                                  ctypes.byref(p), _stream()), "burst_paged_fwd")
+    if lse.numel() < p.rows * p.H:
+        raise ValueError("lse: [rows, H] expected")
+    _check(load().burst_paged_fwd(_tokens(Q, p.H, p.q_strides, p, "Q"), _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"),
+                                  _tokens(O, p.H, p.o_strides, p, "O", torch.float32 if p.out_f32 else None), _f32(lse),
+                                  _ptr(workspace), _bytes(workspace), ctypes.byref(p), _stream()), "burst_paged_fwd")
 
 
 class Event:
