@@ -333,7 +333,7 @@ typedef struct burst_paged_params {
   int32_t causal;                    /* burst_paged_fwd: 0 = every key of the sequence is visible, 1 = those up to the token's position */
   int32_t out_f32;                   /* burst_paged_fwd: 1 = O is fp32 whatever the dtype */
   float   scale;                     /* burst_paged_fwd: as in burst_params */
-  int32_t reserved;                  /* 0 */
+  int32_t full_p;                    /* burst_paged_fwd, bf16: 1 = probabilities with 16 bits at every d (see there) */
   int64_t window;                    /* burst_paged_fwd: as in burst_params */
   const int32_t* starts; const int32_t* lengths; const int32_t* table;   /* DEVICE [sequences + 1], [sequences], [sequences][width] */
   int64_t table_stride;              /* entries from one sequence's pages to the next's; 0 = width */
@@ -352,7 +352,8 @@ int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_page
  * dense.  Tokens that see no key get O = 0 and lse = -inf; rows behind the last sequence are left as they were.  (O as fp32, lse, 1) is
  * a state that burst_merge_state takes: sequences whose cache is spread over a ring are put together so.
  * Hidden keys have no effect whatever they hold.  The order of the sums depends on the sizes, lengths and max_new of the call, all sequences'
- * among them; a call repeated gives the same bits.  bf16 probabilities are rounded to bf16 before the second product.
+ * among them; a call repeated gives the same bits.  bf16 probabilities enter the second product with 16 bits (two bf16 terms); at d = 64 and
+ * d = 128 the kernel of longer chunks rounds them to bf16 once, as burst_local_fwd does there, unless full_p is set.
  * workspace: burst_paged_workspace_bytes(p) bytes of device memory, 16-byte aligned, contents undefined before and after; two
  * calls that may run at the same time need one each. */
 int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,

@@ -62,7 +62,7 @@ class BurstRows(ctypes.Structure):
 class BurstPagedParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "rows", "H", "kv_heads", "d", "dtype", "pages", "page", "width",
                                               "max_new", "causal", "out_f32")] + [
-        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("window", ctypes.c_int64),
+        ("scale", ctypes.c_float), ("full_p", ctypes.c_int32), ("window", ctypes.c_int64),
         ("starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
         ("page_strides", ctypes.c_int64 * 3), ("q_strides", ctypes.c_int64 * 2), ("kv_strides", ctypes.c_int64 * 2),
         ("o_strides", ctypes.c_int64 * 2)]
@@ -494,7 +494,7 @@ def burst_rotate(xs, ys, r, offsets=None, positions=None):
     _check(load().burst_rotate(items, len(xs), ctypes.byref(r), xs[0].shape[3] if len(xs) else 2, dtype, _stream()), "burst_rotate")
 
 
-def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts, scale=1.0, causal=True, window=0, max_new=0, out_f32=False):
+def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts, scale=1.0, causal=True, window=0, max_new=0, out_f32=False, full_p=False):
     """k_pages: [pages, kv_heads, page, d] (its strides go into the block; V_pages lies likewise); table [sequences, width], lengths
     [sequences], starts [sequences + 1]: int32 device tensors.  Token tensors are dense unless their strides are set in the block."""
     code = {torch.bfloat16: BURST_BF16, torch.float32: BURST_F32, "bf16": BURST_BF16, "f32": BURST_F32}.get(dtype, dtype)
@@ -510,7 +510,7 @@ def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts,
         raise ValueError("pages: rows that lie in memory one after the other expected")
     p = BurstPagedParams(sequences=lengths.shape[0], rows=q_rows, H=H, kv_heads=kv_heads, d=d, dtype=code, pages=k_pages.shape[0],
                          page=k_pages.shape[2], width=table.shape[1], max_new=max_new, causal=1 if causal else 0,
-                         out_f32=1 if out_f32 else 0, scale=scale, window=window, starts=starts.data_ptr(), lengths=lengths.data_ptr(),
+                         out_f32=1 if out_f32 else 0, scale=scale, full_p=1 if full_p else 0, window=window, starts=starts.data_ptr(), lengths=lengths.data_ptr(),
                          table=table.data_ptr(), table_stride=table.stride(0) if table.shape[0] > 1 else 0)
     p.page_strides[:] = strides_of(k_pages) or (0, 0, 0)
     return p

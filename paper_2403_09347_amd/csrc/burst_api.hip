@@ -730,6 +730,7 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   a.q_row = g.q[0]; a.q_head = g.q[1]; a.o_row = g.o[0]; a.o_head = g.o[1];
   a.p_page = g.page[0]; a.p_head = g.page[1]; a.p_row = g.page[2];
   a.o_f32 = p->out_f32 != 0 || p->dtype == BURST_F32;
+  a.full_p = p->full_p != 0;
   a.scale = p->scale;
   burst::PagedWork& w = a.w;
   w.starts = p->starts; w.lengths = p->lengths; w.sequences = p->sequences; w.rows = p->rows; w.cap = cap;

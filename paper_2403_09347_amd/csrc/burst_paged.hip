@@ -515,7 +515,12 @@ struct TileFeed {
 // 900, which two wavefronts a SIMD overlap in part.  (Four buffers instead of two at d = 64: 535 / 526 at that size, the others within 1 %.)
 constexpr int kTile = 1 << kTileShift;             // keys
 // C: columns that are computed, of the D that a row of LDS has.
-template <int D, int C>
+// TERMS: bf16 terms that P goes into the second product in.  One (8 bits) at d = 64 and d = 128, as in the walks there, unless the caller asks for
+// full_p; two (16 bits) otherwise.  O is then 2.35e-3 of its norm off 64 bits, or 1.66e-3, which is what rounding O to bf16 does alone, at
+// any number of keys (both the errors and O go with the root of the sum of p^2).  us with one / two: 2048 tokens over 32768 keys, 32 heads over
+// 8, d = 128, 1100 / 1470; 4096 of 8192, d = 64, twice, 544 / 697; 12 sequences of 1 to 512 over 600 to 8000 167 / 173; a window of 1024,
+// d = 64, 36.3 / 41.2; 16 x 8 tokens over 8192 113.5 / 114.7.
+template <int D, int C, int TERMS>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_kernel(PagedArgs a) {
   typedef TileFeed<bf16, D, kTileShift> Feed;
@@ -538,6 +543,9 @@ paged_chunk_kernel(PagedArgs a) {
       taddr[db][sx] = base + 2 * TILE + row * ROWB + ((granule ^ Feed::code(row)) << 4) + (j16 & 1) * 8;
     }
   const float c = a.scale * kLog2e;
+  unsigned c1 = 0x0000bf80u, c2 = 0xbf800000u;     // (-1, 0) and (0, -1), in registers: x - bf16(x) is one dot product, exact
+  asm("" : "+s"(c1), "+s"(c2));
+  const bf16x2 minus_first = __builtin_bit_cast(bf16x2, c1), minus_second = __builtin_bit_cast(bf16x2, c2);
   int buf = 0;
 #pragma unroll 1
   do {
@@ -568,10 +576,6 @@ paged_chunk_kernel(PagedArgs a) {
     const int t0 = s.block * b.w.tokens + 32 * w / b.part_heads, t1 = s.block * b.w.tokens + min((32 * w + 31) / b.part_heads, most);
     const bool rows_here = 32 * w / b.part_heads <= most;
     const KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
-    // Rows of few keys have P in two terms, 16 bits of it: their outputs are not small against V, and what rounding P to 8 bits does to them
-    // would be seen beside the rounding of O.  (5 tokens of 23 keys: O is 2.7e-3 of its norm off 64 bits with one term, 1.7e-3 with two, as with an exact P;
-    // 64 tokens of 500 keys, one term, 2.3e-3.)
-    const bool few = last.hi - first.lo < 256;
 #pragma unroll 1
     for (; at < end; at++, buf ^= 1) {
       __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
@@ -628,46 +632,44 @@ paged_chunk_kernel(PagedArgs a) {
           for (int r = 0; r < 16; r++) o[db][r] *= alpha;
       }
       const float nref = m == BURST_NEG_INF ? 0.f : -m;
-      // P of the next 16 keys is computed between the products of these.
-      bf16x8 p[4], v[4 * DB];
+      // P of the next 16 keys is computed between the products of these, which add the smaller term first.
+      bf16x8 p[4][TERMS], v[4 * DB];
       auto read = [&](int i) __attribute__((always_inline)) {
         const unsigned at = tile + (i / DB) * 16 * ROWB;
         v[i] = __builtin_shufflevector(lds_tr(taddr[i % DB][0] + at), lds_tr(taddr[i % DB][1] + at), 0, 1, 2, 3, 4, 5, 6, 7);
       };
-      auto prob = [&](int kg, int t) __attribute__((always_inline)) {
+      auto prob = [&](int kg, int t) __attribute__((always_inline)) {   // keys t and t + 1
         const float x = fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t], c, nref));
-        p[kg][t] = (bf16)x;
-        l += x;                                    // (unrounded: lse has 24 bits)
+        const float y = fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t + 1], c, nref));
+        l += x + y;                                // (unrounded: lse has 24 bits)
+        bf16x2 pk;
+        pk[0] = (bf16)x; pk[1] = (bf16)y;
+        p[kg][0][t] = pk[0]; p[kg][0][t + 1] = pk[1];
+        if constexpr (TERMS == 2) {
+          p[kg][1][t] = (bf16)__builtin_amdgcn_fdot2_f32_bf16(pk, minus_first, x, false);
+          p[kg][1][t + 1] = (bf16)__builtin_amdgcn_fdot2_f32_bf16(pk, minus_second, y, false);
+        }
       };
 #pragma unroll
       for (int i = 0; i < AHEAD; i++) read(i);
 #pragma unroll
-      for (int t = 0; t < 8; t++) prob(0, t);
+      for (int t = 0; t < 8; t += 2) prob(0, t);
       BURST_FENCE();
 #pragma unroll
-      for (int i = 0; i < 4 * DB; i++) {
-        const int kg = i / DB, db = i % DB;
-        o[db] = mfma32(v[i], p[kg], o[db]);
-        if (i + AHEAD < 4 * DB) read(i + AHEAD);
-        if (kg < 3)
+      for (int kg = 0; kg < 4; kg++)
 #pragma unroll
-          for (int t = 0; t < 8; t++)
-            if (t * DB / 8 == db) prob(kg + 1, t);
-        BURST_FENCE();
-      }
-      if (few) {
-#pragma unroll
-        for (int kg = 0; kg < 4; kg++) {
-          bf16x8 rest;
-#pragma unroll
-          for (int t = 0; t < 8; t++) rest[t] = (bf16)(fast_exp2(__builtin_fmaf(sc[kg >> 1][8 * (kg & 1) + t], c, nref)) - (float)p[kg][t]);
+        for (int term = TERMS - 1; term >= 0; term--)
 #pragma unroll
           for (int db = 0; db < DB; db++) {
-            const unsigned at = tile + kg * 16 * ROWB;
-            o[db] = mfma32(__builtin_shufflevector(lds_tr(taddr[db][0] + at), lds_tr(taddr[db][1] + at), 0, 1, 2, 3, 4, 5, 6, 7), rest, o[db]);
+            const int i = kg * DB + db, at = (TERMS - 1 - term) * DB + db;
+            o[db] = mfma32(v[i], p[kg][term], o[db]);
+            if (term == 0 && i + AHEAD < 4 * DB) read(i + AHEAD);
+            if (kg < 3)
+#pragma unroll
+              for (int t = 0; t < 4; t++)
+                if (t * TERMS * DB / 4 == at) prob(kg + 1, 2 * t);
+            BURST_FENCE();
           }
-        }
-      }
     }
     l = sum_both_halves(l);
     unsigned big = larger_of(0, l);
@@ -959,10 +961,13 @@ int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s) {
 int launch_paged_chunk(const PagedArgs& a, int dtype, hipStream_t s) {
   const dim3 grid((unsigned)a.runs), block(256);
   if (dtype == BURST_BF16) {
-    if (a.d <= 32) BURST_LAUNCH((paged_chunk_kernel<64, 32>), grid, block, 0, s, a);
-    else if (a.d <= 64) BURST_LAUNCH((paged_chunk_kernel<64, 64>), grid, block, 0, s, a);
-    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_kernel<128, 96>), grid, block, 0, s, a);
-    else BURST_LAUNCH((paged_chunk_kernel<128, 128>), grid, block, 0, s, a);
+    const bool one = !a.full_p && (a.d == 64 || a.d == 128);
+    if (a.d <= 32) BURST_LAUNCH((paged_chunk_kernel<64, 32, 2>), grid, block, 0, s, a);
+    else if (a.d <= 64 && one) BURST_LAUNCH((paged_chunk_kernel<64, 64, 1>), grid, block, 0, s, a);
+    else if (a.d <= 64) BURST_LAUNCH((paged_chunk_kernel<64, 64, 2>), grid, block, 0, s, a);
+    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_kernel<128, 96, 2>), grid, block, 0, s, a);
+    else if (one) BURST_LAUNCH((paged_chunk_kernel<128, 128, 1>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_chunk_kernel<128, 128, 2>), grid, block, 0, s, a);
   } else {
     if (a.d <= 64) BURST_LAUNCH((paged_chunk_f32_kernel<64, 64>), grid, block, 0, s, a);
     else if (a.d <= 96) BURST_LAUNCH((paged_chunk_f32_kernel<128, 96>), grid, block, 0, s, a);

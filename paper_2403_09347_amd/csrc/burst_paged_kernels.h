@@ -19,6 +19,7 @@ struct PagedArgs {
   int heads, group, d, pages, page_shift;
   int parts_each, part_heads;        // parts of a key/value head, query heads of a part
   int runs, slack, few, o_f32;       // slack, few: see paged_deal
+  int full_p;                        // see paged_chunk_kernel's TERMS
   float scale;
 };
 // What a run tells the merging launch: the item that is joined from the parts of n runs, from the run before it on (n = 0: none); run 0, which

@@ -480,7 +480,7 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
 
 std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_pages, const Tensor& v_pages, const Tensor& table, const Tensor& lengths,
                                            const Tensor& starts, double scale, bool causal, int64_t window, int64_t max_new,
-                                           const std::optional<Tensor>& o_out, const std::optional<Tensor>& lse_out) {
+                                           const std::optional<Tensor>& o_out, const std::optional<Tensor>& lse_out, bool full_p) {
   burst_paged_params p = describe_paged(k_pages, v_pages, table, lengths, starts);
   check_tokens(q_in, k_pages, "q");
   TORCH_CHECK_VALUE(max_new >= 0 && max_new <= 0x7fffffff && window >= 0, "max_new, window: not negative expected");
@@ -507,6 +507,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   p.rows = (int32_t)q.size(0); p.H = (int32_t)q.size(1);
   p.scale = (float)scale; p.causal = causal; p.window = window; p.max_new = (int32_t)max_new;
   p.out_f32 = O.scalar_type() == torch::kFloat;
+  p.full_p = full_p;
   set_token_strides(p.q_strides, q);
   set_token_strides(p.o_strides, O);
   const size_t need = burst_paged_workspace_bytes(&p);
