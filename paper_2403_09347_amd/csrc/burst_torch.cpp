@@ -289,6 +289,7 @@ variable_list rotate_all(const variable_list& xs, const Tensor& turns, const var
     from.push_back(rows_in_place(xs[i]) ? xs[i] : xs[i].contiguous());
     const Tensor& x = from[i];
     out.push_back(torch::empty_like(x));           // lies in memory like x, without its gaps
+    if (out[i].stride(3) != 1) out[i] = torch::empty(x.sizes(), x.options());   // (x has rows or heads one element apart: windows of a sequence)
     burst_rows& c = items[i];
     c = burst_rows{};
     c.x = x.data_ptr(); c.y = out[i].data_ptr();
