@@ -273,6 +273,10 @@ std::tuple<int, Tensor, std::vector<Tensor>, std::vector<Tensor>> walk_backward(
 void fits_int(const Tensor& t) {
   for (const int64_t n : t.sizes()) TORCH_CHECK_VALUE(n <= 0x7fffffff, "sizes below 2^31 expected");
 }
+// These calls have no rule for tangents: results of a dual tensor would have none, which says that their derivatives are 0.
+void refuse_tangent(const Tensor& t) {
+  TORCH_CHECK_NOT_IMPLEMENTED(!t._fw_grad(0).defined(), "forward-mode derivatives are not implemented for this call: a tensor without a tangent expected");
+}
 // ---- rotary.burst_rotary: several tensors rotated by one call, and their gradients brought back by another.
 bool rows_in_place(const Tensor& t) {              // strides that burst_rotate takes: all zero would mean dense ones
   if (t.size(3) != 1 && t.stride(3) != 1) return false;
@@ -347,6 +351,7 @@ struct RotateBackward : public torch::autograd::Node {
   std::string name() const override { return "BurstRotaryBackward"; }
 };
 variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns, const variable_list& positions, const Turning& how) {
+  for (const Tensor& x : xs) refuse_tangent(x);
   std::shared_ptr<RotateBackward> node;
   if (at::GradMode::is_enabled() && torch::autograd::any_variable_requires_grad(xs)) {
     node = std::shared_ptr<RotateBackward>(new RotateBackward(), torch::autograd::deleteNode);
@@ -367,6 +372,7 @@ variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns
 void check_turns(const Tensor& turns, int64_t d, const Tensor& like) {
   TORCH_CHECK_VALUE(turns.scalar_type() == torch::kDouble && turns.dim() == 1 && turns.is_contiguous() && turns.device() == like.device(),
                     "turns: contiguous float64 tensor [pairs] on the tensors' device expected");
+  refuse_tangent(turns);
   TORCH_CHECK_VALUE(!turns.requires_grad(), "turns: a tensor that needs no gradient expected");
   TORCH_CHECK_VALUE(turns.numel() >= 1 && 2 * turns.numel() <= d, "turns: between one pair and all of the head's columns expected");
 }
@@ -397,6 +403,7 @@ void check_tokens(const Tensor& t, const Tensor& k_pages, const char* what) {
   TORCH_CHECK_VALUE(t.dim() == 3 && t.device() == k_pages.device() && t.scalar_type() == k_pages.scalar_type() && t.size(2) == k_pages.size(3), what,
                     ": [rows, heads, d] of the type, device and d of the pages expected");
   fits_int(t);
+  refuse_tangent(t);
   TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && t.requires_grad()), what, ": the paged calls have no gradient (call them under torch.no_grad)");
 }
 // A token tensor as it is where its strides can be handed on (unit: elements that they have to be multiples of), else a copy.
@@ -416,6 +423,8 @@ burst_paged_params describe_paged(const Tensor& k_pages, const Tensor& v_pages, 
                     "k_pages: device tensor [pages, kv_heads, page, d] of bfloat16 or float32 expected");
   fits_int(k_pages);
   fits_int(table);
+  refuse_tangent(k_pages);
+  refuse_tangent(v_pages);
   TORCH_CHECK_VALUE(v_pages.scalar_type() == k_pages.scalar_type() && v_pages.device() == k_pages.device() && v_pages.sizes() == k_pages.sizes() &&
                     v_pages.strides() == k_pages.strides(), "v_pages: like k_pages in type, sizes and strides expected");
   TORCH_CHECK_VALUE(k_pages.size(3) == 1 || k_pages.stride(3) == 1, "pages: a contiguous last dimension expected");
@@ -491,6 +500,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   Tensor O, lse;
   if (o_out.has_value()) {
     O = *o_out;
+    refuse_tangent(O);
     TORCH_CHECK_VALUE(O.device() == q.device() && O.sizes() == q.sizes() && (O.scalar_type() == q.scalar_type() || O.scalar_type() == torch::kFloat) &&
                       tokens_in_place(O, 16 / (int64_t)O.element_size()) && (p.dtype == BURST_F32 || O.scalar_type() == torch::kFloat || tokens_in_place(O, 8)),
                       "out: like q in sizes, of its type or float32, on 16-byte boundaries expected");
@@ -500,6 +510,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   }
   if (lse_out.has_value()) {
     lse = *lse_out;
+    refuse_tangent(lse);
     TORCH_CHECK_VALUE(lse.device() == q.device() && lse.scalar_type() == torch::kFloat && lse.is_contiguous() && lse.dim() == 2 && lse.size(0) == q.size(0) &&
                       lse.size(1) == q.size(1), "lse: contiguous float32 [rows, H] expected");
   } else {

@@ -32,3 +32,26 @@ def test_rows_that_overlap_in_memory(dtype, shape, strides):
     z = rand(*shape, dtype=dtype).requires_grad_(True)
     (dx,) = torch.autograd.grad(burst_rotary(z, default_turns(shape[3]), 3), z, g)
     check_rotation("dx", dx, g, 3 + np.arange(shape[2])[None, None], f64(default_turns(shape[3])), inverse=True)
+
+
+def test_forward_mode_is_refused():
+    """There is no rule for tangents: a call that dropped them would give derivatives of 0."""
+    x, t = rand(1, 2, 9, 16), default_turns(16)
+    with fwd.dual_level():
+        dual = fwd.make_dual(x, torch.ones_like(x))
+        for tensors in (dual, [x, dual]):
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                burst_rotary(tensors, t)
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            burst_attention(dual, x, x, turns=t)
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            burst_attention(x, dual, x, turns=t)
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            burst_rotary(x, fwd.make_dual(t, torch.ones_like(t)))
+        with torch.no_grad(), pytest.raises(RuntimeError, match="forward-mode"):
+            burst_rotary(dual, t)                             # (no_grad is about the backward mode)
+        y = x.clone().requires_grad_(True)
+        out = burst_rotary(y, t)
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            torch.autograd.grad(out, y, dual)                 # a gradient with a tangent
+        check_rotation("y", burst_rotary(x, t), x, np.arange(9)[None, None], f64(t))
