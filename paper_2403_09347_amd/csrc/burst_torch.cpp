@@ -277,6 +277,10 @@ void fits_int(const Tensor& t) {
 void refuse_tangent(const Tensor& t) {
   TORCH_CHECK_NOT_IMPLEMENTED(!t._fw_grad(0).defined(), "forward-mode derivatives are not implemented for this call: a tensor without a tangent expected");
 }
+// A caller's tensor that a call has written: graphs that saved it are told so.  (Inference tensors have no version; nothing can save them.)
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // ---- rotary.burst_rotary: several tensors rotated by one call, and their gradients brought back by another.
 bool rows_in_place(const Tensor& t) {              // strides that burst_rotate takes: all zero would mean dense ones
   if (t.size(3) != 1 && t.stride(3) != 1) return false;
@@ -484,6 +488,8 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
   check(burst_cache_append(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ptr(q), ptr(out),
                            offsets.has_value() ? offsets->data_ptr<int64_t>() : nullptr, turns.has_value() ? &r : nullptr, &p, stream_of(k_pages)),
         "burst_cache_append");
+  written(k_pages);
+  written(v_pages);
   if (!q_in.has_value()) return std::nullopt;
   return out;
 }
@@ -526,6 +532,8 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   const Tensor ws = need ? torch::empty({(int64_t)need}, q.options().dtype(torch::kByte)) : Tensor();
   check(burst_paged_fwd(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), O.data_ptr(), lse.data_ptr<float>(), ptr(ws), bytes(ws), &p, stream_of(q)),
         "burst_paged_fwd");
+  if (o_out.has_value()) written(O);
+  if (lse_out.has_value()) written(lse);
   return {O, lse};
 }
 

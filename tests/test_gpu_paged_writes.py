@@ -38,3 +38,53 @@ def test_forward_mode_is_refused():
                 burst_paged_attention(**a, **{n: fwd.make_dual(like, like.clone())})
         with pytest.raises(RuntimeError, match="forward-mode"):
             PagedWalk(b.k_pages, b.v_pages, 0.125).step(dual["q"], b.k, b.v, b.table, b.lengths, b.starts)
+
+
+def test_written_tensors_have_another_version():
+    b = Batch([40, 20], [3, 1], 4, 2, 64)
+    before = b.k_pages._version, b.v_pages._version, b.k._version, b.q._version
+    append(b, q=b.q, turns=default_turns(64))
+    after = b.k_pages._version, b.v_pages._version, b.k._version, b.q._version
+    assert after[0] > before[0] and after[1] > before[1] and after[2:] == before[2:]
+    out, lse = torch.empty_like(b.q.contiguous()), torch.empty(4, 4, device=DEV)
+    versions = out._version, lse._version, b.k_pages._version, b.v_pages._version
+    attend(b, out=out, lse=lse)
+    assert out._version > versions[0] and lse._version > versions[1] and (b.k_pages._version, b.v_pages._version) == versions[2:]
+
+
+def test_a_graph_that_saved_the_pool_does_not_use_what_was_written_since():
+    """A walk over a chunk that lies in the pool, its backward after the next token was appended."""
+    pool = [torch.randn(4, 2, 64, 64, device=DEV).to(BF16) for _ in range(2)]
+    q = torch.randn(1, 4, 10, 64, device=DEV).to(BF16).requires_grad_(True)
+    table, lengths = torch.arange(4, dtype=torch.int32, device=DEV).view(1, 4), torch.tensor([200], dtype=torch.int32, device=DEV)
+    starts = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
+    new = torch.randn(1, 2, 64, device=DEV).to(BF16)
+    for i in range(2):
+        O, _ = burst_attention(q, pool[0][:1], pool[1][:1])
+        if i:
+            burst_cache_append(new, new, *pool, table, lengths, starts)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                O.sum().backward()
+        else:
+            O.sum().backward()
+    O, _ = burst_attention(q, pool[0][:1], pool[1][:1])
+    out = q.detach().new_empty(10, 4, 64)
+    y = (q[0].transpose(0, 1) * out).sum()                    # saves out
+    burst_paged_attention(q.detach()[0].transpose(0, 1), *pool, table, lengths, torch.tensor([0, 10], dtype=torch.int32, device=DEV), out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_inference_mode():
+    with torch.inference_mode():
+        b = Batch([40, 20], [3, 1], 4, 2, 64)
+        append(b)
+        want = attend(b)
+    append(b)                                                 # such tensors have no version, and cannot be saved
+    got = attend(b)
+    assert torch.equal(want[0], got[0])
+    c = Batch([40, 20], [3, 1], 4, 2, 64)
+    with torch.inference_mode():
+        append(c)
+        got = attend(c)
+    assert torch.equal(want[0], got[0])
