@@ -499,6 +499,8 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
                                            const std::optional<Tensor>& o_out, const std::optional<Tensor>& lse_out, bool full_p) {
   burst_paged_params p = describe_paged(k_pages, v_pages, table, lengths, starts);
   check_tokens(q_in, k_pages, "q");
+  TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && (k_pages.requires_grad() || v_pages.requires_grad())),
+                    "pages that require a gradient: the paged calls have no gradient (call them under torch.no_grad)");
   TORCH_CHECK_VALUE(max_new >= 0 && max_new <= 0x7fffffff && window >= 0, "max_new, window: not negative expected");
   const c10::DeviceGuard on(k_pages.device());
   const int64_t unit = 16 / (int64_t)q_in.element_size();
@@ -519,6 +521,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
     refuse_tangent(lse);
     TORCH_CHECK_VALUE(lse.device() == q.device() && lse.scalar_type() == torch::kFloat && lse.is_contiguous() && lse.dim() == 2 && lse.size(0) == q.size(0) &&
                       lse.size(1) == q.size(1), "lse: contiguous float32 [rows, H] expected");
+    TORCH_CHECK_VALUE(!lse.requires_grad(), "lse: a tensor that needs no gradient expected");
   } else {
     lse = torch::empty({q.size(0), q.size(1)}, q.options().dtype(torch::kFloat));
   }

@@ -88,3 +88,22 @@ def test_inference_mode():
         append(c)
         got = attend(c)
     assert torch.equal(want[0], got[0])
+
+
+def test_pages_that_want_a_gradient_are_refused():
+    b = Batch([40, 20], [3, 1], 4, 2, 64)
+    wants = lambda t: t.clone().requires_grad_(True)          # noqa: E731
+    plain = (b.table, b.lengths, b.starts)
+    for k, v in ((wants(b.k_pages), b.v_pages), (b.k_pages, wants(b.v_pages))):
+        with pytest.raises(ValueError, match="gradient"):
+            burst_paged_attention(b.q, k, v, *plain)
+        with pytest.raises(ValueError, match="gradient"):
+            burst_cache_append(b.k, b.v, k, v, *plain)
+        with torch.no_grad():
+            O, _ = burst_paged_attention(b.q, k, v, *plain)
+            assert torch.equal(O, attend(b)[0])
+    lse = torch.empty(4, 4, device=DEV)
+    with pytest.raises(ValueError, match="gradient"):
+        attend(b, lse=wants(lse))
+    with pytest.raises(ValueError, match="gradient"):
+        attend(b, out=wants(b.q.contiguous()))
