@@ -287,6 +287,19 @@ bool rows_in_place(const Tensor& t) {              // strides that burst_rotate 
   for (int i = 0; i < 3; i++) if (t.size(i) > 1 && t.stride(i) != 0) return true;
   return t.is_contiguous();
 }
+void check_turns(const Tensor& turns, int64_t d, const Tensor& like) {
+  TORCH_CHECK_VALUE(turns.scalar_type() == torch::kDouble && turns.dim() == 1 && turns.is_contiguous() && turns.device() == like.device(),
+                    "turns: contiguous float64 tensor [pairs] on the tensors' device expected");
+  refuse_tangent(turns);
+  TORCH_CHECK_VALUE(!turns.requires_grad(), "turns: a tensor that needs no gradient expected");
+  TORCH_CHECK_VALUE(turns.numel() >= 1 && 2 * turns.numel() <= d, "turns: between one pair and all of the head's columns expected");
+}
+// The positions of x's rows as they are where their rows are contiguous, else a copy.
+Tensor positions_for(const Tensor& p, const Tensor& x) {
+  TORCH_CHECK_VALUE(p.scalar_type() == torch::kLong && p.device() == x.device() && (p.dim() == 1 || (p.dim() == 2 && p.size(0) == x.size(0))) &&
+                    p.size(-1) == x.size(2), "positions: int64 [rows] or [B, rows] on the tensors' device expected");
+  return p.size(-1) <= 1 || p.stride(-1) == 1 ? p : p.contiguous();
+}
 variable_list rotate_all(const variable_list& xs, const Tensor& turns, const variable_list& positions, const std::vector<int64_t>& position_of,
                          const std::vector<int64_t>& offsets, bool interleaved, double amplitude, bool inverse) {
   const Tensor& like = xs[0];
@@ -339,11 +352,13 @@ struct RotateBackward : public torch::autograd::Node {
       if (!grads[i].defined()) continue;
       some.push_back(grads[i].scalar_type() == type ? grads[i] : grads[i].to(type));
       back.position_of.push_back(how.position_of[i] >= 0 ? (int64_t)where.size() : -1);
-      if (how.position_of[i] >= 0) where.push_back(positions[how.position_of[i]].unpack());
+      if (how.position_of[i] >= 0) where.push_back(positions_for(positions[how.position_of[i]].unpack(), some.back()));
       back.offsets.push_back(how.offsets[i]);
     }
     if (some.empty()) return out;
-    const variable_list g = rotate_differentiably(some, turns.unpack(), where, back);   // (create_graph: a rotation again)
+    const Tensor t = turns.unpack().contiguous();  // (hooks on saved tensors may return them in another layout than they were saved in)
+    check_turns(t, some[0].size(3), some[0]);
+    const variable_list g = rotate_differentiably(some, t, where, back);   // (create_graph: a rotation again)
     for (size_t i = 0, k = 0; i < grads.size(); i++)
       if (grads[i].defined()) out[i] = g[k++];
     return out;
@@ -373,13 +388,6 @@ variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns
   if (node) torch::autograd::set_history(out, node);
   return out;
 }
-void check_turns(const Tensor& turns, int64_t d, const Tensor& like) {
-  TORCH_CHECK_VALUE(turns.scalar_type() == torch::kDouble && turns.dim() == 1 && turns.is_contiguous() && turns.device() == like.device(),
-                    "turns: contiguous float64 tensor [pairs] on the tensors' device expected");
-  refuse_tangent(turns);
-  TORCH_CHECK_VALUE(!turns.requires_grad(), "turns: a tensor that needs no gradient expected");
-  TORCH_CHECK_VALUE(turns.numel() >= 1 && 2 * turns.numel() <= d, "turns: between one pair and all of the head's columns expected");
-}
 std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, const std::vector<int64_t>& offsets,
                            const std::vector<std::optional<Tensor>>& positions, bool interleaved, double amplitude) {
   TORCH_CHECK_VALUE(!xs.empty() && offsets.size() == xs.size() && positions.size() == xs.size(), "one offset and one entry of positions per tensor expected");
@@ -395,9 +403,7 @@ std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, c
     const auto& p = positions[i];
     how.position_of.push_back(p.has_value() ? (int64_t)at.size() : -1);
     if (!p.has_value()) continue;
-    TORCH_CHECK_VALUE(p->scalar_type() == torch::kLong && p->device() == xs[i].device() && (p->dim() == 1 || (p->dim() == 2 && p->size(0) == xs[i].size(0))) &&
-                      p->size(-1) == xs[i].size(2), "positions: int64 [rows] or [B, rows] on the tensors' device expected");
-    at.push_back(p->size(-1) <= 1 || p->stride(-1) == 1 ? *p : p->contiguous());
+    at.push_back(positions_for(*p, xs[i]));
   }
   return rotate_differentiably(xs, turns, at, how);
 }

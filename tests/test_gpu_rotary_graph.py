@@ -55,3 +55,36 @@ def test_forward_mode_is_refused():
         with pytest.raises(RuntimeError, match="forward-mode"):
             torch.autograd.grad(out, y, dual)                 # a gradient with a tangent
         check_rotation("y", burst_rotary(x, t), x, np.arange(9)[None, None], f64(t))
+
+
+@pytest.mark.parametrize("shape", [(11,), (2, 11)])
+def test_hooks_that_give_saved_tensors_back_in_another_layout(shape):
+    x, g, t = rand(2, 3, 11, 32).requires_grad_(True), rand(2, 3, 11, 32, seed=1), default_turns(32)
+    pos = torch.randint(0, 1 << 20, shape, generator=torch.Generator().manual_seed(3)).to(DEV)
+    seen = []
+
+    def spread(saved):                                        # the same values, every second element of a larger tensor
+        seen.append(saved.shape)
+        wide = torch.full((*saved.shape, 2), 77, dtype=saved.dtype, device=saved.device)
+        wide[..., 0] = saved
+        return wide[..., 0]
+
+    def turned(saved):                                        # (of two dimensions) column by column
+        return saved.t().contiguous().t() if saved.dim() == 2 else spread(saved)
+
+    def narrow(saved):                                        # rows with gaps between them
+        wide = torch.full((*saved.shape[:-1], saved.shape[-1] + 3), 77, dtype=saved.dtype, device=saved.device)
+        wide[..., :-3] = saved
+        return wide[..., :-3]
+
+    for unpack in (spread, turned, narrow, lambda saved: saved.cpu().to(DEV)):
+        with torch.autograd.graph.saved_tensors_hooks(lambda saved: saved.clone(), unpack):
+            y = burst_rotary(x, t, 5, positions=pos)
+        (dx,) = torch.autograd.grad(y, x, g)
+        check_rotation("dx", dx, g, 5 + f64(pos if pos.dim() == 2 else pos[None])[:, None], f64(t), inverse=True)
+    assert len(seen) >= 2
+    for unpack in (lambda saved: saved[..., :4], lambda saved: saved.float(), lambda saved: saved.cpu()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda saved: saved.clone(), unpack):
+            y = burst_rotary(x, t, 5, positions=pos)
+        with pytest.raises(ValueError):                       # what the kernel could not read
+            torch.autograd.grad(y, x, g)
