@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/functions/utils.h>
 
 #include <cmath>
+#include <mutex>
 #include <optional>
 #include <string>
 #include <vector>
@@ -346,6 +347,7 @@ struct RotateBackward : public torch::autograd::Node {
   Turning how;
   at::ScalarType type;
   variable_list apply(variable_list&& grads) override {
+    const std::lock_guard<std::mutex> lock(mutex_);   // (threads that go back through one graph: another one's release_variables)
     variable_list out(grads.size()), some, where;
     Turning back{{}, {}, how.interleaved, how.amplitude, !how.inverse};
     for (size_t i = 0; i < grads.size(); i++) {
@@ -364,6 +366,7 @@ struct RotateBackward : public torch::autograd::Node {
     return out;
   }
   void release_variables() override {
+    const std::lock_guard<std::mutex> lock(mutex_);
     turns.reset_data();
     for (auto& p : positions) p.reset_data();
   }

@@ -88,3 +88,25 @@ def test_hooks_that_give_saved_tensors_back_in_another_layout(shape):
             y = burst_rotary(x, t, 5, positions=pos)
         with pytest.raises(ValueError):                       # what the kernel could not read
             torch.autograd.grad(y, x, g)
+
+
+def test_several_threads_go_back_through_one_graph():
+    x, g, t = rand(1, 4, 200, 64).requires_grad_(True), rand(1, 4, 200, 64, seed=1), default_turns(64)
+    pos = torch.arange(200, device=DEV)
+    y = burst_rotary(x, t, 5, positions=pos)
+    (want,) = torch.autograd.grad(y, x, g, retain_graph=True)
+    torch.cuda.synchronize()
+    bad = []
+
+    def back():
+        for _ in range(20):
+            (dx,) = torch.autograd.grad(y, x, g, retain_graph=True)
+            if not torch.equal(dx, want):
+                bad.append(1)
+
+    threads = [threading.Thread(target=back) for _ in range(4)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not bad
