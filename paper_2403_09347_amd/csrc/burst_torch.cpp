@@ -331,7 +331,7 @@ variable_list rotate_all(const variable_list& xs, const Tensor& turns, const var
                      stream_of(like)), "burst_rotate");
   return out;
 }
-// What a rotation is, but for its tensors; position_of: for each tensor the place of its positions, -1 = none.
+// What the rotation of some tensors is; position_of: for each tensor the place of its positions, -1 = none.
 struct Turning {
   std::vector<int64_t> position_of, offsets;
   bool interleaved;
@@ -350,8 +350,10 @@ struct RotateBackward : public torch::autograd::Node {
     const std::lock_guard<std::mutex> lock(mutex_);   // (threads that go back through one graph: another one's release_variables)
     variable_list out(grads.size()), some, where;
     Turning back{{}, {}, how.interleaved, how.amplitude, !how.inverse};
+    std::vector<size_t> to;
     for (size_t i = 0; i < grads.size(); i++) {
-      if (!grads[i].defined()) continue;
+      if (!grads[i].defined() || !task_should_compute_output(i)) continue;
+      to.push_back(i);
       some.push_back(grads[i].scalar_type() == type ? grads[i] : grads[i].to(type));
       back.position_of.push_back(how.position_of[i] >= 0 ? (int64_t)where.size() : -1);
       if (how.position_of[i] >= 0) where.push_back(positions_for(positions[how.position_of[i]].unpack(), some.back()));
@@ -361,8 +363,7 @@ struct RotateBackward : public torch::autograd::Node {
     const Tensor t = turns.unpack().contiguous();  // (hooks on saved tensors may return them in another layout than they were saved in)
     check_turns(t, some[0].size(3), some[0]);
     const variable_list g = rotate_differentiably(some, t, where, back);   // (create_graph: a rotation again)
-    for (size_t i = 0, k = 0; i < grads.size(); i++)
-      if (grads[i].defined()) out[i] = g[k++];
+    for (size_t k = 0; k < to.size(); k++) out[to[k]] = g[k];
     return out;
   }
   void release_variables() override {
@@ -375,12 +376,20 @@ struct RotateBackward : public torch::autograd::Node {
 variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns, const variable_list& positions, const Turning& how) {
   for (const Tensor& x : xs) refuse_tangent(x);
   std::shared_ptr<RotateBackward> node;
-  if (at::GradMode::is_enabled() && torch::autograd::any_variable_requires_grad(xs)) {
+  std::vector<size_t> wanted;                      // the tensors that need a gradient: the others, frozen keys say, are no part of the graph
+  if (at::GradMode::is_enabled())
+    for (size_t i = 0; i < xs.size(); i++)
+      if (xs[i].requires_grad()) wanted.push_back(i);
+  if (!wanted.empty()) {
     node = std::shared_ptr<RotateBackward>(new RotateBackward(), torch::autograd::deleteNode);
-    node->set_next_edges(torch::autograd::collect_next_edges(xs));
+    node->how = Turning{{}, {}, how.interleaved, how.amplitude, how.inverse};
+    for (const size_t i : wanted) {
+      node->add_next_edge(torch::autograd::impl::gradient_edge(xs[i]));
+      node->how.position_of.push_back(how.position_of[i] >= 0 ? (int64_t)node->positions.size() : -1);
+      if (how.position_of[i] >= 0) node->positions.emplace_back(positions[how.position_of[i]], false);
+      node->how.offsets.push_back(how.offsets[i]);
+    }
     node->turns = torch::autograd::SavedVariable(turns, false);
-    for (const Tensor& p : positions) node->positions.emplace_back(p, false);
-    node->how = how;
     node->type = xs[0].scalar_type();
   }
   variable_list out;
@@ -388,7 +397,7 @@ variable_list rotate_differentiably(const variable_list& xs, const Tensor& turns
     const at::NoGradGuard no_grad;
     out = rotate_all(xs, turns, positions, how.position_of, how.offsets, how.interleaved, how.amplitude, how.inverse);
   }
-  if (node) torch::autograd::set_history(out, node);
+  for (const size_t i : wanted) torch::autograd::set_history(out[i], node);
   return out;
 }
 std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, const std::vector<int64_t>& offsets,

@@ -110,3 +110,30 @@ def test_several_threads_go_back_through_one_graph():
     for th in threads:
         th.join()
     assert not bad
+
+
+def test_inputs_that_need_no_gradient_get_none():
+    """Frozen keys beside trained queries: their rotation is no part of the graph, and nothing is computed for them."""
+    q, k, g, t = rand(1, 2, 9, 16).requires_grad_(True), rand(1, 4, 9, 16), rand(1, 2, 9, 16, seed=1), default_turns(16)
+    pos = torch.arange(9, device=DEV)
+    a, b, c = burst_rotary([k, q, k], t, offset=[1, 2, 3], positions=[None, pos, pos])
+    assert b.requires_grad and not a.requires_grad and not c.requires_grad and a.grad_fn is None
+    (dq,) = torch.autograd.grad(b, q, g)
+    check_rotation("dq", dq, g, 2 + np.arange(9)[None, None], f64(t), inverse=True)
+    check_rotation("c", c, k, 3 + np.arange(9)[None, None], f64(t))
+
+
+def test_gradients_that_nobody_asks_for_are_not_computed():
+    q, t = rand(1, 1, 8, 64).requires_grad_(True), default_turns(64)
+    k = rand(1, 8, 8192, 64).requires_grad_(True)             # 16 MiB
+    y, z = burst_rotary([q, k], t)
+    g, h = torch.ones_like(y), torch.ones_like(z)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.max_memory_allocated()
+    (dq,) = torch.autograd.grad([y, z], [q], [g, h], retain_graph=True)
+    assert torch.cuda.max_memory_allocated() - before < 1 << 20
+    check_rotation("dq", dq, g, np.arange(8)[None, None], f64(t), inverse=True)
+    dq2, dk = torch.autograd.grad([y, z], [q, k], [g, h])
+    assert torch.equal(dq, dq2) and dk.shape == k.shape
+    check_rotation("dk", dk, h, np.arange(8192)[None, None], f64(t), inverse=True)
