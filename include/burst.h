@@ -321,8 +321,9 @@ int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d,
 /* The new tokens of several sequences and the pages of their caches.  New tokens lie packed, sequence after sequence:
  * sequence s has rows starts[s] .. starts[s + 1] - 1 of the token tensors, which are indexed [row, head, d].  lengths[s] counts
  * the tokens of the sequence, the new ones among them: new token t of n is at position lengths[s] - n + t, and position p
- * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to 0 .. width * page and starts to 0 .. rows, and a
- * page that is not in 0 .. pages - 1 holds no keys.  Starts do not decrease: where they do, burst_paged_fwd writes nothing, and which tokens
+ * is row p % page of page table[s * table_stride + p / page].  Lengths are cut to 0 .. 2^30 and starts to 0 .. rows; a
+ * page that is not in 0 .. pages - 1 holds no keys, and neither does a position behind the table's row (from width * page on): new tokens there are
+ * not kept, and see the keys that are.  Starts do not decrease: where they do, burst_paged_fwd writes nothing, and which tokens
  * burst_cache_append takes for whose is not defined.  The arrays are not to
  * change while a call that reads them runs. */
 typedef struct burst_paged_params {
@@ -343,7 +344,7 @@ typedef struct burst_paged_params {
 } burst_paged_params;
 /* Writes the new tokens' keys and values (K, V [rows, kv_heads, d]) to their places in K_pages and V_pages, the keys rotated by their
  * positions + offsets[s] (int64 DEVICE [sequences], NULL: 0; what the ring keeps before this device's share).  r = NULL: nothing is rotated.
- * Q, if not NULL: the queries [rows, H, d] are rotated likewise to Q_out.  Tokens at positions below 0 or in pages that are none are left
+ * Q, if not NULL: the queries [rows, H, d] are rotated likewise to Q_out.  Tokens at positions below 0, behind the table or in pages that are none are left
  * out (their queries are rotated if they have a position), rows of Q_out behind the last sequence left as they were.  One launch.
  * Pages that share a place, by equal table entries of two sequences say, must not both get a new token there. */
 int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_pages, const void* Q, void* Q_out,

@@ -11,14 +11,18 @@
 
 namespace burst {
 
-// A sequence of the batch: rows [first, first + n) of the packed tokens, keys [0, len).  Token t has position len - n + t.
-struct PagedSeq { int first, n, len; };
+// A sequence of the batch: rows [first, first + n) of the packed tokens, keys [0, len).  Token t has position at + t; a sequence that has
+// outgrown its row of the table has tokens at positions from `cap` on, which have no place among the keys.
+constexpr int kMostTokens = 1 << 30;               // of a sequence: every position is below
+struct PagedSeq { int first, n, len, at; };
 BURST_HD PagedSeq paged_seq(int start, int end, int length, int rows, int cap) {
   PagedSeq q;
   q.first = start < 0 ? 0 : start < rows ? start : rows;
   const int e = end < q.first ? q.first : end < rows ? end : rows;
   q.n = e - q.first;
-  q.len = length < 0 ? 0 : length < cap ? length : cap;
+  const int all = length < 0 ? 0 : length < kMostTokens ? length : kMostTokens;
+  q.len = all < cap ? all : cap;
+  q.at = all - q.n;
   return q;
 }
 
@@ -40,9 +44,9 @@ struct PagedWork {
   BURST_HD void keys(const PagedSeq& q, int block, int& lo, int& hi) const {
     const int t0 = block * tokens, t1 = (q.n - t0 < tokens ? q.n : t0 + tokens) - 1;
     lo = 0; hi = q.len;
-    if (causal && q.len - q.n + t1 + 1 < hi) hi = q.len - q.n + t1 + 1;
+    if (causal && q.at + t1 + 1 < hi) hi = q.at + t1 + 1;
     if (window > 0) {
-      const int first = q.len - q.n + t0 - window + 1;   // (all of them below 2^30)
+      const int first = q.at + t0 - window + 1;   // (all of them at most 2^30)
       if (first > 0) lo = first < hi ? first : hi;
     }
     if (hi < lo) hi = lo;
@@ -72,9 +76,10 @@ struct PagedWork {
     }
     return t;
   }
-  // units of two blocks that follow one another, at most; most: of the largest block
+  // units of two blocks that follow one another, at most; most: of the largest block.  (Blocks of a sequence that has outgrown its table all
+  // see its last keys: the ends are no more than those between.)
   BURST_HD int pair(const PagedSeq& q, int n, int most) const {
-    return in_turn() && n > 1 ? cost(q, 0) + cost(q, n - 1) + (tokens >> unit_shift) + 2 : 2 * most;   // (rounded up)
+    return in_turn() && n > 1 && q.at + q.n <= q.len ? cost(q, 0) + cost(q, n - 1) + (tokens >> unit_shift) + 2 : 2 * most;   // (rounded up)
   }
   // Whether a sequence ends behind its start.  Where one does not, rows could belong to several sequences, and there could be more units than
   // 32 bits hold: such a call does nothing.

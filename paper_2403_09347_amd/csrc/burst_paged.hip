@@ -40,7 +40,7 @@ __device__ __forceinline__ ItemRow item_row(const PagedArgs& a, const PagedSegme
 // The keys [lo, hi] that a token sees
 struct KeyRange { int lo, hi; };
 __device__ __forceinline__ KeyRange seen_keys(const PagedWork& w, const PagedSeq& q, int token) {
-  const int pos = q.len - q.n + token;
+  const int pos = q.at + token;
   KeyRange k = {0, w.causal ? min(pos, q.len - 1) : q.len - 1};
   if (w.window > 0) k.lo = max(0, pos - w.window + 1);
   return k;
@@ -229,7 +229,7 @@ paged_short_kernel(PagedArgs a) {
       i32x4* const to = segs[seg_in % NSEG];
       to[0] = i32x4{fet.g.q.first, fet.g.q.n, fet.g.q.len, fet.g.part};
       to[1] = i32x4{fet.g.block, fet.g.from, fet.g.to, fet.s};
-      to[2] = i32x4{f_at, f_end, fet.g.whole() ? 1 : 0, fet.g.from == fet.g.lo ? 1 : 0};
+      to[2] = i32x4{f_at, f_end, fet.g.q.at, (fet.g.whole() ? 1 : 0) | (fet.g.from == fet.g.lo ? 2 : 0)};
     }
     seg_in++;
     look_up();
@@ -289,12 +289,12 @@ paged_short_kernel(PagedArgs a) {
       const i32x4 *const from = segs[seg_out % NSEG], d0 = from[0], d1 = from[1], d2 = from[2];
       auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
       seg_out++;
-      s.q = PagedSeq{one(d0[0]), one(d0[1]), one(d0[2])};
+      s.q = PagedSeq{one(d0[0]), one(d0[1]), one(d0[2]), one(d2[2])};
       s.part = one(d0[3]); s.block = one(d1[0]); s.from = one(d1[1]); s.to = one(d1[2]);
       seg_s = one(d1[3]);
       st = one(d2[0]); end = one(d2[1]);
-      s.lo = one(d2[3]) ? s.from : s.from - 1;     // (as far as whole() and partial_slot() look at them)
-      s.hi = one(d2[2]) ? s.to : s.to + 1;
+      s.lo = one(d2[3]) & 2 ? s.from : s.from - 1; // (as far as whole() and partial_slot() look at them)
+      s.hi = one(d2[3]) & 1 ? s.to : s.to + 1;
       x = item_row(b, s, r);
       see = seen_keys(b.w, s.q, x.token);
       const T* const qr = (const T*)b.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * b.q_row + (size_t)(x.there ? x.head : 0) * b.q_head;

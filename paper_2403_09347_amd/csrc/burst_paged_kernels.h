@@ -71,7 +71,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane,
   PagedTotals mine = {0, 0, 0, 0}, all = {0, 0, 0, 0};
   unsigned long long disorder = 0;
   auto totals = [&](int s) __attribute__((always_inline)) {
-    q = PagedSeq{0, 0, 0};
+    q = PagedSeq{0, 0, 0, 0};
     bool bad = false;
     if (s < w.sequences) {
       const int start = w.starts[s], end = w.starts[s + 1];
@@ -89,7 +89,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane,
 #pragma unroll 1
     for (; longer != 0; longer &= longer - 1) {
       const int at = __builtin_ctzll(longer);
-      const PagedSeq there = {0, __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at)};
+      const PagedSeq there = {0, __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at), __builtin_amdgcn_readlane(q.at, at)};
       PagedTotals t = w.totals(there, __builtin_amdgcn_readlane(n, at), lane, 64);
       t.units = __builtin_amdgcn_readlane(wave_scan(t.units), 63);
       t.most = wave_most(t.most);
@@ -124,7 +124,8 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane,
       before += here;
     }
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(begin < before + scan));
-    const PagedSeq there = {__builtin_amdgcn_readlane(q.first, at), __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at)};
+    const PagedSeq there = {__builtin_amdgcn_readlane(q.first, at), __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at),
+                            __builtin_amdgcn_readlane(q.at, at)};
     const int one = __builtin_amdgcn_readlane(deal.by_items ? mine.items : mine.units, at);
     some = cur.place(w, base + at, there, one, begin - (before + __builtin_amdgcn_readlane(scan - own, at)), deal, min(deal.each, total - begin),
                      [&](int& rem, int n) __attribute__((always_inline)) {   // 64 blocks at a time

@@ -68,12 +68,12 @@ rotate_kernel(RotateArgs a) {
       long long pos = 0, dst = -1;
       if (s >= 0) {
         const PagedSeq q = paged_seq(a.starts[s], a.starts[s + 1], a.lengths[s], a.tokens, a.cap);
-        const int p = q.len - q.n + (row - q.first);
+        const int p = q.at + (row - q.first);
         if (row - q.first < q.n && p >= 0) {
           pos = p + (a.offsets != nullptr ? a.offsets[s] : 0);
           if (!it.paged) {
             dst = (long long)row * it.ys_r;
-          } else {
+          } else if (p < a.cap) {                  // (no entry of the table is behind its row)
             const int page = checked_page(a.table[(long long)s * a.table_stride + (p >> a.page_shift)], a.pages);
             if (page >= 0) dst = page * it.ys_b + (long long)(p & ((1 << a.page_shift) - 1)) * it.ys_r;
           }

@@ -7,7 +7,8 @@ Several sequences at once: token tensors [rows, heads, d] hold the new tokens of
 it is row p % page of page table[s, p // page] of k_pages and v_pages [pages, kv_heads, page, d] (any strides with a contiguous last
 dimension; page: a power of two, 16 or more).  table, lengths and starts are int32 tensors on the device and are read there, so
 that a captured call can be replayed with other contents (they are not to change while a call runs); values outside their
-ranges are cut to them, a page that is not one of the pages holds no keys, and attention with starts that decrease writes nothing."""
+ranges are cut to them, a page that is not one of the pages holds no keys, nor does a position behind the table's row (new tokens there are
+not kept, and see the keys that are), and attention with starts that decrease writes nothing."""
 from . import binding as B
 
 
