@@ -1,7 +1,7 @@
 // Rotation of rows by their positions (burst_rotate), and the same on the way into a paged cache (burst_cache_append).
 // A pair of columns (a, b) of a row at position p becomes (a cos - b sin, b cos + a sin) x amplitude, with the angle
-// 2 pi frac(p x turns[pair]): the product and its fraction in 64 bits (at position 10^6 a product in 32 bits is 0.06 off), the
-// rest in 32.  The gradient is the rotation by the negative angle.
+// 2 pi frac(p x turns[pair]): the angle, its cos and sin in 64 bits (at position 10^6 a product in 32 bits is 0.06 off), which are rounded to
+// 32; the products with a and b in 32.  The gradient is the rotation by the negative angle.
 // Bound by HBM: every row is read and written once.  A workgroup takes some rows of some heads, and computes the angles of
 // its rows once, into LDS, for all of those heads.  Measured: 32 + 32 heads of 4096 rows, d = 128, bf16 (134 MB in and out), 27 us, 4.9 TB/s;
 // appending 7 prompts of 300 to 4096 tokens with their queries, 32 heads over 8 (272 MB), 53 us, 5.1 TB/s.  A device copy moves 5.0 TB/s.
@@ -9,13 +9,13 @@
 
 namespace burst {
 
-// cos and sin of 2 pi x, |x| <= 1/2: the nearest quarter turn, and Taylor's series within pi/4 of it (terms up to x^10 and
-// x^9: the next ones are below 2^-32 and 2^-28).
-__device__ __forceinline__ void cos_sin_turns(float x, float& c, float& s) {
-  const float q = rintf(4.f * x);
-  const float t = (x - 0.25f * q) * 6.283185307179586f, u = t * t;   // (x - q/4 is exact)
-  float cs = 1.f + u * (-0.5f + u * (1.f / 24 + u * (-1.f / 720 + u * (1.f / 40320 - u * (1.f / 3628800)))));
-  float sn = t + t * u * (-1.f / 6 + u * (1.f / 120 + u * (-1.f / 5040 + u * (1.f / 362880))));
+// cos and sin of 2 pi x, in 64 bits: the nearest quarter turn taken off (exactly), and Taylor's series within pi/4 of it (terms up to x^12 and
+// x^11: the next ones are below 2^-41 and 2^-37).  Rounded to 32 bits by the caller, once.
+__device__ __forceinline__ void cos_sin_turns(double x, double& c, double& s) {
+  const double q = rint(4 * x);
+  const double t = (x - 0.25 * q) * 6.283185307179586, u = t * t;
+  const double cs = 1 + u * (-0.5 + u * (1. / 24 + u * (-1. / 720 + u * (1. / 40320 + u * (-1. / 3628800 + u * (1. / 479001600))))));
+  const double sn = t + t * u * (-1. / 6 + u * (1. / 120 + u * (-1. / 5040 + u * (1. / 362880 - u * (1. / 39916800)))));
   const int n = (int)q & 3;
   c = n == 0 ? cs : n == 1 ? -sn : n == 2 ? -cs : sn;
   s = n == 0 ? sn : n == 1 ? cs : n == 2 ? -sn : -cs;
@@ -90,9 +90,9 @@ rotate_kernel(RotateArgs a) {
   for (int k = tid; k < rows * pairs; k += kRowsThreads) {
     const int row = k / pairs;
     const double p = (double)at[row], t = a.turns[k - row * pairs];
-    float c, s;
-    cos_sin_turns((float)__builtin_fma(p, t, -rint(p * t)), c, s);   // (the product's own rounding does not come in)
-    turn[k] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
+    double c, s;
+    cos_sin_turns(__builtin_fma(p, t, -rint(p * t)), c, s);   // (the product's own rounding does not come in)
+    turn[k] = make_float2((float)(c * a.amplitude), (float)((a.inverse ? -s : s) * a.amplitude));
   }
   __syncthreads();
   if (!active) return;
