@@ -311,7 +311,7 @@ typedef struct burst_rows {
   const int64_t* positions;          /* DEVICE: row n of batch entry b is at offset + positions[b * positions_stride + n]; NULL: offset + n */
   int64_t positions_stride, offset;
   int64_t x_strides[3], y_strides[3];/* element strides {batch, head, row}; all zero = contiguous */
-  int32_t B, heads, rows;            /* >= 0 */
+  int32_t B, heads, rows;            /* 0 .. 2^31 - 256 */
   int32_t reserved;                  /* 0 */
 } burst_rows;
 /* Rotates n tensors (queries and the chunks' keys of a walk) of head dimension d, 2 <= d <= 128, and type `dtype`.  Rows may start anywhere

@@ -1152,7 +1152,8 @@ int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d,
   const unsigned size = dtype == BURST_BF16 ? 2 : 4;
   auto item = [&](const burst_rows& t, burst::RotateItem& it, bool& some) -> int {
     it = burst::RotateItem{};
-    if (t.B < 0 || t.heads < 0 || t.rows < 0) return BURST_ERR_SHAPE;
+    for (const int32_t size : {t.B, t.heads, t.rows})
+      if (size < 0 || size > burst::kMaxRotateSize) return BURST_ERR_SHAPE;
     some = t.B > 0 && t.heads > 0 && t.rows > 0;
     if (!some) return BURST_OK;
     REQUIRE_ALIGNED(t.x, size); REQUIRE_ALIGNED(t.y, size);

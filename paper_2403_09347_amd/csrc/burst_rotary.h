@@ -6,6 +6,7 @@
 namespace burst {
 
 constexpr int kRotateRows = 16;                    // most rows of a workgroup
+constexpr int kMaxRotateSize = 0x7fffff00;         // of a dimension: rows and heads of a workgroup are counted past the last one in 32 bits
 constexpr int kMaxRotateItems = 20;                // of a launch: they travel in its arguments, which hold 4 KB
 struct RotateItem {
   const void* x; void* y;

@@ -164,12 +164,12 @@ int launch_rotate(RotateArgs& a, int dtype, hipStream_t s) {
   bool copies = false;
   for (int i = 0; i < a.n; i++) copies = copies || !a.it[i].rotated;
   const int slots = copies ? copied : rotated;     // (the larger number)
-  long long all = 0;                               // rows x heads
-  for (int i = 0; i < a.n; i++) all += (long long)a.it[i].B * a.it[i].rows * a.it[i].heads;
+  double all = 0;                                  // rows x heads
+  for (int i = 0; i < a.n; i++) all += (double)a.it[i].B * a.it[i].rows * a.it[i].heads;
   a.rows_each = kRotateRows;
   while (a.rows_each > 1 && a.rows_each * slots > kRowsThreads) a.rows_each /= 2;
   // Few rows: smaller blocks, so that every CU has some
-  while (a.rows_each > 1 && all < 2048LL * a.rows_each) a.rows_each /= 2;
+  while (a.rows_each > 1 && all < 2048. * a.rows_each) a.rows_each /= 2;
   const int heads_each = 8;
   long long blocks = 0;
   for (int i = 0; i < a.n; i++) {
@@ -178,8 +178,8 @@ int launch_rotate(RotateArgs& a, int dtype, hipStream_t s) {
     it.row_tiles = (it.rows + a.rows_each - 1) / a.rows_each;
     it.heads_each = heads_each;
     it.head_tiles = (it.heads + heads_each - 1) / heads_each;
+    if (blocks + (double)it.B * it.row_tiles * it.head_tiles > 0x7fffffff) return BURST_ERR_SHAPE;
     blocks += (long long)it.B * it.row_tiles * it.head_tiles;
-    if (blocks > 0x7fffffffLL) return BURST_ERR_SHAPE;
   }
   constexpr long long kMost = 1 << 23;             // blocks of a launch: it can have 2^32 threads
   for (long long first = 0; first < blocks; first += kMost) {

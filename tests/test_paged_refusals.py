@@ -135,3 +135,10 @@ def test_torch_calls_refuse_host_tensors_and_lists_that_do_not_fit():
     for bad in (dict(dims=3), dict(dims=0), dict(dims=8, base=0.0), dict(dims=8, factor=-1.0), dict(dims=8, scaling="other")):
         with pytest.raises(ValueError):
             rotary_turns(**bad, device="cpu")
+
+
+def test_sizes_of_rotated_tensors():
+    """Up to 2^31 - 256: the rows and heads of a workgroup are counted past the last one in 32 bits."""
+    for size in ("B", "heads", "rows"):
+        for n in (0x7fffff01, 0x7fffffff):
+            assert rotate(rows(**{size: n}), rotary()) == E_SHAPE, (size, n)
