@@ -544,6 +544,10 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
     lse = torch::empty({q.size(0), q.size(1)}, q.options().dtype(torch::kFloat));
   }
   p.rows = (int32_t)q.size(0); p.H = (int32_t)q.size(1);
+  // No more rows than sequences, and nothing said about them: single tokens, as a step of serving has.  (us a call as if nothing were known / so:
+  // 64 sequences of 16 to 16384 keys, 32 heads over 8, 147 / 128; 256 of 16 to 300 59 / 37; 32 over 2000, 32 heads, 201 / 190; 16 over 4096, fp32,
+  // 177 / 110; 1 over 32768 36.3 / 36.4.)
+  if (max_new == 0 && q.size(0) <= lengths.size(0)) max_new = 1;
   p.scale = (float)scale; p.causal = causal; p.window = window; p.max_new = (int32_t)max_new;
   p.out_f32 = O.scalar_type() == torch::kFloat;
   p.full_p = full_p;

@@ -27,8 +27,9 @@ def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=Non
     """Attention of the new tokens q [rows, H, d] (H a multiple of kv_heads) over the keys of their sequences up to their own positions (causal =
     False: all of them), the last `window` of them if that is not 0.  Returns (O [rows, H, d], lse [rows, H] fp32): new tensors, or out
     (of q's type or float32) and lse; rows behind the last sequence are not written, tokens that see no key get 0 and -inf.
-    max_new: the most new tokens of any sequence, if the caller knows it (chooses the kernel only: 1 gives single tokens the one that is
-    made for them).  O as float32, lse and a sum of 1 are a state that binding.burst_merge_state joins with those of
+    max_new: the most new tokens of any sequence, if the caller knows it (chooses the kernel only: single tokens, with up to 16 query heads for each
+    of keys and values, have one that is made for them).  0: not known; 1 is taken where there are no more rows than sequences.
+    O as float32, lse and a sum of 1 are a state that binding.burst_merge_state joins with those of
     the ring's other devices.  full_p (bfloat16): probabilities enter the product with the values with 16 bits in any call; otherwise the kernel
     of longer chunks rounds them to 8 at d = 64 and d = 128, as the walks do.  No gradient."""
     scale = float(scale) if scale is not None else q.shape[-1] ** -0.5
