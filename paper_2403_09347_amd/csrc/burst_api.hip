@@ -719,6 +719,10 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   // among them.  (Two launches for a call's short and long sequences, each with its join, took longer.  us, two kernels / this one: 12
   // sequences of 1 to 512 new tokens over 600 to 8000 keys, 32 heads, 176 / 165; 64 of 1 to 40 over 4096 to 16384, 32 over 8 heads, 487 / 472;
   // 4 with a window of 1024, d = 64, 42 / 37.)
+  // So are single tokens of groups of more than 16 heads: the short kernel would read the cache once for every 16 of them.  (us, so / by parts of 16
+  // heads in the short kernel: bf16, d = 128, 64 sequences of 4096 to 8192 keys over one head, groups of 17, 32 and 64 52 / 68, 54 / 70, 60 / 116, one of
+  // 32768 22 / 35, 24 / 37, 34 / 36, 128 of 250 to 500 24.3 / 23.4, 24.6 / 25.0, 24.9 / 30.2; fp32, d = 128, 136 / 127, 136 / 129, 219 / 225, 35 / 40, 37 / 42,
+  // 47 / 42, 48 / 31, 49 / 32, 53 / 43.)
   plan.chunk = (long long)most * group > burst::kShortRows;
   const int rows = plan.chunk ? burst::kChunkRows : burst::kShortRows;
   burst::PagedArgs& a = plan.a;

@@ -168,6 +168,7 @@ __device__ __forceinline__ void wait_lds() {
 }
 
 // ------------------------------------------------------------------------------- short
+// Groups of up to 16 heads: an item's part is its key/value head.
 // S^T = K Q^T of 16 keys x 16 rows: lane (r = lane % 16, g = lane / 16) gets row r, keys 4g .. 4g + 3, which is also how the second
 // product, O^T += V^T P^T, wants P.  The order of the summed columns is free, so a lane's operands are 16-byte pieces of a row of K or
 // Q: granule 4 ks + g in step ks.  A stage is 16 keys, K and V, brought to LDS by DMA (rows beyond the sequence arrive as
@@ -216,7 +217,7 @@ paged_short_kernel(PagedArgs a) {
     const int key = (f_at + lane) << 4, entry = table_entry(key, fet.g.q.len, b.page_shift);
     int page = -1;
     if (entry >= 0) page = checked_page(b.table[(long long)fet.s * b.table_stride + entry], b.pages);
-    const long long at = (long long)max(page, 0) * b.p_page + (long long)((unsigned)fet.g.part / (unsigned)b.parts_each) * b.p_head +
+    const long long at = (long long)max(page, 0) * b.p_page + (long long)fet.g.part * b.p_head +
                          (long long)(key & ((1 << b.page_shift) - 1)) * b.p_row;
     const long long where = (long long)(size_t)b.K + at * (long long)sizeof(T);
     where_lo = (int)where; where_hi = (int)(where >> 32);
