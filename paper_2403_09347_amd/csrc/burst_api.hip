@@ -742,10 +742,9 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   w.parts = p->kv_heads * a.parts_each;
   w.causal = p->causal != 0;
   w.window = p->window < 1 << 30 ? (int)p->window : 1 << 30;   // (positions are below)
-  // Units of 32 keys (bf16 chunks: of 64), and what an item's beginning and a join are worth of them.  us a call of the short kernel, units of
-  // 64 keys, beginning 1, slack 2 / so: one token over 32768 keys 38.2 / 37.7, over 4000 18.5 / 16.7, 64 ragged sequences 126.3 / 125.2,
-  // 256 of 16 to 300 keys 39.1 / 35.5 (beginning 1: 137 and 38.5).  The chunk kernel, slack 4 / 8: 4 sequences with a window of 1024, d = 64,
-  // 46 / 37; the others that were tried take the same time with a beginning of 0 to 3 and a slack of 4 to 16.
+  // Units of 32 keys (bf16 chunks: of 64), and what an item's beginning is worth of them.  us a call of the short kernel, units of
+  // 64 keys, beginning 1 / so: one token over 32768 keys 38.2 / 37.7, over 4000 18.5 / 16.7, 64 ragged sequences 126.3 / 125.2,
+  // 256 of 16 to 300 keys 39.1 / 35.5 (beginning 1: 137 and 38.5).  The chunk kernels take the same time with a beginning of 0 to 3.
   w.item_cost = plan.chunk ? 1 : 2;
   double units;                                    // at most so many: 32 bits hold them
   for (w.unit_shift = plan.chunk && p->dtype == BURST_BF16 ? burst::kTileShift : burst::kTileShiftF32;; w.unit_shift++) {
@@ -757,7 +756,18 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   a.runs = units < slots ? (int)units : slots;
   if (a.runs < 1) a.runs = 1;
   if (a.runs > 8) a.runs &= ~7;
-  a.slack = plan.chunk ? 8 : 2;
+  // Runs of whole items: up to `slack` units (and a 16th) longer than the even share, for what cutting costs: partial results and their join, which
+  // grow with the rows that an item has, and a segment more.  Time with whole items over time with cut ones, mean (least, most), by how many units
+  // longer the runs are (windows, prompts, ragged chunks and single tokens of 32 to 2048 items a call):
+  //   bf16 chunks, items of 100 to 128 rows, 184 calls  to 3: 0.76 (0.65, 1.00)  4 to 6: 0.74 (0.62, 0.87)  7 to 8: 0.78 (0.62, 0.94)  9 to 10: 0.86
+  //     (0.70, 1.02)  11 to 12: 0.89 (0.68, 1.22)  13 to 16: 0.93 (0.81, 1.11)  17 to 20: 1.05 (0.88, 1.30)  21 to 25: 1.13 (0.96, 1.56)
+  //     64 to 96 rows, 32 calls  4 to 6: 0.90 (0.86, 0.93)  7 to 8: 0.88 (0.74, 1.06)  9 to 12: 1.02 (0.77, 1.16)  13 to 16: 1.25 (1.17, 1.34)
+  //     20 to 32 rows, 32 calls  4 to 6: 1.00 (0.98, 1.01)  7 to 8: 1.00 (0.87, 1.18)  9 to 12: 1.15 (0.98, 1.27)  13 to 16: 1.39 (1.37, 1.41)
+  //   fp32 chunks, 134 calls  to 2: 0.84 (0.73, 0.94)  3: 0.97 (0.87, 1.07)  4: 1.06 (0.93, 1.18)  5: 1.11 (0.83, 1.27)  6: 1.22 (0.86, 1.40)
+  //   short, 66 calls  to 0: 0.97 (0.90, 1.00)  2: 0.92 (0.87, 0.98)  3 to 4: 0.98 (0.94, 1.02)  6: 1.00 (0.93, 1.08)  8 to 9: 1.06 (1.00, 1.15)
+  // By this rule the 248 bf16 calls take 0.9 % longer in the mean than with the better of the two; 8 units for all of them would be 4.7 %, 12 2.4 %.
+  const int item_rows = (long long)most * group < rows ? most * group : rows;
+  a.slack = !plan.chunk ? 4 : p->dtype == BURST_F32 ? 3 : 4 + 12 * item_rows / burst::kChunkRows;
   // Chunk runs of four units at most: half as many of twice the length, a workgroup a CU, fewer parts to join.  us a call, as many runs as the chip
   // holds / so: 256 tokens over 4096 keys, 8 heads, 36.8 / 28.2, 2 x 40 over 2000, fp32, d = 64, 31.6 / 25.5, 3 of 30 to 300 over 400 to 1500, fp32,
   // 47.1 / 43.1; 16 x 5 over 300 to 900, 32 heads over 8, 21.4 / 22.5.  Up to eight units: 8 x 8 over 4096, fp32, 48 / 56.
