@@ -484,8 +484,9 @@ def burst_rotate(xs, ys, r, offsets=None, positions=None):
             raise ValueError("x, y: device tensors of the same sizes and type expected")
     items = (BurstRows * len(xs))()
     for x, y, at, offset, c in zip(xs, ys, positions, offsets, items):
-        if not all(t.is_cuda for t in (x, y, at) if t is not None):
-            raise ValueError("x, y, positions: device tensors expected")
+        for t, what in ((x, "x"), (y, "y"), (at, "positions")):
+            if t is not None:
+                _here(t, what)
         c.x_strides[:], c.y_strides[:] = strides_of(x) or (0, 0, 0), strides_of(y) or (0, 0, 0)
         c.x, c.y, c.B, c.heads, c.rows, c.offset = x.data_ptr(), y.data_ptr(), x.shape[0], x.shape[1], x.shape[2], offset
         if at is not None:
@@ -516,6 +517,14 @@ def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts,
     return p
 
 
+def _here(t, what):
+    """The device that the library launches on is the current one: a tensor of another device would be read across devices."""
+    if not t.is_cuda:
+        raise ValueError(f"{what}: device tensor expected")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: tensor on the current device expected")
+
+
 _TYPES = {BURST_BF16: torch.bfloat16, BURST_F32: torch.float32}
 
 
@@ -531,8 +540,7 @@ def _lying(t, shape, dtype, want, what):
         lies = t.is_contiguous()
     if not lies:
         raise ValueError(f"{what}: strides as the parameter block says expected")
-    if not t.is_cuda:
-        raise ValueError("device tensor expected")
+    _here(t, what)
     return ctypes.c_void_p(t.data_ptr())
 
 

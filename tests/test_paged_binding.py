@@ -17,7 +17,7 @@ def test_rotated_tensors_and_positions():
             B.burst_rotate([x], [x], R, positions=[bad])
     for good in (at, at[:1].expand(2, 5), at[:, :1]):         # these are fine: it is x that is refused
         y = x[:, :, :good.shape[1]]
-        with pytest.raises(ValueError, match="device tensors"):
+        with pytest.raises(ValueError, match="device tensor"):
             B.burst_rotate([y], [y], R, positions=[good])
     for other in (torch.zeros(2, 3, 5, 8), x.to(BF16), x[0]):
         with pytest.raises(ValueError, match="of one type and d"):
@@ -103,3 +103,15 @@ def test_tensors_of_a_block():
     with pytest.raises(ValueError, match="offsets"):
         B._offsets(torch.zeros(2, dtype=I64), p)
     assert B._offsets(None, p) is None
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """The library launches on the current device."""
+    class Elsewhere:
+        is_cuda, device = True, torch.device("cuda", 1)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device"):
+        B._here(Elsewhere(), "x")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    B._here(Elsewhere(), "x")
