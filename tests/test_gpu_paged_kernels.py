@@ -1,8 +1,9 @@
 """Which kernel a paged attention runs, as its bits show: at d = 128 the kernel of longer chunks rounds P once, the one of single tokens does not."""
+import numpy as np
 import pytest
 import torch
 
-from paged_util import Batch
+from paged_util import Batch, f64
 from paper_2403_09347_amd.harness import PagedWalk
 from paper_2403_09347_amd.paged import burst_cache_append, burst_paged_attention
 
@@ -56,3 +57,24 @@ def test_hidden_values_in_the_kernel_of_chunks(dtype, value):
         at = (int(b.table[1, p // 16]), slice(None), p % 16)
         b.k_pages[at], b.v_pages[at] = value, value
     b.check(*attend(b, max_new=100, window=60), window=60)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("d,H", [(128, 4), (64, 16), (96, 2)])
+def test_rows_that_do_not_see_an_infinity_keep_their_bounds(dtype, value, where, d, H):
+    """Keys 60 and 95 of 100 hold it, the new tokens are those from 55 on: whose window of five keys has neither is held to the bound of the same
+    batch without them."""
+    b = Batch([100, 64], [45, 1], H, 2, d, dtype=dtype, seed=5)
+    O_ref, lse_ref, O_err, lse_err = b.reference(True, 5)
+    pages = b.k_pages if where == "k" else b.v_pages
+    for key in (60, 95):
+        pages[int(b.table[0, key // 16]), :, key % 16] = value
+    O, lse = attend(b, window=5, max_new=60)
+    sees = np.array([any(p - 5 < key <= p for key in (60, 95)) for p in range(55, 100)] + [False])
+    got, got_lse = f64(O), f64(lse)
+    assert np.all(np.abs(got - O_ref)[~sees] <= O_err[~sees]) and np.all(np.abs(got_lse - lse_ref)[~sees] <= lse_err[~sees])
+    assert sees.sum() == 10
+    if where == "v":
+        assert not np.isfinite(got[sees]).any() and np.all(np.abs(got_lse - lse_ref)[sees] <= lse_err[sees])
