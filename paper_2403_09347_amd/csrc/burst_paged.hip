@@ -520,7 +520,8 @@ constexpr int kTile = 1 << kTileShift;             // keys
 // full_p; two (16 bits) otherwise.  O is then 2.35e-3 of its norm off 64 bits, or 1.66e-3, which is what rounding O to bf16 does alone, at
 // any number of keys (both the errors and O go with the root of the sum of p^2).  us with one / two: 2048 tokens over 32768 keys, 32 heads over
 // 8, d = 128, 1100 / 1470; 4096 of 8192, d = 64, twice, 544 / 697; 12 sequences of 1 to 512 over 600 to 8000 167 / 173; a window of 1024,
-// d = 64, 36.3 / 41.2; 16 x 8 tokens over 8192 113.5 / 114.7.
+// d = 64, 36.3 / 41.2; 16 x 8 tokens over 8192 113.5 / 114.7; two prompts of 4096 of 8192, 32 heads over 8, at d = 32 433 / 508, d = 80 674 / 879, d = 96
+// 698 / 915, d = 104 799 / 1061.
 template <int D, int C, int TERMS>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_kernel(PagedArgs a) {
@@ -704,7 +705,8 @@ paged_chunk_kernel(PagedArgs a) {
 }
 
 // fp32: tiles of 32 keys, products as in the short kernel, two blocks of 16 rows a wavefront (each operand of K and V read from LDS serves
-// both).  Bound by the fp32 matrix rate: 4096 tokens over themselves, causal, 8 heads, d = 128, 324 us (106 TFLOP/s; a large library product 153).
+// both).  C: columns of the first product; the second one computes all D, whose blocks of 16 columns each hold every fourth column of 64.
+// Bound by the fp32 matrix rate: 4096 tokens over themselves, causal, 8 heads, d = 128, 324 us (106 TFLOP/s; a large library product 153).
 template <int D, int C>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_f32_kernel(PagedArgs a) {

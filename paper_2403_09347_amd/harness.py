@@ -373,18 +373,18 @@ class GraphedStep:
 class PagedWalk:
     """A cache in pages and what a step of serving does with it: the new tokens' keys and values are appended, rotated by their
     positions (turns: see rotary.rotary_turns; None: not rotated), and the new tokens attend to their sequences.  k_pages, v_pages, and
-    the table, lengths and starts of a step: see the paged module.  Nothing is kept but the pages: a captured step reads
+    the table, lengths and starts of a step, and full_p: see the paged module.  Nothing is kept but the pages: a captured step reads
     its token tensors and the three arrays where they lie, and can be replayed with other contents."""
 
-    def __init__(self, k_pages, v_pages, scale, turns=None, interleaved=False, amplitude=1.0, window=0):
-        self.k_pages, self.v_pages, self.scale, self.window = k_pages, v_pages, float(scale), int(window)
+    def __init__(self, k_pages, v_pages, scale, turns=None, interleaved=False, amplitude=1.0, window=0, full_p=False):
+        self.k_pages, self.v_pages, self.scale, self.window, self.full_p = k_pages, v_pages, float(scale), int(window), bool(full_p)
         self.rotary = {} if turns is None else dict(turns=turns, interleaved=interleaved, amplitude=amplitude)
 
     def step(self, q, k, v, table, lengths, starts, max_new=0):
         """q [rows, H, d], k, v [rows, kv_heads, d]; returns (O, lse) of the new tokens."""
         turned = burst_cache_append(k, v, self.k_pages, self.v_pages, table, lengths, starts, q=q if self.rotary else None, **self.rotary)
         return burst_paged_attention(q if turned is None else turned, self.k_pages, self.v_pages, table, lengths, starts, self.scale,
-                                     window=self.window, max_new=max_new)
+                                     window=self.window, max_new=max_new, full_p=self.full_p)
 
 
 class SpanWalk:

@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from paged_util import Batch, f64
+from paper_2403_09347_amd.harness import PagedWalk
 from paper_2403_09347_amd.paged import burst_paged_attention
 
 pytestmark = pytest.mark.gpu
@@ -42,6 +43,11 @@ def test_chunks_of_other_widths(d, L, window):
 def test_chunks_on_request(d, L, window, causal):
     b = Batch([L, 40], [40, 1], 8, 2, d, seed=d + L)
     assert error(b, window, causal, full_p=True) <= BAR
+    if causal:
+        walk = PagedWalk(b.k_pages, b.v_pages, b.scale, window=window, full_p=True)
+        O, lse = walk.step(b.q, b.k, b.v, b.table, b.lengths, b.starts)      # (the new tokens' keys are in the cache from here on)
+        want = burst_paged_attention(b.q, *b.args(), window=window, full_p=True)
+        assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
 
 
 @pytest.mark.parametrize("d", [128, 64])
