@@ -482,6 +482,9 @@ def burst_rotate(xs, ys, r, offsets=None, positions=None):
             raise ValueError("positions: int64 device tensor [B, rows] with contiguous rows expected")
         if x.shape != y.shape or x.dtype != y.dtype:
             raise ValueError("x, y: device tensors of the same sizes and type expected")
+        if not any(strides_of(x) or (1,)) or any(n > 1 and t == 0 for n, t in zip(y.shape, y.stride())):
+            # (strides of 0 throughout, as of one row that stands for all, mean dense ones in the block)
+            raise ValueError("x: not one row for all, y: a place for every row expected")
     items = (BurstRows * len(xs))()
     for x, y, at, offset, c in zip(xs, ys, positions, offsets, items):
         for t, what in ((x, "x"), (y, "y"), (at, "positions")):

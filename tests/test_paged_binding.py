@@ -19,6 +19,12 @@ def test_rotated_tensors_and_positions():
         y = x[:, :, :good.shape[1]]
         with pytest.raises(ValueError, match="device tensor"):
             B.burst_rotate([y], [y], R, positions=[good])
+    one = torch.zeros(1, 1, 1, 16).expand(2, 3, 5, 16)        # its strides are 0, which a block takes for dense ones
+    for a, b in ((one, x), (x, one), (x, x[:1].expand(2, 3, 5, 16)), (x, x[:, :1].expand(2, 3, 5, 16)), (x, x[:, :, :1].expand(2, 3, 5, 16))):
+        with pytest.raises(ValueError, match="not one row for all"):
+            B.burst_rotate([a], [b], R)
+    with pytest.raises(ValueError, match="device tensor"):    # heads that share rows are read as they are
+        B.burst_rotate([x[:, :1].expand(2, 3, 5, 16)], [x], R)
     for other in (torch.zeros(2, 3, 5, 8), x.to(BF16), x[0]):
         with pytest.raises(ValueError, match="of one type and d"):
             B.burst_rotate([x, other], [x, other], R)
