@@ -307,7 +307,7 @@ typedef struct burst_rotary {
 } burst_rotary;
 /* One tensor [B, heads, rows, d] and its rotated copy. */
 typedef struct burst_rows {
-  const void* x; void* y;            /* y: written; x itself (then with the same strides) or memory that x does not share */
+  const void* x; void* y;            /* y: written, every row in a place of its own; x itself (then with the same strides) or memory that x does not share */
   const int64_t* positions;          /* DEVICE: row n of batch entry b is at offset + positions[b * positions_stride + n]; NULL: offset + n */
   int64_t positions_stride, offset;
   int64_t x_strides[3], y_strides[3];/* element strides {batch, head, row}; all zero = contiguous */
@@ -340,7 +340,7 @@ typedef struct burst_paged_params {
   int64_t table_stride;              /* entries from one sequence's pages to the next's; 0 = width */
   int64_t page_strides[3];           /* elements {page, head, row} of K_pages and V_pages; all zero = dense [pages, kv_heads, page, d] */
   int64_t q_strides[2], kv_strides[2], o_strides[2];   /* elements {row, head} of Q; of K and V (new tokens); of O or Q_out; both zero = dense.
-                                      * Strides in multiples of 16 bytes (burst_cache_append: any), none negative */
+                                      * Strides in multiples of 16 bytes (burst_cache_append: any), none negative, none 0 between rows that are written */
 } burst_paged_params;
 /* Writes the new tokens' keys and values (K, V [rows, kv_heads, d]) to their places in K_pages and V_pages, the keys rotated by their
  * positions + offsets[s] (int64 DEVICE [sequences], NULL: 0; what the ring keeps before this device's share).  r = NULL: nothing is rotated.

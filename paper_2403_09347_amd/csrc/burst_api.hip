@@ -708,6 +708,8 @@ int check_paged(const burst_paged_params* p, Paged& g, bool attend) {
       !set_strides(g.o, p->o_strides, q, attend && p->out_f32 != 0 ? 4 : u) ||
       !set_strides(g.page, p->page_strides, page, u)) return BURST_ERR_SHAPE;
   if (g.page[2] < d || g.page[2] >= 1LL << 25) return BURST_ERR_SHAPE;
+  if ((p->rows > 1 && g.o[0] == 0) || (p->H > 1 && g.o[1] == 0)) return BURST_ERR_SHAPE;   // (written twice; pages are by appending)
+  if (!attend && ((p->pages > 1 && g.page[0] == 0) || (p->kv_heads > 1 && g.page[1] == 0))) return BURST_ERR_SHAPE;
   return BURST_OK;
 }
 // The kernel of a burst_paged_fwd call and its runs: as many as the chip holds at once, or as there can be units.
@@ -1175,6 +1177,7 @@ int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d,
     const long long dense[3] = {(long long)t.heads * t.rows * d, (long long)t.rows * d, d};
     long long xs[3], ys[3];
     if (!set_strides(xs, t.x_strides, dense, 1) || !set_strides(ys, t.y_strides, dense, 1)) return BURST_ERR_SHAPE;
+    if ((t.B > 1 && ys[0] == 0) || (t.heads > 1 && ys[1] == 0) || (t.rows > 1 && ys[2] == 0)) return BURST_ERR_SHAPE;   // (written twice)
     if (t.positions != nullptr && t.positions_stride < 0) return BURST_ERR_SHAPE;
     if (t.x == t.y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2])) return BURST_ERR_SHAPE;
     it.x = t.x; it.y = t.y;
@@ -1308,6 +1311,6 @@ const char* burst_strerror(int status) {
   }
 }
 
-int burst_version(void) { return 114; }
+int burst_version(void) { return 115; }
 
 }  // extern "C"

@@ -142,3 +142,12 @@ def test_sizes_of_rotated_tensors():
     for size in ("B", "heads", "rows"):
         for n in (0x7fffff01, 0x7fffffff):
             assert rotate(rows(**{size: n}), rotary()) == E_SHAPE, (size, n)
+
+
+def test_rows_that_would_be_written_to_one_place():
+    for size, strides in (("B", [0, 640, 64]), ("heads", [640, 0, 64]), ("rows", [640, 64, 0])):
+        assert rotate(rows(**dict(dict(B=1, heads=1, rows=1), **{size: 2}), y_strides=strides), rotary()) == E_SHAPE, size
+    for strides in ([0, 64], [256, 0]):
+        assert attend(paged(o_strides=strides)) == append(paged(o_strides=strides)) == E_SHAPE, strides
+    for strides in ([0, 1024, 64], [2048, 0, 64]):
+        assert append(paged(page_strides=strides)) == E_SHAPE, strides
