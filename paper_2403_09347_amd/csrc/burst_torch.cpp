@@ -355,6 +355,9 @@ struct RotateBackward : public torch::autograd::Node {
       if (!grads[i].defined() || !task_should_compute_output(i)) continue;
       to.push_back(i);
       some.push_back(grads[i].scalar_type() == type ? grads[i] : grads[i].to(type));
+      // (the engine gives gradients of the outputs' sizes; a caller of the node itself, what it likes)
+      TORCH_CHECK_VALUE(some.back().dim() == 4 && some.back().size(3) == some[0].size(3) && some.back().device() == some[0].device(),
+                        "gradients: [B, heads, rows, d] tensors of one d and device expected");
       back.position_of.push_back(how.position_of[i] >= 0 ? (int64_t)where.size() : -1);
       if (how.position_of[i] >= 0) where.push_back(positions_for(positions[how.position_of[i]].unpack(), some.back()));
       back.offsets.push_back(how.offsets[i]);

@@ -137,3 +137,15 @@ def test_gradients_that_nobody_asks_for_are_not_computed():
     dq2, dk = torch.autograd.grad([y, z], [q, k], [g, h])
     assert torch.equal(dq, dq2) and dk.shape == k.shape
     check_rotation("dk", dk, h, np.arange(8192)[None, None], f64(t), inverse=True)
+
+
+def test_the_node_by_itself_refuses_gradients_of_other_sizes():
+    x, z, t = rand(1, 2, 9, 16).requires_grad_(True), rand(1, 2, 9, 16).requires_grad_(True), default_turns(16)
+    y, _ = burst_rotary([x, z], t)
+    g = torch.ones_like(y)
+    dx, dz = y.grad_fn(g, g)
+    check_rotation("dx", dx, g, np.arange(9)[None, None], f64(t), inverse=True)
+    assert torch.equal(dx, dz)
+    for bad in ((g[0], g[0]), (g, torch.ones(1, 2, 9, 8, device=DEV)), (g, g.cpu()), (g.cpu(), g.cpu())):
+        with pytest.raises(ValueError):
+            y.grad_fn(*bad)
