@@ -149,3 +149,18 @@ def test_the_node_by_itself_refuses_gradients_of_other_sizes():
     for bad in ((g[0], g[0]), (g, torch.ones(1, 2, 9, 8, device=DEV)), (g, g.cpu()), (g.cpu(), g.cpu())):
         with pytest.raises(ValueError):
             y.grad_fn(*bad)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_of_rotated_rows_with_frozen_keys(dtype):
+    """The gradient of the queries is the same bits whether the keys and values need theirs or not, and the other way round."""
+    t = default_turns(64)
+    q, k, v, g = (rand(1, h, n, 64, dtype=dtype, seed=i) for i, (h, n) in enumerate(((4, 70), (2, 90), (2, 90), (4, 70))))
+    grads = []
+    for needs in ((True, True, True), (True, False, False), (False, True, False)):
+        x = [s.clone().requires_grad_(need) for s, need in zip((q, k, v), needs)]
+        O, _ = burst_attention(x[0], [x[1][:, :, :50], x[1][:, :, 50:]], [x[2][:, :, :50], x[2][:, :, 50:]], causal=True, q_off=20, turns=t)
+        O.backward(g)
+        grads.append([s.grad for s in x])
+    assert torch.equal(grads[0][0], grads[1][0]) and torch.equal(grads[0][1], grads[2][1])
+    assert grads[1][1] is None and grads[1][2] is None and grads[2][0] is None
