@@ -466,7 +466,9 @@ def rotary(turns, interleaved=False, amplitude=1.0, inverse=False):
     """turns: a contiguous float64 device tensor with an entry for every pair of columns (see burst.h)."""
     if turns.dtype != torch.float64:
         raise ValueError("turns: float64 tensor expected")
-    return BurstRotary(_ptr(turns), 2 * turns.numel(), 1 if interleaved else 0, amplitude, 1 if inverse else 0)
+    r = BurstRotary(_ptr(turns), 2 * turns.numel(), 1 if interleaved else 0, amplitude, 1 if inverse else 0)
+    r.holds = turns                                           # (the block has its address alone)
+    return r
 
 
 def burst_rotate(xs, ys, r, offsets=None, positions=None):
@@ -517,6 +519,7 @@ def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts,
                          out_f32=1 if out_f32 else 0, scale=scale, full_p=1 if full_p else 0, window=window, starts=starts.data_ptr(), lengths=lengths.data_ptr(),
                          table=table.data_ptr(), table_stride=table.stride(0) if table.shape[0] > 1 else 0)
     p.page_strides[:] = strides_of(k_pages) or (0, 0, 0)
+    p.holds = (starts, lengths, table)
     return p
 
 
@@ -564,7 +567,8 @@ def _offsets(t, p):
 def burst_cache_append(K, V, k_pages, v_pages, Q, Q_out, offsets, r, p):
     """Q, Q_out, offsets, r: None where there are none."""
     k, v = _tokens(K, p.kv_heads, p.kv_strides, p, "K"), _tokens(V, p.kv_heads, p.kv_strides, p, "V")
-    q, q_out = (None, None) if Q is None else (_tokens(Q, p.H, p.q_strides, p, "Q"), _tokens(Q_out, p.H, p.o_strides, p, "Q_out"))
+    q = None if Q is None else _tokens(Q, p.H, p.q_strides, p, "Q")
+    q_out = None if Q_out is None else _tokens(Q_out, p.H, p.o_strides, p, "Q_out")
     _check(load().burst_cache_append(k, v, _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"), q, q_out, _offsets(offsets, p),
                                      None if r is None else ctypes.byref(r), ctypes.byref(p), _stream()), "burst_cache_append")
 

@@ -121,3 +121,12 @@ def test_tensors_of_another_device(monkeypatch):
         B._here(Elsewhere(), "x")
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     B._here(Elsewhere(), "x")
+
+
+def test_blocks_keep_what_they_point_to(monkeypatch):
+    t = cache()
+    p = block(**t)
+    assert all(a is b for a, b in zip(p.holds, (t["starts"], t["lengths"], t["table"])))
+    monkeypatch.setattr(B, "_ptr", lambda t: t.data_ptr())
+    turns = torch.zeros(8, dtype=torch.float64)
+    assert B.rotary(turns).holds is turns
