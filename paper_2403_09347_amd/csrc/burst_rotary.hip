@@ -9,18 +9,6 @@
 
 namespace burst {
 
-// cos and sin of 2 pi x, in 64 bits: the nearest quarter turn taken off (exactly), and Taylor's series within pi/4 of it (terms up to x^12 and
-// x^11: the next ones are below 2^-41 and 2^-37).  Rounded to 32 bits by the caller, once.
-__device__ __forceinline__ void cos_sin_turns(double x, double& c, double& s) {
-  const double q = rint(4 * x);
-  const double t = (x - 0.25 * q) * 6.283185307179586, u = t * t;
-  const double cs = 1 + u * (-0.5 + u * (1. / 24 + u * (-1. / 720 + u * (1. / 40320 + u * (-1. / 3628800 + u * (1. / 479001600))))));
-  const double sn = t + t * u * (-1. / 6 + u * (1. / 120 + u * (-1. / 5040 + u * (1. / 362880 - u * (1. / 39916800)))));
-  const int n = (int)q & 3;
-  c = n == 0 ? cs : n == 1 ? -sn : n == 2 ? -cs : sn;
-  s = n == 0 ? sn : n == 1 ? cs : n == 2 ? -sn : -cs;
-}
-
 constexpr int kRowsThreads = 256;
 
 // Slots: the units of work of a row.  Half layout, VEC: 16 bytes of the first half of a pair's columns with the 16 bytes that
