@@ -318,6 +318,35 @@ typedef struct burst_rows {
  * (elements aligned to their own size); rows and column pairs on 16-byte boundaries are read and written 16 bytes at a time. */
 int burst_rotate(const burst_rows* tensors, int n, const burst_rotary* r, int d, int dtype, void* stream);
 
+/* Rows normalised by their root mean square, weighted and rotated, in one pass (models that normalise every head's queries and keys before the
+ * rotation): with r = (mean of x^2 over the d columns + eps)^(-1/2), y is the rotation (see burst_rotate) of x r w.  All of it in 32 bits (angles in
+ * 64), rounded once; sums of squares beyond 32 bits' range count as infinite. */
+typedef struct burst_norm_rows {
+  burst_rows rows;                   /* x and y.  burst_norm_rotate_bwd: x is the gradient of the result and y that of what it was made of, NULL: not wanted */
+  const void* from;                  /* burst_norm_rotate_bwd: what the forward call read */
+  int64_t from_strides[3];           /* as in burst_rows */
+  int32_t weight;                    /* which of the weights; -1: none (1 for every column) */
+  int32_t reserved;                  /* 0 */
+} burst_norm_rows;
+typedef struct burst_norm_weight {
+  const void* w;                     /* DEVICE [d], elements aligned to their own size */
+  void* dw;                          /* burst_norm_rotate_bwd: written, [d] of the type of w; NULL: not wanted */
+  int32_t f32;                       /* w and dw are fp32 whatever the dtype */
+  int32_t reserved;                  /* 0 */
+} burst_norm_weight;
+/* n tensors with `weights` weights, each of one tensor or of several; r = NULL: not rotated.  eps > 0.  y is x itself (then with the same strides)
+ * or memory that x does not share. */
+int burst_norm_rotate(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
+                      int dtype, void* stream);
+/* Gradients of all of them, those of a weight summed over every row of all its tensors (in fp32, in an order that follows from the sizes of the call; rounded
+ * once).  r as in the forward call (r->inverse = 0).  workspace: burst_norm_workspace_bytes of the same arguments, 16-byte aligned; none is needed where no
+ * weight's gradient is wanted. */
+int burst_norm_rotate_bwd(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
+                          int dtype, void* workspace, size_t workspace_bytes, void* stream);
+/* Follows from the sizes, strides and alignments of the tensors and from which gradients are wanted; 0 for invalid arguments.  Host logic, no device call. */
+size_t burst_norm_workspace_bytes(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
+                                  int dtype);
+
 /* The new tokens of several sequences and the pages of their caches.  New tokens lie packed, sequence after sequence:
  * sequence s has rows starts[s] .. starts[s + 1] - 1 of the token tensors, which are indexed [row, head, d].  lengths[s] counts
  * the tokens of the sequence, the new ones among them: new token t of n is at position lengths[s] - n + t, and position p
@@ -349,6 +378,21 @@ typedef struct burst_paged_params {
  * Pages that share a place, by equal table entries of two sequences say, must not both get a new token there. */
 int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_pages, const void* Q, void* Q_out,
                        const int64_t* offsets, const burst_rotary* r, const burst_paged_params* p, void* stream);
+/* burst_cache_append with more to say about the rows. */
+typedef struct burst_store {
+  const void* q_weight; const void* k_weight;   /* DEVICE [d]: Q, K are normalised first (see burst_norm_rotate); NULL: not */
+  int32_t q_weight_f32, k_weight_f32;           /* these weights are fp32 whatever the dtype */
+  float   eps;                                  /* of the norms, > 0 if there are any */
+  int32_t reserved;                             /* 0 */
+  const int64_t* slots;                         /* DEVICE [rows]: row i's key and value go to row slots[i] % page of page slots[i] / page, instead of by the
+                                                 * table; negative, or in a page that is none: left out */
+  const int64_t* positions;                     /* DEVICE [rows]: positions of the rotation, instead of the place in the sequence; negative: the row is left out */
+  const int64_t* offsets;                       /* as burst_cache_append's; NULL if there are positions */
+} burst_store;
+/* With both slots and positions nothing else is read of the batch (starts, lengths and table may be NULL); with one of them, rows that belong to no sequence
+ * are left out. */
+int burst_cache_store(const void* K, const void* V, void* K_pages, void* V_pages, const void* Q, void* Q_out,
+                      const burst_store* how, const burst_rotary* r, const burst_paged_params* p, void* stream);
 /* Attention of the new tokens over their sequences' pages: O [rows, H, d] of `dtype` (fp32 with out_f32) and lse [rows, H] fp32,
  * dense.  Tokens that see no key get O = 0 and lse = -inf; rows behind the last sequence are left as they were.  (O as fp32, lse, 1) is
  * a state that burst_merge_state takes: sequences whose cache is spread over a ring are put together so.

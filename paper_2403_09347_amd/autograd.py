@@ -5,11 +5,11 @@ chunks are simply all resident; in a ring the same calls are made once per recei
 import torch
 
 from . import binding as B
-from .rotary import burst_rotary
+from .rotary import burst_norm_rotary, burst_rotary
 
 
 def burst_attention(q, k_chunks, v_chunks, scale=None, causal=False, q_off=0, window=0, block_masks=None, block=0,
-                    turns=None, interleaved=False, amplitude=1.0):
+                    turns=None, interleaved=False, amplitude=1.0, norms=None, eps=1e-6):
     """q [B, H, Nq, d]; k_chunks / v_chunks: lists of [B, Hkv, Nc_j, d] (Hkv divides H), chunk j
     starting at global key position sum(Nc_0..Nc_{j-1}); q_off = global position of query row 0.
     Returns (O [B, H, Nq, d] in q's dtype and memory layout, lse [B, H, Nq] fp32).  Gradients flow
@@ -18,6 +18,8 @@ def burst_attention(q, k_chunks, v_chunks, scale=None, causal=False, q_off=0, wi
     block_masks: one uint8 device tensor of block flags per chunk (see binding.params) with blocks
     of `block` rows / keys, or None for a chunk without flags; or None.
     turns, interleaved, amplitude: q and the keys are rotated by their global positions first (see rotary.burst_rotary).
+    norms, eps: a pair of weights [d], q's and the keys': their rows are normalised before that (see rotary.burst_norm_rotary); gradients
+    flow to the weights.
     Results are the same bits whenever a call is repeated; the order of the fp32 sums, and with it the last bits, depends on all
     sizes of a call, the number of heads among them.
     The node saves its inputs, O and lse as torch's own operations do: a tensor changed in place before the backward is
@@ -26,7 +28,11 @@ def burst_attention(q, k_chunks, v_chunks, scale=None, causal=False, q_off=0, wi
         k_chunks, v_chunks = [k_chunks], [v_chunks]
     assert len(k_chunks) == len(v_chunks) and len(k_chunks) > 0
     scale = float(scale) if scale is not None else q.shape[-1] ** -0.5
-    if turns is not None:
+    if norms is not None:
+        firsts = [sum(k.shape[2] for k in k_chunks[:j]) for j in range(len(k_chunks))]
+        q, *k_chunks = burst_norm_rotary([q, *k_chunks], [norms[0]] + [norms[1]] * len(k_chunks), turns, eps, [int(q_off)] + firsts, None, interleaved,
+                                         amplitude)
+    elif turns is not None:
         firsts = [sum(k.shape[2] for k in k_chunks[:j]) for j in range(len(k_chunks))]
         q, *k_chunks = burst_rotary([q, *k_chunks], turns, [int(q_off)] + firsts, None, interleaved, amplitude)
     if block_masks is not None:

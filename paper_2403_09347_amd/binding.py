@@ -24,7 +24,7 @@ EXPORTS = [
     "burst_materialized_bwd_workspace_bytes", "burst_local_bwd_materialized", "burst_set_kernel_family",
     "burst_kernel_family_for", "burst_local_bwd_static", "burst_probe_mfma", "burst_probe_atomic_dq",
     "burst_walk_fwd", "burst_walk_bwd", "burst_walk_workspace_bytes", "burst_walk_dkv_form",
-    "burst_rotate", "burst_cache_append", "burst_paged_fwd", "burst_paged_workspace_bytes",
+    "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_norm_workspace_bytes", "burst_cache_append", "burst_cache_store", "burst_paged_fwd", "burst_paged_workspace_bytes",
 ]
 
 
@@ -57,6 +57,21 @@ class BurstRows(ctypes.Structure):
                 ("positions_stride", ctypes.c_int64), ("offset", ctypes.c_int64),
                 ("x_strides", ctypes.c_int64 * 3), ("y_strides", ctypes.c_int64 * 3),
                 ("B", ctypes.c_int32), ("heads", ctypes.c_int32), ("rows", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class BurstNormRows(ctypes.Structure):
+    _fields_ = [("rows", BurstRows), ("from_", ctypes.c_void_p), ("from_strides", ctypes.c_int64 * 3), ("weight", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class BurstNormWeight(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("f32", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class BurstStore(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("q_weight_f32", ctypes.c_int32), ("k_weight_f32", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
 
 
 class BurstPagedParams(ctypes.Structure):
@@ -158,7 +173,13 @@ def load():
     lib.burst_rotate.argtypes = [ctypes.POINTER(BurstRows), ci, rp, ci, ci, vp]
     lib.burst_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, rp, gp, vp]
     lib.burst_paged_fwd.argtypes = [vp, vp, vp, vp, fp, vp, sz, gp, vp]
-    for name in ("burst_rotate", "burst_cache_append", "burst_paged_fwd"):
+    np_, wp = ctypes.POINTER(BurstNormRows), ctypes.POINTER(BurstNormWeight)
+    lib.burst_norm_rotate.argtypes = [np_, ci, wp, ci, ctypes.c_float, rp, ci, ci, vp]
+    lib.burst_norm_rotate_bwd.argtypes = [np_, ci, wp, ci, ctypes.c_float, rp, ci, ci, vp, sz, vp]
+    lib.burst_norm_workspace_bytes.argtypes = [np_, ci, wp, ci, ctypes.c_float, rp, ci, ci]
+    lib.burst_norm_workspace_bytes.restype = sz
+    lib.burst_cache_store.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(BurstStore), rp, gp, vp]
+    for name in ("burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_cache_append", "burst_cache_store", "burst_paged_fwd"):
         getattr(lib, name).restype = ci
     lib.burst_paged_workspace_bytes.argtypes = [gp]
     lib.burst_paged_workspace_bytes.restype = sz
@@ -500,6 +521,66 @@ def burst_rotate(xs, ys, r, offsets=None, positions=None):
     _check(load().burst_rotate(items, len(xs), ctypes.byref(r), xs[0].shape[3] if len(xs) else 2, dtype, _stream()), "burst_rotate")
 
 
+def _norm_call(tensors, weights, r):
+    """The C arrays of a call that normalises rows.  tensors: (x, y, from or None, place of its weight or -1, offset, positions or None) for each; weights:
+    (w, dw or None) for each."""
+    items, ws = (BurstNormRows * len(tensors))(), (BurstNormWeight * len(weights))()
+    like = tensors[0][0] if tensors else None
+    if like is not None and (like.dtype not in _TYPES.values() or like.dim() != 4):
+        raise ValueError("[B, heads, rows, d] tensors of bfloat16 or float32 expected")
+    for c, (x, y, frm, weight, offset, at) in zip(items, tensors):
+        for t, what in ((x, "x"), (y, "y"), (frm, "from")):
+            if t is None:
+                continue
+            if t.shape != x.shape or t.dtype != like.dtype or t.dim() != 4 or t.shape[3] != like.shape[3]:
+                raise ValueError(f"{what}: a tensor [B, heads, rows, d] of the sizes of x, of one type and d, expected")
+            if not any(strides_of(t) or (1,)) or (t is y and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride()))):
+                raise ValueError(f"{what}: not one row for all expected")   # (strides of 0 throughout mean dense ones in the block)
+            _here(t, what)
+        if at is not None:
+            if at.dtype != torch.int64 or tuple(at.shape) != (x.shape[0], x.shape[2]) or (at.shape[1] > 1 and at.stride(1) != 1):
+                raise ValueError("positions: int64 device tensor [B, rows] with contiguous rows expected")
+            _here(at, "positions")
+            c.rows.positions, c.rows.positions_stride = at.data_ptr(), at.stride(0)
+        c.rows.x, c.rows.B, c.rows.heads, c.rows.rows, c.rows.offset = x.data_ptr(), x.shape[0], x.shape[1], x.shape[2], offset
+        c.rows.x_strides[:] = strides_of(x) or (0, 0, 0)
+        if y is not None:
+            c.rows.y, c.rows.y_strides[:] = y.data_ptr(), strides_of(y) or (0, 0, 0)
+        if frm is not None:
+            c.from_, c.from_strides[:] = frm.data_ptr(), strides_of(frm) or (0, 0, 0)
+        c.weight = weight
+    for c, (w, dw) in zip(ws, weights):
+        for t, what in ((w, "w"), (dw, "dw")):
+            if t is None:
+                continue
+            if t.dtype != w.dtype or (like is not None and (t.dtype not in (like.dtype, torch.float32) or t.numel() != like.shape[3])) or not t.is_contiguous():
+                raise ValueError(f"{what}: contiguous [d] of the tensors' type or float32 expected")
+            _here(t, what)
+        c.w, c.dw, c.f32 = w.data_ptr(), None if dw is None else dw.data_ptr(), 1 if w.dtype == torch.float32 else 0
+    dtype = BURST_BF16 if like is None or like.dtype == torch.bfloat16 else BURST_F32
+    return items, len(tensors), ws, len(weights), None if r is None else ctypes.byref(r), like.shape[3] if like is not None else 2, dtype
+
+
+def burst_norm_rotate(tensors, weights, eps, r):
+    """tensors: (x, y, None, place of its weight or -1, offset, positions or None) for each; weights: (w, None) for each; r: see rotary, or None."""
+    items, n, ws, k, rp, d, dtype = _norm_call(tensors, weights, r)
+    _check(load().burst_norm_rotate(items, n, ws, k, eps, rp, d, dtype, _stream()), "burst_norm_rotate")
+
+
+def burst_norm_workspace_bytes(tensors, weights, eps, r):
+    items, n, ws, k, rp, d, dtype = _norm_call(tensors, weights, r)
+    return int(load().burst_norm_workspace_bytes(items, n, ws, k, eps, rp, d, dtype))
+
+
+def burst_norm_rotate_bwd(tensors, weights, eps, r, workspace=None):
+    """tensors: (gradient of the result, gradient of x or None, x, place of its weight or -1, offset, positions or None) for each; weights: (w, dw or
+    None) for each."""
+    if any(t[2] is None for t in tensors):
+        raise ValueError("from: what the forward call read expected")
+    items, n, ws, k, rp, d, dtype = _norm_call(tensors, weights, r)
+    _check(load().burst_norm_rotate_bwd(items, n, ws, k, eps, rp, d, dtype, _ptr(workspace), _bytes(workspace), _stream()), "burst_norm_rotate_bwd")
+
+
 def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts, scale=1.0, causal=True, window=0, max_new=0, out_f32=False, full_p=False):
     """k_pages: [pages, kv_heads, page, d] (its strides go into the block; V_pages lies likewise); table [sequences, width], lengths
     [sequences], starts [sequences + 1]: int32 device tensors.  Token tensors are dense unless their strides are set in the block."""
@@ -571,6 +652,37 @@ def burst_cache_append(K, V, k_pages, v_pages, Q, Q_out, offsets, r, p):
     q_out = None if Q_out is None else _tokens(Q_out, p.H, p.o_strides, p, "Q_out")
     _check(load().burst_cache_append(k, v, _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"), q, q_out, _offsets(offsets, p),
                                      None if r is None else ctypes.byref(r), ctypes.byref(p), _stream()), "burst_cache_append")
+
+
+def store(p, q_weight=None, k_weight=None, eps=1e-6, slots=None, positions=None, offsets=None):
+    """What burst_cache_store is told beside the parameter block: weights [d] of its type or float32, slots and positions int64 [rows]."""
+    s = BurstStore(eps=eps)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if w.dtype not in (_TYPES.get(p.dtype), torch.float32) or tuple(w.shape) != (p.d,) or not w.is_contiguous():
+            raise ValueError(f"{name}: contiguous [d] of the block's type or float32 expected")
+        _here(w, name)
+        setattr(s, name, w.data_ptr())
+        setattr(s, name + "_f32", 1 if w.dtype == torch.float32 else 0)
+    for name, t, n in (("slots", slots, p.rows), ("positions", positions, p.rows), ("offsets", offsets, p.sequences)):
+        if t is None:
+            continue
+        if t.dtype != torch.int64 or tuple(t.shape) != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: contiguous int64 device tensor [{n}] expected")
+        _here(t, name)
+        setattr(s, name, t.data_ptr())
+    s.holds = (q_weight, k_weight, slots, positions, offsets)
+    return s
+
+
+def burst_cache_store(K, V, k_pages, v_pages, Q, Q_out, how, r, p):
+    """how: see store.  Q, Q_out, r: None where there are none."""
+    k, v = _tokens(K, p.kv_heads, p.kv_strides, p, "K"), _tokens(V, p.kv_heads, p.kv_strides, p, "V")
+    q = None if Q is None else _tokens(Q, p.H, p.q_strides, p, "Q")
+    q_out = None if Q_out is None else _tokens(Q_out, p.H, p.o_strides, p, "Q_out")
+    _check(load().burst_cache_store(k, v, _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"), q, q_out, ctypes.byref(how),
+                                    None if r is None else ctypes.byref(r), ctypes.byref(p), _stream()), "burst_cache_store")
 
 
 def burst_paged_workspace_bytes(p):

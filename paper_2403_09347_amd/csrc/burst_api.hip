@@ -8,6 +8,7 @@
 #include <mutex>
 #include <vector>
 #include "burst_common.h"
+#include "burst_norm.h"
 #include "burst_paged_kernels.h"
 #include "burst_rotary.h"
 
@@ -778,6 +779,114 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
   return BURST_OK;
 }
 
+// ---- rows normalised and rotated
+// One item of a call that normalises rows, checked.  `some`: it has rows.
+int norm_item(const burst_norm_rows& t, const burst_norm_weight* w, int weights, const burst_rotary* r, int d, unsigned size, bool backward,
+              burst::NormItem& it, bool& some) {
+  it = burst::NormItem{};
+  for (const int32_t n : {t.rows.B, t.rows.heads, t.rows.rows})
+    if (n < 0 || n > burst::kMaxRotateSize) return BURST_ERR_SHAPE;
+  if (t.weight < -1 || t.weight >= weights) return BURST_ERR_SHAPE;
+  some = t.rows.B > 0 && t.rows.heads > 0 && t.rows.rows > 0;
+  if (!some) return BURST_OK;
+  const burst_rows& x = t.rows;
+  REQUIRE_ALIGNED(x.x, size);
+  if (!backward || x.y != nullptr) REQUIRE_ALIGNED(x.y, size);
+  if (backward) REQUIRE_ALIGNED(t.from, size);
+  if ((reinterpret_cast<uintptr_t>(x.positions) & 7u) != 0) return BURST_ERR_ALIGN;
+  const long long dense[3] = {(long long)x.heads * x.rows * d, (long long)x.rows * d, d};
+  long long xs[3], ys[3], fs[3];
+  if (!set_strides(xs, x.x_strides, dense, 1) || !set_strides(ys, x.y_strides, dense, 1) || !set_strides(fs, t.from_strides, dense, 1)) return BURST_ERR_SHAPE;
+  if (x.y != nullptr && ((x.B > 1 && ys[0] == 0) || (x.heads > 1 && ys[1] == 0) || (x.rows > 1 && ys[2] == 0))) return BURST_ERR_SHAPE;   // (written twice)
+  if (x.positions != nullptr && x.positions_stride < 0) return BURST_ERR_SHAPE;
+  auto differ = [&](const long long (&a)[3], const long long (&b)[3]) { return a[0] != b[0] || a[1] != b[1] || a[2] != b[2]; };
+  if (x.y != nullptr && ((x.x == x.y && differ(xs, ys)) || (backward && t.from == x.y && differ(fs, ys)))) return BURST_ERR_SHAPE;
+  it.x = backward ? t.from : x.x; it.y = x.y; it.g = backward ? x.x : nullptr;
+  if (t.weight >= 0) { it.w = w[t.weight].w; it.w_f32 = w[t.weight].f32 != 0; }
+  it.positions = (const long long*)x.positions; it.positions_stride = x.positions_stride; it.offset = x.offset;
+  const long long (&from)[3] = backward ? fs : xs;
+  it.xs_b = from[0]; it.xs_h = from[1]; it.xs_r = from[2]; it.ys_b = ys[0]; it.ys_h = ys[1]; it.ys_r = ys[2];
+  if (backward) { it.gs_b = xs[0]; it.gs_h = xs[1]; it.gs_r = xs[2]; }
+  it.B = x.B; it.heads = x.heads; it.rows = x.rows; it.normed = 1; it.rotated = r != nullptr; it.part = -1;
+  return BURST_OK;
+}
+// A call's launches, laid out; backward: the rows of partial sums of every weight whose gradient is wanted, one after the other.
+struct NormPlan {
+  struct Launch { burst::NormArgs a; long long blocks; };
+  std::vector<Launch> launches;
+  std::vector<burst::NormSum> sums;
+  long long parts = 0;
+};
+int plan_norm(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d, int dtype,
+              bool backward, NormPlan& plan) {
+  if (n < 0 || weights < 0 || d < 2 || d > 128 || !(eps > 0.f) || !std::isfinite(eps)) return BURST_ERR_SHAPE;
+  if (dtype != BURST_BF16 && dtype != BURST_F32) return BURST_ERR_DTYPE;
+  int st;
+  if (r != nullptr && (st = check_rotary(r, d)) != BURST_OK) return st;
+  if (r != nullptr && r->inverse != 0) return BURST_ERR_SHAPE;
+  if ((n > 0 && tensors == nullptr) || (weights > 0 && w == nullptr)) return BURST_ERR_NULL;
+  const unsigned size = dtype == BURST_BF16 ? 2 : 4;
+  for (int k = 0; k < weights; k++) {
+    const unsigned each = w[k].f32 != 0 ? 4 : size;
+    REQUIRE_ALIGNED(w[k].w, each);
+    if (backward && w[k].dw != nullptr) REQUIRE_ALIGNED(w[k].dw, each);
+  }
+  std::vector<int> weight_of;
+  for (int i = 0; i < n; i++) {
+    burst::NormItem it;
+    bool some = false;
+    if ((st = norm_item(tensors[i], w, weights, r, d, size, backward, it, some)) != BURST_OK) return st;
+    const int k = tensors[i].weight;
+    const bool summed = backward && k >= 0 && w[k].dw != nullptr;
+    if (!some || (backward && it.y == nullptr && !summed)) continue;
+    if (plan.launches.empty() || plan.launches.back().a.n == burst::kMaxNormItems) {
+      plan.launches.emplace_back();
+      burst::NormArgs& a = plan.launches.back().a;
+      a = burst::NormArgs{};
+      a.d = d; a.eps = eps;
+      if (r != nullptr) { a.turns = r->turns; a.dims = r->dims; a.interleaved = r->interleaved != 0; a.amplitude = r->amplitude; }
+    }
+    burst::NormArgs& a = plan.launches.back().a;
+    a.it[a.n++] = it;
+    weight_of.push_back(summed ? k : -1);
+  }
+  for (NormPlan::Launch& l : plan.launches)
+    if ((l.blocks = burst::set_tiles(l.a, dtype, backward)) < 0) return BURST_ERR_SHAPE;
+  if (!backward) return BURST_OK;
+  for (int k = 0; k < weights; k++) {
+    if (w[k].dw == nullptr) continue;
+    const long long first = plan.parts;
+    size_t i = 0;
+    for (NormPlan::Launch& l : plan.launches)
+      for (int j = 0; j < l.a.n; j++) {
+        if (weight_of[i++] != k) continue;
+        l.a.it[j].part = (int)plan.parts;
+        plan.parts += (j + 1 < l.a.n ? l.a.it[j + 1].first_block : l.blocks) - l.a.it[j].first_block;
+        if (plan.parts > 0x7fffffff) return BURST_ERR_SHAPE;
+      }
+    plan.sums.push_back(burst::NormSum{w[k].dw, (int)first, (int)(plan.parts - first), w[k].f32 != 0 || dtype == BURST_F32});
+  }
+  return BURST_OK;
+}
+int run_norm(NormPlan& plan, int d, int dtype, bool backward, void* workspace, hipStream_t s) {
+  return validated([&] {
+    for (NormPlan::Launch& l : plan.launches) {
+      l.a.part = (float*)workspace;
+      const int e = backward ? burst::launch_norm_bwd(l.a, dtype, l.blocks, s) : burst::launch_norm(l.a, dtype, l.blocks, s);
+      if (e != BURST_OK) return e;
+    }
+    for (size_t i = 0; i < plan.sums.size(); i += burst::kMaxNormWeights) {
+      burst::NormSums a = {};
+      const int n = (int)std::min<size_t>(burst::kMaxNormWeights, plan.sums.size() - i);
+      std::copy(plan.sums.begin() + i, plan.sums.begin() + i + n, a.s);
+      a.part = (const float*)workspace; a.d = d;
+      const int e = burst::launch_norm_sums(a, n, s);
+      if (e != BURST_OK) return e;
+    }
+    return (int)BURST_OK;
+  });
+}
+
 }  // namespace
 
 extern "C" {
@@ -1243,6 +1352,95 @@ int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_page
   return burst::launch_rotate(a, p->dtype, (hipStream_t)stream);
 }
 
+int burst_norm_rotate(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
+                      int dtype, void* stream) {
+  try {
+    NormPlan plan;
+    int st = plan_norm(tensors, n, w, weights, eps, r, d, dtype, false, plan);
+    if (st != BURST_OK || plan.launches.empty()) return st;
+    if ((st = check_arch()) != BURST_OK) return st;
+    return run_norm(plan, d, dtype, false, nullptr, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return BURST_ERR_ALLOC;
+  }
+}
+
+size_t burst_norm_workspace_bytes(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
+                                  int dtype) {
+  try {
+    NormPlan plan;
+    if (plan_norm(tensors, n, w, weights, eps, r, d, dtype, true, plan) != BURST_OK) return 0;
+    return (size_t)plan.parts * d * sizeof(float);
+  } catch (const std::bad_alloc&) {
+    return 0;
+  }
+}
+
+int burst_norm_rotate_bwd(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
+                          int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    NormPlan plan;
+    int st = plan_norm(tensors, n, w, weights, eps, r, d, dtype, true, plan);
+    if (st != BURST_OK || (plan.launches.empty() && plan.sums.empty())) return st;
+    if (plan.parts > 0) {
+      REQUIRE_PTR(workspace);
+      if (workspace_bytes < (size_t)plan.parts * d * sizeof(float)) return BURST_ERR_SHAPE;
+    }
+    if ((st = check_arch()) != BURST_OK) return st;
+    return run_norm(plan, d, dtype, true, workspace, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return BURST_ERR_ALLOC;
+  }
+}
+
+int burst_cache_store(const void* K, const void* V, void* K_pages, void* V_pages, const void* Q, void* Q_out,
+                      const burst_store* how, const burst_rotary* r, const burst_paged_params* p, void* stream) {
+  Paged g;
+  int st = check_paged(p, g, false);
+  if (st != BURST_OK) return st;
+  if (how == nullptr) return BURST_ERR_NULL;
+  if (r != nullptr && (st = check_rotary(r, p->d)) != BURST_OK) return st;
+  if (r != nullptr && r->inverse != 0) return BURST_ERR_SHAPE;
+  const bool norms = how->q_weight != nullptr || how->k_weight != nullptr;
+  if (norms && (!(how->eps > 0.f) || !std::isfinite(how->eps))) return BURST_ERR_SHAPE;
+  if (how->positions != nullptr && how->offsets != nullptr) return BURST_ERR_SHAPE;
+  const bool told = how->slots != nullptr && how->positions != nullptr;   // the rows' places, all of them
+  if (p->rows == 0 || (p->sequences == 0 && !told)) return BURST_OK;
+  const unsigned size = p->dtype == BURST_BF16 ? 2 : 4;
+  REQUIRE_ALIGNED(K, size); REQUIRE_ALIGNED(V, size);
+  if (p->pages > 0) { REQUIRE_ALIGNED(K_pages, size); REQUIRE_ALIGNED(V_pages, size); }
+  if (!told) {
+    REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4);
+    if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
+  }
+  if (Q != nullptr) { REQUIRE_ALIGNED(Q, size); REQUIRE_ALIGNED(Q_out, size); }
+  for (const int64_t* at : {how->slots, how->positions, how->offsets})
+    if ((reinterpret_cast<uintptr_t>(at) & 7u) != 0) return BURST_ERR_ALIGN;
+  if (how->q_weight != nullptr) REQUIRE_ALIGNED(how->q_weight, how->q_weight_f32 != 0 ? 4 : size);
+  if (how->k_weight != nullptr) REQUIRE_ALIGNED(how->k_weight, how->k_weight_f32 != 0 ? 4 : size);
+  if (Q != nullptr && Q == Q_out && (g.q[0] != g.o[0] || g.q[1] != g.o[1])) return BURST_ERR_SHAPE;
+  if ((st = check_arch()) != BURST_OK) return st;
+  burst::NormArgs a = {};
+  a.d = p->d; a.eps = how->eps;
+  if (r != nullptr) { a.turns = r->turns; a.dims = r->dims; a.interleaved = r->interleaved != 0; a.amplitude = r->amplitude; }
+  a.cached = 1;
+  a.slots = (const long long*)how->slots; a.places = (const long long*)how->positions; a.offsets = (const long long*)how->offsets;
+  a.starts = p->starts; a.lengths = p->lengths; a.table = p->table; a.table_stride = g.table_stride;
+  a.sequences = p->sequences; a.tokens = p->rows; a.cap = p->width * p->page; a.pages = p->pages; a.page_shift = g.page_shift;
+  auto add = [&](const void* x, void* y, const long long (&xs)[2], int heads, const void* w, int f32, int rotated, int paged) {
+    burst::NormItem& it = a.it[a.n++];
+    it.x = x; it.y = y; it.xs_r = xs[0]; it.xs_h = xs[1]; it.w = w; it.w_f32 = f32 != 0; it.normed = w != nullptr;
+    if (paged) { it.ys_b = g.page[0]; it.ys_h = g.page[1]; it.ys_r = g.page[2]; }
+    else { it.ys_r = g.o[0]; it.ys_h = g.o[1]; }
+    it.B = 1; it.heads = heads; it.rows = p->rows; it.rotated = rotated; it.paged = paged; it.part = -1;
+  };
+  if (Q != nullptr) add(Q, Q_out, g.q, p->H, how->q_weight, how->q_weight_f32, r != nullptr, 0);
+  add(K, K_pages, g.kv, p->kv_heads, how->k_weight, how->k_weight_f32, r != nullptr, 1);
+  add(V, V_pages, g.kv, p->kv_heads, nullptr, 0, 0, 1);
+  const long long blocks = burst::set_tiles(a, p->dtype, false);
+  return blocks < 0 ? (int)BURST_ERR_SHAPE : burst::launch_norm(a, p->dtype, blocks, (hipStream_t)stream);
+}
+
 size_t burst_paged_workspace_bytes(const burst_paged_params* p) {
   Paged g;
   if (check_paged(p, g, true) != BURST_OK) return 0;
@@ -1311,6 +1509,6 @@ const char* burst_strerror(int status) {
   }
 }
 
-int burst_version(void) { return 115; }
+int burst_version(void) { return 116; }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// The torch calls of the package: rotary.burst_rotary and its gradient, paged's two calls, RingWalk's usual calls, and
+// The torch calls of the package: rotary.burst_rotary and burst_norm_rotary with their gradients, paged's calls, RingWalk's usual calls, and
 // the differentiable call behind autograd.burst_attention: attention of a query slice against key/value
 // chunks as one torch autograd node, in C++.  Argument marshalling and buffers only; every arithmetic
 // step is a call into libburst.so (paper Alg. 1 forward, Alg. 2 backward).
@@ -8,6 +8,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
 
 #include <cmath>
@@ -423,6 +424,213 @@ std::vector<Tensor> rotate(const std::vector<Tensor>& xs, const Tensor& turns, c
   return rotate_differentiably(xs, turns, at, how);
 }
 
+// ---- rotary.burst_norm_rotary: tensors normalised, weighted and rotated by one call, and all gradients by another.
+struct Norming {
+  std::vector<int64_t> weight_of, position_of, offsets;   // for each tensor: the place of its weight and of its positions, -1 = none
+  bool rotated, interleaved;
+  double amplitude, eps;
+};
+struct NormCall {                                  // what both of its calls take, and the tensors that it points into
+  std::vector<burst_norm_rows> items;
+  std::vector<burst_norm_weight> weights;
+  variable_list holds;
+  burst_rotary r{};
+  const burst_rotary* rotary = nullptr;
+  int d = 0, dtype = 0;
+};
+void set_rows(burst_rows& c, const Tensor& x, const Tensor& y, const Tensor* positions, int64_t offset) {
+  c.x = x.data_ptr();
+  set_strides(c.x_strides, x);
+  c.B = (int32_t)x.size(0); c.heads = (int32_t)x.size(1); c.rows = (int32_t)x.size(2);
+  if (y.defined()) {
+    c.y = y.data_ptr();
+    set_strides(c.y_strides, y);
+  }
+  c.offset = offset;
+  if (positions != nullptr) {
+    c.positions = positions->data_ptr<int64_t>();
+    c.positions_stride = positions->dim() == 2 && positions->size(0) > 1 ? positions->stride(0) : 0;
+  }
+}
+Tensor result_like(const Tensor& x) {              // lies in memory like x, without its gaps
+  Tensor y = torch::empty_like(x);
+  return y.stride(3) == 1 ? y : torch::empty(x.sizes(), x.options());   // (x has rows or heads one element apart: windows of a sequence)
+}
+void set_norm(NormCall& c, const Tensor& like, const variable_list& weights, const Tensor& turns, const Norming& how) {
+  c.d = (int)like.size(3);
+  c.dtype = like.scalar_type() == torch::kBFloat16 ? BURST_BF16 : BURST_F32;
+  for (const Tensor& w : weights) {
+    burst_norm_weight b{};
+    b.w = w.data_ptr();
+    b.f32 = w.scalar_type() == torch::kFloat;
+    c.weights.push_back(b);
+  }
+  if (how.rotated) {
+    c.r.turns = turns.data_ptr<double>(); c.r.dims = (int32_t)(2 * turns.numel()); c.r.interleaved = how.interleaved; c.r.amplitude = (float)how.amplitude;
+    c.rotary = &c.r;
+  }
+}
+void check_weight(const Tensor& w, const Tensor& like) {
+  TORCH_CHECK_VALUE(w.dim() == 1 && w.size(0) == like.size(3) && w.device() == like.device() && (w.scalar_type() == like.scalar_type() || w.scalar_type() == torch::kFloat),
+                    "weights: [d] on the tensors' device, of their type or float32, expected");
+  refuse_tangent(w);
+}
+struct NormRotaryBackward : public torch::autograd::Node {
+  std::vector<torch::autograd::SavedVariable> xs, weights, positions;
+  torch::autograd::SavedVariable turns;
+  Norming how;
+  at::ScalarType type;
+  variable_list apply(variable_list&& grads) override {
+    const std::lock_guard<std::mutex> lock(mutex_);   // (threads that go back through one graph: another one's release_variables)
+    const size_t n = xs.size();
+    variable_list out(n + weights.size()), x(n), g(n), at(positions.size()), w;
+    const Tensor* like = nullptr;
+    for (size_t i = 0; i < n; i++) {
+      if (!grads[i].defined()) continue;
+      const int64_t k = how.weight_of[i];
+      if (!task_should_compute_output(i) && !(k >= 0 && task_should_compute_output(n + k))) continue;
+      x[i] = xs[i].unpack();
+      g[i] = grads[i].scalar_type() == type ? grads[i] : grads[i].to(type);
+      // (the engine gives gradients of the outputs' sizes; a caller of the node itself, what it likes.  So do hooks on saved tensors.)
+      TORCH_CHECK_VALUE(x[i].dim() == 4 && x[i].scalar_type() == type && g[i].sizes() == x[i].sizes() && g[i].device() == x[i].device(),
+                        "gradients and saved tensors: of the sizes and device of the call's tensors expected");
+      if (like == nullptr) like = &x[i];
+      TORCH_CHECK_VALUE(x[i].device() == like->device() && x[i].size(3) == like->size(3), "gradients and saved tensors: of one d and device expected");
+    }
+    if (like == nullptr) return out;
+    const c10::DeviceGuard on(like->device());
+    Tensor t;
+    variable_list given(x);                        // (as they are part of a graph)
+    given.insert(given.end(), g.begin(), g.end());
+    {
+      const at::NoGradGuard no_grad;
+      for (auto& s : weights) {
+        w.push_back(s.unpack().contiguous());
+        check_weight(w.back(), *like);
+        given.push_back(w.back());
+      }
+      if (how.rotated) {
+        t = turns.unpack().contiguous();
+        check_turns(t, like->size(3), *like);
+      }
+      NormCall c;
+      set_norm(c, *like, w, t, how);
+      std::vector<bool> fed(weights.size(), false);
+      for (size_t i = 0; i < n; i++) {
+        if (!g[i].defined()) continue;
+        const Tensor from = rows_in_place(x[i]) ? x[i].detach() : x[i].contiguous(), grad = rows_in_place(g[i]) ? g[i].detach() : g[i].contiguous();
+        Tensor p;
+        if (how.position_of[i] >= 0) p = positions_for(positions[how.position_of[i]].unpack(), from);
+        if (task_should_compute_output(i)) out[i] = result_like(from);
+        burst_norm_rows b{};
+        set_rows(b.rows, grad, out[i], p.defined() ? &p : nullptr, how.offsets[i]);
+        b.from = from.data_ptr();
+        set_strides(b.from_strides, from);
+        b.weight = (int32_t)how.weight_of[i];
+        if (b.weight >= 0) fed[b.weight] = true;
+        c.items.push_back(b);
+        c.holds.insert(c.holds.end(), {from, grad, p});
+      }
+      for (size_t k = 0; k < weights.size(); k++) {
+        if (!fed[k] || !task_should_compute_output(n + k)) continue;
+        out[n + k] = torch::empty(w[k].sizes(), w[k].options());
+        c.weights[k].dw = out[n + k].data_ptr();
+      }
+      const size_t need = burst_norm_workspace_bytes(c.items.data(), (int)c.items.size(), c.weights.data(), (int)c.weights.size(), (float)how.eps, c.rotary, c.d, c.dtype);
+      const Tensor ws = need ? torch::empty({(int64_t)need}, like->options().dtype(torch::kByte)) : Tensor();
+      check(burst_norm_rotate_bwd(c.items.data(), (int)c.items.size(), c.weights.data(), (int)c.weights.size(), (float)how.eps, c.rotary, c.d, c.dtype, ptr(ws),
+                                  bytes(ws), stream_of(*like)), "burst_norm_rotate_bwd");
+    }
+    if (at::GradMode::is_enabled()) {              // (create_graph: these gradients are right, theirs are not implemented)
+      variable_list some;
+      for (const Tensor& v : given) if (v.defined()) some.push_back(v);
+      const auto end = std::make_shared<torch::autograd::Error>("burst_norm_rotary: gradients of its gradients are not implemented",
+                                                                torch::autograd::collect_next_edges(some));
+      for (Tensor& v : out) if (v.defined()) torch::autograd::set_history(v, end);
+    }
+    return out;
+  }
+  void release_variables() override {
+    const std::lock_guard<std::mutex> lock(mutex_);
+    turns.reset_data();
+    for (auto* l : {&xs, &weights, &positions})
+      for (auto& v : *l) v.reset_data();
+  }
+  std::string name() const override { return "BurstNormRotaryBackward"; }
+};
+std::vector<Tensor> norm_rotate(const std::vector<Tensor>& xs, const std::vector<Tensor>& weights_in, const std::vector<int64_t>& weight_of,
+                                const std::optional<Tensor>& turns, double eps, const std::vector<int64_t>& offsets,
+                                const std::vector<std::optional<Tensor>>& positions, bool interleaved, double amplitude) {
+  TORCH_CHECK_VALUE(!xs.empty() && offsets.size() == xs.size() && positions.size() == xs.size() && weight_of.size() == xs.size(),
+                    "one offset and one entry of weights and of positions per tensor expected");
+  for (const Tensor& x : xs) {
+    TORCH_CHECK_VALUE(x.dim() == 4 && x.is_cuda() && x.device() == xs[0].device() && x.scalar_type() == xs[0].scalar_type() && x.size(3) == xs[0].size(3) &&
+                      (x.scalar_type() == torch::kBFloat16 || x.scalar_type() == torch::kFloat),
+                      "[B, heads, rows, d] tensors of bfloat16 or float32, of one type, d and device, expected");
+    fits_int(x);
+    refuse_tangent(x);
+  }
+  TORCH_CHECK_VALUE(xs[0].size(3) >= 2, "at least two columns expected");
+  TORCH_CHECK_VALUE(eps > 0 && std::isfinite((float)eps) && (float)eps > 0, "eps: positive expected");
+  variable_list weights;
+  for (const Tensor& w : weights_in) {
+    check_weight(w, xs[0]);
+    weights.push_back(w.is_contiguous() ? w : w.contiguous());   // (a copy that is part of the graph)
+  }
+  if (turns.has_value()) check_turns(*turns, xs[0].size(3), xs[0]);
+  Norming how{weight_of, {}, offsets, turns.has_value(), interleaved, amplitude, eps};
+  variable_list at;
+  for (size_t i = 0; i < xs.size(); i++) {
+    TORCH_CHECK_VALUE(weight_of[i] >= -1 && weight_of[i] < (int64_t)weights.size(), "weights: a place among them expected");
+    const auto& p = positions[i];
+    how.position_of.push_back(p.has_value() ? (int64_t)at.size() : -1);
+    if (p.has_value()) at.push_back(positions_for(*p, xs[i]));
+  }
+  std::shared_ptr<NormRotaryBackward> node;
+  std::vector<size_t> wanted;                      // the tensors that are part of a graph
+  if (at::GradMode::is_enabled())
+    for (size_t i = 0; i < xs.size(); i++)
+      if (xs[i].requires_grad() || (weight_of[i] >= 0 && weights[weight_of[i]].requires_grad())) wanted.push_back(i);
+  if (!wanted.empty()) {
+    node = std::shared_ptr<NormRotaryBackward>(new NormRotaryBackward(), torch::autograd::deleteNode);
+    node->how = Norming{{}, {}, {}, how.rotated, interleaved, amplitude, eps};
+    for (const size_t i : wanted) {
+      node->add_next_edge(torch::autograd::impl::gradient_edge(xs[i]));
+      node->xs.emplace_back(xs[i], false);
+      node->how.weight_of.push_back(how.weight_of[i]);
+      node->how.position_of.push_back(how.position_of[i] >= 0 ? (int64_t)node->positions.size() : -1);
+      if (how.position_of[i] >= 0) node->positions.emplace_back(at[how.position_of[i]], false);
+      node->how.offsets.push_back(offsets[i]);
+    }
+    for (const Tensor& w : weights) {
+      node->add_next_edge(torch::autograd::impl::gradient_edge(w));
+      node->weights.emplace_back(w, false);
+    }
+    if (turns.has_value()) node->turns = torch::autograd::SavedVariable(*turns, false);
+    node->type = xs[0].scalar_type();
+  }
+  variable_list out;
+  {
+    const at::NoGradGuard no_grad;
+    const c10::DeviceGuard on(xs[0].device());
+    NormCall c;
+    set_norm(c, xs[0], weights, turns.has_value() ? *turns : Tensor(), how);
+    for (size_t i = 0; i < xs.size(); i++) {
+      const Tensor x = rows_in_place(xs[i]) ? xs[i] : xs[i].contiguous();
+      out.push_back(result_like(x));
+      burst_norm_rows b{};
+      set_rows(b.rows, x, out[i], how.position_of[i] >= 0 ? &at[how.position_of[i]] : nullptr, offsets[i]);
+      b.weight = (int32_t)weight_of[i];
+      c.items.push_back(b);
+      c.holds.push_back(x);
+    }
+    check(burst_norm_rotate(c.items.data(), (int)c.items.size(), c.weights.data(), (int)c.weights.size(), (float)eps, c.rotary, c.d, c.dtype,
+                            stream_of(xs[0])), "burst_norm_rotate");
+  }
+  for (const size_t i : wanted) torch::autograd::set_history(out[i], node);
+  return out;
+}
+
 // ---- paged: new tokens [rows, heads, d], pages [pages, kv_heads, page, d]
 void check_tokens(const Tensor& t, const Tensor& k_pages, const char* what) {
   TORCH_CHECK_VALUE(t.dim() == 3 && t.device() == k_pages.device() && t.scalar_type() == k_pages.scalar_type() && t.size(2) == k_pages.size(3), what,
@@ -474,7 +682,8 @@ burst_paged_params describe_paged(const Tensor& k_pages, const Tensor& v_pages, 
 
 std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const Tensor& k_pages, const Tensor& v_pages, const Tensor& table,
                                    const Tensor& lengths, const Tensor& starts, const std::optional<Tensor>& q_in, const std::optional<Tensor>& turns,
-                                   bool interleaved, double amplitude, const std::optional<Tensor>& offsets) {
+                                   bool interleaved, double amplitude, const std::optional<Tensor>& offsets, const std::optional<Tensor>& q_norm,
+                                   const std::optional<Tensor>& k_norm, double eps, const std::optional<Tensor>& slots, const std::optional<Tensor>& positions) {
   burst_paged_params p = describe_paged(k_pages, v_pages, table, lengths, starts);
   check_tokens(k_in, k_pages, "k");
   check_tokens(v_in, k_pages, "v");
@@ -484,6 +693,35 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
   if (offsets.has_value())
     TORCH_CHECK_VALUE(offsets->scalar_type() == torch::kLong && offsets->device() == k_pages.device() && offsets->is_contiguous() &&
                       offsets->sizes() == lengths.sizes(), "offsets: contiguous int64 [sequences] on the pages' device expected");
+  burst_store how{};
+  bool told = false;                               // more than burst_cache_append can be told
+  Tensor norms[2];
+  for (int i = 0; i < 2; i++) {
+    const auto& w = i ? k_norm : q_norm;
+    if (!w.has_value()) continue;
+    TORCH_CHECK_VALUE(w->dim() == 1 && w->size(0) == k_pages.size(3) && w->device() == k_pages.device() &&
+                      (w->scalar_type() == k_pages.scalar_type() || w->scalar_type() == torch::kFloat),
+                      "q_norm, k_norm: [d] on the pages' device, of their type or float32, expected");
+    refuse_tangent(*w);
+    TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && w->requires_grad()), "q_norm, k_norm: the paged calls have no gradient (call them under torch.no_grad)");
+    TORCH_CHECK_VALUE(eps > 0 && std::isfinite((float)eps) && (float)eps > 0, "eps: positive expected");
+    norms[i] = w->contiguous();
+    (i ? how.k_weight : how.q_weight) = norms[i].data_ptr();
+    (i ? how.k_weight_f32 : how.q_weight_f32) = w->scalar_type() == torch::kFloat;
+    told = true;
+  }
+  how.eps = (float)eps;
+  for (int i = 0; i < 2; i++) {
+    const auto& at = i ? positions : slots;
+    if (!at.has_value()) continue;
+    TORCH_CHECK_VALUE(at->scalar_type() == torch::kLong && at->device() == k_pages.device() && at->is_contiguous() && at->dim() == 1 && at->size(0) == k_in.size(0),
+                      "slots, positions: contiguous int64 [rows] on the pages' device expected");
+    (i ? how.positions : how.slots) = at->data_ptr<int64_t>();
+    told = true;
+  }
+  TORCH_CHECK_VALUE(!(positions.has_value() && offsets.has_value()), "positions say where the tokens are: no offsets expected");
+  TORCH_CHECK_VALUE(!q_norm.has_value() || q_in.has_value(), "q_norm without q: there is nothing to do with it");
+  how.offsets = offsets.has_value() ? offsets->data_ptr<int64_t>() : nullptr;
   const c10::DeviceGuard on(k_pages.device());
   Tensor k = k_in, v = v_in, q, out;
   if (!(tokens_in_place(k, 1) && tokens_in_place(v, 1)) || (k.size(0) > 1 && k.stride(0) != v.stride(0)) || (k.size(1) > 1 && k.stride(1) != v.stride(1))) {
@@ -494,7 +732,7 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
   p.H = p.kv_heads;
   set_token_strides(p.kv_strides, k);
   if (q_in.has_value()) {
-    TORCH_CHECK_VALUE(turns.has_value(), "q without turns: there is nothing to do to it");
+    TORCH_CHECK_VALUE(turns.has_value() || q_norm.has_value(), "q without turns: there is nothing to do to it");
     check_tokens(*q_in, k_pages, "q");
     TORCH_CHECK_VALUE(q_in->size(0) == k.size(0) && q_in->size(1) >= 1 && q_in->size(1) % k_pages.size(1) == 0, "q: [rows, H, d] with H a multiple of kv_heads expected");
     q = tokens_in_place(*q_in, 1) ? *q_in : q_in->contiguous();
@@ -506,9 +744,13 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
   if (turns.has_value()) {
     r.turns = turns->data_ptr<double>(); r.dims = (int32_t)(2 * turns->numel()); r.interleaved = interleaved; r.amplitude = (float)amplitude;
   }
-  check(burst_cache_append(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ptr(q), ptr(out),
-                           offsets.has_value() ? offsets->data_ptr<int64_t>() : nullptr, turns.has_value() ? &r : nullptr, &p, stream_of(k_pages)),
-        "burst_cache_append");
+  if (told)
+    check(burst_cache_store(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ptr(q), ptr(out), &how, turns.has_value() ? &r : nullptr, &p,
+                            stream_of(k_pages)), "burst_cache_store");
+  else
+    check(burst_cache_append(k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ptr(q), ptr(out),
+                             how.offsets, turns.has_value() ? &r : nullptr, &p, stream_of(k_pages)),
+          "burst_cache_append");
   written(k_pages);
   written(v_pages);
   if (!q_in.has_value()) return std::nullopt;
@@ -569,6 +811,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("attention", &attention, pybind11::call_guard<pybind11::gil_scoped_release>());
+  m.def("norm_rotate", &norm_rotate, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("rotate", &rotate, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("cache_append", &cache_append, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("paged_attention", &paged_attention, pybind11::call_guard<pybind11::gil_scoped_release>());

@@ -12,13 +12,19 @@ not kept, and see the keys that are), and attention with starts that decrease wr
 from . import binding as B
 
 
-def burst_cache_append(k, v, k_pages, v_pages, table, lengths, starts, q=None, turns=None, interleaved=False, amplitude=1.0, offsets=None):
+def burst_cache_append(k, v, k_pages, v_pages, table, lengths, starts, q=None, turns=None, interleaved=False, amplitude=1.0, offsets=None, q_norm=None,
+                       k_norm=None, eps=1e-6, slots=None, positions=None):
     """Writes the new tokens' k and v [rows, kv_heads, d] to their pages, k rotated by its positions (turns, interleaved, amplitude: see
     rotary.burst_rotary; None: not rotated); q [rows, H, d], if given, is rotated likewise and returned as a new tensor (rows behind the
     last sequence are not written).  offsets: int64 [sequences], added to the positions of the rotation (what of the
-    sequence lies on the ring's other devices).  One launch; no gradient."""
+    sequence lies on the ring's other devices).  q_norm, k_norm [d] (of the pages' type or float32): q, k are normalised first, as
+    rotary.burst_norm_rotary does, with these weights and eps.  slots: int64 [rows], the places of the tokens' keys and values (row slots[i] %
+    page of page slots[i] // page; negative or no page: left out) instead of those that the table says; positions: int64 [rows], the positions of the rotation
+    instead of the places in the sequences (a tree's tokens have those of their depth; negative: the row is left out).  With both, the batch's three arrays
+    are not read.  One launch; no gradient."""
     try:
-        return B.load_torch_module().cache_append(k, v, k_pages, v_pages, table, lengths, starts, q, turns, bool(interleaved), float(amplitude), offsets)
+        return B.load_torch_module().cache_append(k, v, k_pages, v_pages, table, lengths, starts, q, turns, bool(interleaved), float(amplitude), offsets,
+                                                  q_norm, k_norm, float(eps), slots, positions)
     except RuntimeError as e:
         raise B.from_native(e) from None
 

@@ -1,5 +1,6 @@
 """Rotation of queries and keys by their positions, as models apply it before the attention: one differentiable torch call
-for all tensors of a layer (native, csrc/burst_torch.cpp; the kernel is csrc/burst_rotary.hip)."""
+for all tensors of a layer (native, csrc/burst_torch.cpp; the kernel is csrc/burst_rotary.hip), and the same with the norm that many
+models put before it (csrc/burst_norm.hip)."""
 import math
 
 import torch
@@ -45,6 +46,33 @@ def burst_rotary(x, turns, offset=0, positions=None, interleaved=False, amplitud
     at = list(positions) if isinstance(positions, (list, tuple)) else [positions] * len(xs)
     try:
         y = B.load_torch_module().rotate(xs, turns, offsets, at, bool(interleaved), float(amplitude))
+    except RuntimeError as e:
+        raise B.from_native(e) from None
+    return y[0] if one else y
+
+
+def burst_norm_rotary(x, weights, turns=None, eps=1e-6, offset=0, positions=None, interleaved=False, amplitude=1.0):
+    """x: a [B, heads, rows, d] tensor or a list of them (bfloat16 or float32, d from 2 to 128), every row divided by the root of its mean square
+    (+ eps, positive), multiplied by the weights [d] (of x's type or float32; one tensor for all, or a list with an entry for each, None: 1), and rotated as
+    burst_rotary does (turns, offset, positions, interleaved, amplitude: see there; turns=None: not rotated), out of place, by one launch (12
+    tensors each).  All of it in 32 bits (the angles in 64), rounded once; sums of squares beyond 32 bits' range count as infinite.  Returns a
+    tensor or a list; results lie in memory like x.  Gradients flow to x and to the weights, whose gradients are summed in fp32 over all rows of all
+    tensors that share them (the same tensor in the list) and rounded once; gradients of gradients are an error."""
+    one = isinstance(x, torch.Tensor)
+    xs = [x] if one else list(x)
+    ws = [weights] * len(xs) if weights is None or isinstance(weights, torch.Tensor) else list(weights)
+    if len(ws) != len(xs):
+        raise ValueError("one entry of weights per tensor expected")
+    each, weight_of = [], []
+    for w in ws:
+        at = -1 if w is None else next((i for i, e in enumerate(each) if e is w), len(each))
+        if at == len(each):
+            each.append(w)
+        weight_of.append(at)
+    offsets = [int(o) for o in offset] if isinstance(offset, (list, tuple)) else [int(offset)] * len(xs)
+    at = list(positions) if isinstance(positions, (list, tuple)) else [positions] * len(xs)
+    try:
+        y = B.load_torch_module().norm_rotate(xs, each, weight_of, turns, float(eps), offsets, at, bool(interleaved), float(amplitude))
     except RuntimeError as e:
         raise B.from_native(e) from None
     return y[0] if one else y
