@@ -405,6 +405,13 @@ int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, voi
                     size_t workspace_bytes, const burst_paged_params* p, void* stream);
 /* Does not depend on what the arrays on the device hold; 0 for invalid parameters.  Host logic, no device call. */
 size_t burst_paged_workspace_bytes(const burst_paged_params* p);
+/* The same for drafted tokens, a tree of them a sequence (causal != 0).  tree: DEVICE [rows][words], row i's mask at tree + i * tree_stride (0 = words): new
+ * token t of a sequence sees all keys before the sequence's new tokens, and new token j if bit j % 64 of word j / 64 of its row is set (itself among
+ * them; bits from the number of new tokens on mean nothing).  With a window w, the keys before the new tokens at positions up to b + depth - w are hidden, where b is the
+ * position of the first new token and depth + 1 the number of bits; the mask alone says which new tokens are seen.  Sequences with more than 64 * words new
+ * tokens are chunks of prompts, as in burst_paged_fwd.  The masks are not to change while the call runs.  Workspace as burst_paged_fwd's. */
+int burst_paged_tree_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, const int64_t* tree, int words, int64_t tree_stride,
+                         void* workspace, size_t workspace_bytes, const burst_paged_params* p, void* stream);
 
 /* For tests and tuning (no counterpart in the paper): which of the two kernel families serves
  * bf16, d = 128 calls.  0 = chosen per call (the default): forward and dQ from how well the call's

@@ -24,7 +24,7 @@ EXPORTS = [
     "burst_materialized_bwd_workspace_bytes", "burst_local_bwd_materialized", "burst_set_kernel_family",
     "burst_kernel_family_for", "burst_local_bwd_static", "burst_probe_mfma", "burst_probe_atomic_dq",
     "burst_walk_fwd", "burst_walk_bwd", "burst_walk_workspace_bytes", "burst_walk_dkv_form",
-    "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_norm_workspace_bytes", "burst_cache_append", "burst_cache_store", "burst_paged_fwd", "burst_paged_workspace_bytes",
+    "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_norm_workspace_bytes", "burst_cache_append", "burst_cache_store", "burst_paged_fwd", "burst_paged_workspace_bytes", "burst_paged_tree_fwd",
 ]
 
 
@@ -179,7 +179,8 @@ def load():
     lib.burst_norm_workspace_bytes.argtypes = [np_, ci, wp, ci, ctypes.c_float, rp, ci, ci]
     lib.burst_norm_workspace_bytes.restype = sz
     lib.burst_cache_store.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(BurstStore), rp, gp, vp]
-    for name in ("burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_cache_append", "burst_cache_store", "burst_paged_fwd"):
+    lib.burst_paged_tree_fwd.argtypes = [vp, vp, vp, vp, fp, vp, ci, ctypes.c_int64, vp, sz, gp, vp]
+    for name in ("burst_paged_tree_fwd", "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_cache_append", "burst_cache_store", "burst_paged_fwd"):
         getattr(lib, name).restype = ci
     lib.burst_paged_workspace_bytes.argtypes = [gp]
     lib.burst_paged_workspace_bytes.restype = sz
@@ -695,6 +696,20 @@ def burst_paged_fwd(Q, k_pages, v_pages, O, lse, p, workspace=None):
     _check(load().burst_paged_fwd(_tokens(Q, p.H, p.q_strides, p, "Q"), _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"),
                                   _tokens(O, p.H, p.o_strides, p, "O", torch.float32 if p.out_f32 else None), _f32(lse),
                                   _ptr(workspace), _bytes(workspace), ctypes.byref(p), _stream()), "burst_paged_fwd")
+
+
+def burst_paged_tree_fwd(Q, k_pages, v_pages, O, lse, tree, p, workspace=None):
+    """tree: int64 device tensor [rows, words] with contiguous rows (see burst.h)."""
+    if lse.numel() < p.rows * p.H:
+        raise ValueError("lse: [rows, H] expected")
+    if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != p.rows or (tree.shape[1] > 1 and tree.stride(1) != 1) or \
+            (p.rows > 1 and tree.stride(0) < tree.shape[1]):
+        raise ValueError("tree: int64 [rows, words] with contiguous rows expected")
+    _here(tree, "tree")
+    _check(load().burst_paged_tree_fwd(_tokens(Q, p.H, p.q_strides, p, "Q"), _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"),
+                                       _tokens(O, p.H, p.o_strides, p, "O", torch.float32 if p.out_f32 else None), _f32(lse),
+                                       ctypes.c_void_p(tree.data_ptr()), tree.shape[1], tree.stride(0) if p.rows > 1 else 0, _ptr(workspace), _bytes(workspace),
+                                       ctypes.byref(p), _stream()), "burst_paged_tree_fwd")
 
 
 class Event:

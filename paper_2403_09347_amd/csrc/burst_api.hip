@@ -1448,16 +1448,21 @@ size_t burst_paged_workspace_bytes(const burst_paged_params* p) {
   return plan_paged(p, g, plan) == BURST_OK ? plan.bytes : 0;
 }
 
-int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,
-                    size_t workspace_bytes, const burst_paged_params* p, void* stream) {
+}  // extern "C"
+
+namespace {
+int paged_forward(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, const int64_t* tree, int words, int64_t tree_stride,
+                  void* workspace, size_t workspace_bytes, const burst_paged_params* p, void* stream) {
   Paged g;
   int st = check_paged(p, g, true);
   if (st != BURST_OK) return st;
+  if (words > 0 && (p->causal == 0 || words > 1 << 20 || (tree_stride != 0 && tree_stride < words))) return BURST_ERR_SHAPE;
   if (p->sequences == 0 || p->rows == 0) return BURST_OK;
   REQUIRE_PTR(Q); REQUIRE_PTR(O); REQUIRE_PTR(lse);
   if (p->pages > 0) { REQUIRE_PTR(K_pages); REQUIRE_PTR(V_pages); }
   REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4);
   if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
+  if (words > 0) REQUIRE_ALIGNED(tree, 8);
   PagedPlan plan;
   if ((st = plan_paged(p, g, plan)) != BURST_OK) return st;
   if (plan.bytes > 0) {
@@ -1469,11 +1474,29 @@ int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, voi
   const int rows = plan.chunk ? burst::kChunkRows : burst::kShortRows;
   a.Q = Q; a.O = O; a.lse = lse; a.K = K_pages; a.V = V_pages; a.part = (float*)workspace;
   a.join = a.runs < 2 ? nullptr : (burst::PagedJoin*)(a.part + (size_t)2 * a.runs * rows * (p->d + 2));
+  if (words > 0) {
+    a.tree = (const unsigned long long*)tree; a.words = words; a.tree_row = tree_stride != 0 ? tree_stride : words;
+    a.w.tree = 64 * words;
+  }
   hipStream_t s = (hipStream_t)stream;
   return validated([&] {
     const int e = plan.chunk ? burst::launch_paged_chunk(a, p->dtype, s) : burst::launch_paged_short(a, p->dtype, s);
     return e != BURST_OK ? e : burst::launch_paged_merge(a, rows, s);
   });
+}
+}  // namespace
+
+extern "C" {
+
+int burst_paged_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, void* workspace,
+                    size_t workspace_bytes, const burst_paged_params* p, void* stream) {
+  return paged_forward(Q, K_pages, V_pages, O, lse, nullptr, 0, 0, workspace, workspace_bytes, p, stream);
+}
+
+int burst_paged_tree_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, const int64_t* tree, int words, int64_t tree_stride,
+                         void* workspace, size_t workspace_bytes, const burst_paged_params* p, void* stream) {
+  if (words < 1) return BURST_ERR_SHAPE;
+  return paged_forward(Q, K_pages, V_pages, O, lse, tree, words, tree_stride, workspace, workspace_bytes, p, stream);
 }
 
 void* burst_event_create(void) {

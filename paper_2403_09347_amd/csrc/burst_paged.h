@@ -39,14 +39,19 @@ struct PagedWork {
   int causal, window;                // window: 0 = none
   int unit_shift;
   int item_cost;                     // what the beginning of an item costs, in units: it counts in a run's length
+  // Calls with trees (TREE, which the kernels of other calls do without): sequences of up to so many new tokens are some, masks say which new
+  // tokens theirs see.  (Asked at run time by all kernels, this cost those of longer chunks up to 25 scalar registers more, which they spill.)
+  int tree;
+  BURST_HD bool is_tree(const PagedSeq& q) const { return q.n <= tree; }
   BURST_HD int blocks(const PagedSeq& q) const { return (q.n + tokens - 1) / tokens; }
   // keys [lo, hi) that the rows of a block see between them
+  template <bool TREE = false>
   BURST_HD void keys(const PagedSeq& q, int block, int& lo, int& hi) const {
     const int t0 = block * tokens, t1 = (q.n - t0 < tokens ? q.n : t0 + tokens) - 1;
     lo = 0; hi = q.len;
-    if (causal && q.at + t1 + 1 < hi) hi = q.at + t1 + 1;
+    if (causal && !(TREE && is_tree(q)) && q.at + t1 + 1 < hi) hi = q.at + t1 + 1;
     if (window > 0) {
-      const int first = q.at + t0 - window + 1;   // (all of them at most 2^30)
+      const int first = TREE && is_tree(q) ? q.at - window : q.at + t0 - window + 1;   // (all of them at most 2^30; a tree's token that sees no new one: see tree_depth)
       if (first > 0) lo = first < hi ? first : hi;
     }
     if (hi < lo) hi = lo;
@@ -55,22 +60,25 @@ struct PagedWork {
   // see about the same.
   BURST_HD bool in_turn() const { return causal && window == 0; }
   BURST_HD int block_at(int place, int n) const { return !in_turn() ? place : place & 1 ? n - 1 - (place >> 1) : place >> 1; }
+  template <bool TREE = false>
   BURST_HD void units(const PagedSeq& q, int block, int& lo, int& hi) const {
     int k0, k1;
-    keys(q, block, k0, k1);
+    keys<TREE>(q, block, k0, k1);
     lo = k0 >> unit_shift;
     hi = k1 > k0 ? ((k1 - 1) >> unit_shift) + 1 : lo + 1;
   }
+  template <bool TREE = false>
   BURST_HD int cost(const PagedSeq& q, int block) const {   // units, an item's beginning among them
     int lo, hi;
-    units(q, block, lo, hi);
+    units<TREE>(q, block, lo, hi);
     return hi - lo + item_cost;
   }
   // blocks from, from + step .. of the n of a sequence, for one part of a head: all blocks' number, these ones' units, and those of the largest
+  template <bool TREE = false>
   BURST_HD PagedTotals totals(const PagedSeq& q, int n, int from, int step) const {
     PagedTotals t = {0, n, 0, 0};
     for (int b = from; b < n; b += step) {
-      const int c = cost(q, b);
+      const int c = cost<TREE>(q, b);
       t.units += c;
       if (c > t.most) t.most = c;
     }
@@ -78,8 +86,9 @@ struct PagedWork {
   }
   // units of two blocks that follow one another, at most; most: of the largest block.  (Blocks of a sequence that has outgrown its table all
   // see its last keys: the ends are no more than those between.)
+  template <bool TREE = false>
   BURST_HD int pair(const PagedSeq& q, int n, int most) const {
-    return in_turn() && n > 1 && q.at + q.n <= q.len ? cost(q, 0) + cost(q, n - 1) + (tokens >> unit_shift) + 2 : 2 * most;   // (rounded up)
+    return in_turn() && n > 1 && q.at + q.n <= q.len ? cost<TREE>(q, 0) + cost<TREE>(q, n - 1) + (tokens >> unit_shift) + 2 : 2 * most;   // (rounded up)
   }
   // Whether a sequence ends behind its start.  Where one does not, rows could belong to several sequences, and there could be more units than
   // 32 bits hold: such a call does nothing.
@@ -109,7 +118,7 @@ struct PagedSegment {
   BURST_HD bool whole() const { return from == lo && to == hi; }
 };
 // Where a run is.  Read: element i of one of the caller's arrays (device: by a scalar load).
-template <typename Read>
+template <typename Read, bool TREE = false>
 struct PagedCursor {
   PagedSegment g;
   int s, at;                         // sequence; place of the block
@@ -131,7 +140,7 @@ struct PagedCursor {
     const int n = w.blocks(g.q);
     for (at = by_items ? rem : skip(rem, n);; at++) {
       g.block = w.block_at(at, n);
-      w.units(g.q, g.block, g.lo, g.hi);
+      w.template units<TREE>(g.q, g.block, g.lo, g.hi);
       if (by_items || rem < g.hi - g.lo + w.item_cost) break;
       rem -= g.hi - g.lo + w.item_cost;
     }
@@ -160,15 +169,16 @@ struct PagedCursor {
       }
     }
     g.block = w.block_at(at, w.blocks(g.q));
-    w.units(g.q, g.block, g.lo, g.hi);
+    w.template units<TREE>(g.q, g.block, g.lo, g.hi);
     return cut(w, 0);
   }
 };
 // The tiles of 1 << shift keys (shift <= unit_shift) of a segment that hold a key which some row of its item sees: [first, end).  A segment
 // without any has one tile all the same (its rows are written), the only one that may begin at the end of the sequence or behind it.
+template <bool TREE = false>
 BURST_HD void segment_tiles(const PagedWork& w, const PagedSegment& g, int shift, int& first, int& end) {
   int k0, k1;
-  w.keys(g.q, g.block, k0, k1);
+  w.keys<TREE>(g.q, g.block, k0, k1);
   const int u = w.unit_shift - shift, e = (k1 + (1 << shift) - 1) >> shift;
   first = k0 >> shift > g.from << u ? k0 >> shift : g.from << u;
   end = e < g.to << u ? e : g.to << u;
@@ -191,6 +201,30 @@ BURST_HD int parts_to_join(const PagedSegment& g, int run_units) {
   const int before = g.from - g.lo;
   if (before == 0 || before > run_units) return 0;
   return 2 + (g.hi - g.from - 1) / run_units;
+}
+
+// Of a tree's token: which of the 64 keys from place `off` among the new tokens on (before them, if negative) its mask names.
+template <typename Word>
+BURST_HD unsigned long long tree_bits(const Word* mask, int words, int off) {
+  if (off <= -64 || off >= 64 * words) return 0;
+  if (off < 0) return (unsigned long long)mask[0] << -off;
+  const int i = off >> 6, shift = off & 63;
+  unsigned long long bits = (unsigned long long)mask[i] >> shift;
+  if (shift != 0 && i + 1 < words) bits |= (unsigned long long)mask[i + 1] << (64 - shift);
+  return bits;
+}
+// Its depth: the number of new tokens (n of them) that it sees, less itself.  A window counts from position at + depth back among the keys before the new ones.
+template <typename Word>
+BURST_HD int tree_depth(const Word* mask, int words, int n) {
+  int depth = -1;
+  for (int i = 0; i < words && 64 * i < n; i++) depth += __builtin_popcountll((unsigned long long)mask[i] & (n - 64 * i < 64 ? (1ull << (n - 64 * i)) - 1 : ~0ull));
+  return depth;
+}
+// Bits lo .. hi of 64 (any numbers).
+BURST_HD unsigned long long bit_range(int lo, int hi) {
+  lo = lo < 0 ? 0 : lo;
+  hi = hi > 63 ? 63 : hi;
+  return hi < lo ? 0 : ~0ull << lo & ~0ull >> (63 - hi);
 }
 
 // An entry of the page table, or -1 if it is no page.

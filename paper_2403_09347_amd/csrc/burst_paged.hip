@@ -46,6 +46,30 @@ __device__ __forceinline__ KeyRange seen_keys(const PagedWork& w, const PagedSeq
   return k;
 }
 
+// Trees (TREE: the call has some): a token sees the keys before the new tokens, in the window, and the new tokens that its mask names.
+__device__ __forceinline__ const unsigned long long* tree_mask(const PagedArgs& a, const PagedSeq& q, const ItemRow& x) {
+  return a.tree + (size_t)(q.first + (x.there ? x.token : 0)) * a.tree_row;
+}
+// see: of a token, as seen_keys has it.
+__device__ __forceinline__ void tree_keys(const PagedArgs& a, const PagedSeq& q, const ItemRow& x, KeyRange& see) {
+  if (!a.w.is_tree(q)) return;
+  see = KeyRange{0, min(q.at, q.len) - 1};
+  if (a.w.window > 0) see.lo = max(0, q.at + tree_depth(tree_mask(a, q, x), a.words, q.n) - a.w.window + 1);
+}
+// first, last: of a block's first and last token.  Keys up to first.hi and from last.lo on are seen by all between them, keys below first.lo and
+// above last.hi by none.
+__device__ __forceinline__ void tree_block_keys(const PagedWork& w, const PagedSeq& q, KeyRange& first, KeyRange& last) {
+  if (!w.is_tree(q)) return;
+  first = KeyRange{w.window > 0 ? max(0, q.at - w.window) : 0, min(q.at, q.len) - 1};
+  last = KeyRange{w.window > 0 ? max(0, q.at + q.n - w.window) : 0, q.len - 1};
+}
+// The keys of the 64 from key0 on that the lane's row sees, pages aside.  (see: tree_keys.)
+__device__ __forceinline__ unsigned long long tree_sight(const PagedArgs& a, const PagedSeq& q, const ItemRow& x, const KeyRange& see, int key0) {
+  unsigned long long bits = bit_range(see.lo - key0, see.hi - key0);
+  if (a.w.is_tree(q)) bits |= tree_bits(tree_mask(a, q, x), a.words, key0 - q.at) & bit_range(q.at - key0, q.len - 1 - key0);
+  return bits;
+}
+
 // A finished row (m in natural units, l, and its columns by `each`): the output and lse, or its partial result.
 struct RowPlace {
   bool whole;
@@ -83,13 +107,17 @@ __device__ __forceinline__ float row_lse(float m, float l) { return is_zero(l) ?
 // multiplies hidden pairs too (by a probability of 0, and 0 x inf is NaN).  One wavefront, one row at a time: 512 tokens over 8192 keys, 32 heads
 // over 8, take 0.12 ms, 33 with an infinity that 8 x 512 rows see.  (Loads of 16 bytes and eight keys' at a time made that 21, and every
 // call of the chunk kernel 1 % longer, which spilled more scalar registers.)
-template <typename T>
+template <typename T, bool TREE>
 __device__ __forceinline__ void row_again(const PagedArgs& a, const PagedSegment& g, int s_of, int run, int rows_of_item, int r, int lane) {
   const ItemRow x = item_row(a, g, r);
   if (!x.there) return;
   const int d = a.d, kvhead = g.part / a.parts_each;
   const T* const q = (const T*)a.Q + (size_t)(g.q.first + x.token) * a.q_row + (size_t)x.head * a.q_head;
-  KeyRange k = seen_keys(a.w, g.q, x.token);
+  KeyRange k = seen_keys(a.w, g.q, x.token), see = k;
+  if constexpr (TREE) {                            // (the new tokens, whatever the window leaves of the keys before them)
+    tree_keys(a, g.q, x, see);
+    if (a.w.is_tree(g.q)) k = KeyRange{min(see.lo, max(g.q.at, 0)), g.q.len - 1};
+  }
   k.lo = max(k.lo, g.from << a.w.unit_shift);
   k.hi = min(k.hi, (g.to << a.w.unit_shift) - 1);
   float m = BURST_NEG_INF, l = 0.f, o0 = 0.f, o1 = 0.f;
@@ -98,7 +126,7 @@ __device__ __forceinline__ void row_again(const PagedArgs& a, const PagedSegment
     const int key = k0 + lane;
     int page = -1;
     if (key <= k.hi) page = checked_page(a.table[(long long)s_of * a.table_stride + (key >> a.page_shift)], a.pages);
-    const bool seen = page >= 0;
+    const bool seen = page >= 0 && (!TREE || (tree_sight(a, g.q, x, see, k0) >> lane & 1) != 0);
     const long long row = (long long)page * a.p_page + (long long)kvhead * a.p_head + (long long)(key & ((1 << a.page_shift) - 1)) * a.p_row;
     float s = 0.f;
     if (seen) {
@@ -180,7 +208,7 @@ __device__ __forceinline__ void wait_lds() {
 template <int GR>
 __device__ __forceinline__ int short_code(int row) { return GR == 8 ? (row >> 1) & 7 : row_code(row & 15); }
 
-template <typename T, int D>
+template <typename T, int D, bool TREE>
 __global__ void __launch_bounds__(64, 1)
 paged_short_kernel(PagedArgs a) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -195,8 +223,8 @@ paged_short_kernel(PagedArgs a) {
   __shared__ i32x4 segs[NSEG][3];
   const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
   int run;
-  DeviceCursor fet;
-  if (!start_run(a, blockIdx.x, lane, lane == 0, fet, run)) return;
+  DeviceCursor<TREE> fet;
+  if (!start_run<TREE>(a, blockIdx.x, lane, lane == 0, fet, run)) return;
   const unsigned lds0 = lds_addr(smem);
   const int d = a.d;
   const unsigned pitch = (unsigned)(a.p_row * sizeof(T)), row_bytes = (unsigned)(d * sizeof(T));
@@ -225,7 +253,7 @@ paged_short_kernel(PagedArgs a) {
     f_base = f_at;
   };
   auto enter = [&]() __attribute__((always_inline)) {
-    segment_tiles(args_again<PagedArgs>().w, fet.g, 4, f_at, f_end);
+    segment_tiles<TREE>(args_again<PagedArgs>().w, fet.g, 4, f_at, f_end);
     if (lane == 0) {
       i32x4* const to = segs[seg_in % NSEG];
       to[0] = i32x4{fet.g.q.first, fet.g.q.n, fet.g.q.len, fet.g.part};
@@ -298,6 +326,7 @@ paged_short_kernel(PagedArgs a) {
       s.hi = one(d2[3]) & 1 ? s.to : s.to + 1;
       x = item_row(b, s, r);
       see = seen_keys(b.w, s.q, x.token);
+      if constexpr (TREE) tree_keys(b, s.q, x, see);
       const T* const qr = (const T*)b.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * b.q_row + (size_t)(x.there ? x.head : 0) * b.q_head;
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) {
@@ -312,7 +341,9 @@ paged_short_kernel(PagedArgs a) {
       for (int b = 0; b < OB; b++) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
       m = BURST_NEG_INF; l = 0.f;
       const int t0 = s.block * b.w.tokens, t1 = min(s.q.n, t0 + b.w.tokens) - 1;
-      all = KeyRange{seen_keys(b.w, s.q, t1).lo, seen_keys(b.w, s.q, t0).hi};
+      KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+      if constexpr (TREE) tree_block_keys(b.w, s.q, first, last);
+      all = KeyRange{last.lo, first.hi};
     }
     if (ahead == NST) wait_loads<(NST - 1) * LOADS>();
     else wait_loads<0>();
@@ -335,10 +366,17 @@ paged_short_kernel(PagedArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; j++) sc[j] = product(sc[j], a.scale);
     if (none || key0 < all.lo || key0 + 15 > all.hi) {
+      if constexpr (TREE) {
+        const unsigned bits = none ? 0u : (unsigned)(tree_sight(args_again<PagedArgs>(), s.q, x, see, key0) >> (4 * g));
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const int key = key0 + 4 * g + j;
-        if (none || key < see.lo || key > see.hi) sc[j] = BURST_NEG_INF;
+        for (int j = 0; j < 4; j++)
+          if ((bits >> j & 1) == 0) sc[j] = BURST_NEG_INF;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int key = key0 + 4 * g + j;
+          if (none || key < see.lo || key > see.hi) sc[j] = BURST_NEG_INF;
+        }
       }
     }
     const float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
@@ -420,7 +458,7 @@ paged_short_kernel(PagedArgs a) {
         else { at.ml[0] = m; at.ml[kShortRows] = l; }
       }
     }
-    for (; redo != 0; redo &= redo - 1) row_again<T>(b, s, seg_s, run, kShortRows, __builtin_ctz(redo), lane);
+    for (; redo != 0; redo &= redo - 1) row_again<T, TREE>(b, s, seg_s, run, kShortRows, __builtin_ctz(redo), lane);
   }
 }
 
@@ -429,13 +467,13 @@ paged_short_kernel(PagedArgs a) {
 // vector work overlaps the other's matrix work.
 // The fetching side, a tile of 1 << SHIFT keys ahead: tiles [f_at, f_end) of fet.g are still to be asked for.  A wavefront fetches a quarter of
 // every tile, whose keys lie in one page; the lanes hold the places of the 64 groups of 16 keys from tile f_base on.
-template <typename T, int D, int SHIFT>
+template <typename T, int D, int SHIFT, bool TREE>
 struct TileFeed {
   static constexpr int ROWB = D * (int)sizeof(T), GR = ROWB / 16, TILE = ROWB << SHIFT;   // LDS bytes and granules of a row; bytes of a tile
   static constexpr int GROUPS = (1 << SHIFT) / 16, ROWS = (1 << SHIFT) / 4;               // of 16 keys in a tile; keys of a wavefront's quarter
   static constexpr int RPL = 1024 / ROWB, NL = ROWS / RPL;                                // rows of a load; loads
   static __device__ __forceinline__ int code(int row) { return short_code<GR>(row); }
-  DeviceCursor fet;
+  DeviceCursor<TREE> fet;
   int w, lane;
   int f_first, f_at, f_end, f_base, where_lo, where_hi, goff[NL];
   unsigned long long pages;          // those of the 64 groups that have a page
@@ -448,7 +486,7 @@ struct TileFeed {
   __device__ __forceinline__ bool start(const PagedArgs& a, int& run, const char* smem) {
     lane = threadIdx.x & 63;
     w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (!start_run(a, blockIdx.x, lane, threadIdx.x == 0, fet, run)) return false;
+    if (!start_run<TREE>(a, blockIdx.x, lane, threadIdx.x == 0, fet, run)) return false;
     lds0 = lds_addr(smem) + (unsigned)(w * NL) * 1024u;
     pitch = (unsigned)(a.p_row * (int)sizeof(T)); row_bytes = (unsigned)(a.d * (int)sizeof(T));
     v_off = (const char*)a.V - (const char*)a.K;
@@ -476,7 +514,7 @@ struct TileFeed {
     f_base = f_at;
   }
   __device__ __forceinline__ void enter() {
-    segment_tiles(args_again<PagedArgs>().w, fet.g, SHIFT, f_at, f_end);
+    segment_tiles<TREE>(args_again<PagedArgs>().w, fet.g, SHIFT, f_at, f_end);
     f_first = f_at;
     look_up();
   }
@@ -522,10 +560,10 @@ constexpr int kTile = 1 << kTileShift;             // keys
 // 8, d = 128, 1100 / 1470; 4096 of 8192, d = 64, twice, 544 / 697; 12 sequences of 1 to 512 over 600 to 8000 167 / 173; a window of 1024,
 // d = 64, 36.3 / 41.2; 16 x 8 tokens over 8192 113.5 / 114.7; two prompts of 4096 of 8192, 32 heads over 8, at d = 32 433 / 508, d = 80 674 / 879, d = 96
 // 698 / 915, d = 104 799 / 1061.
-template <int D, int C, int TERMS>
+template <int D, int C, int TERMS, bool TREE>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_kernel(PagedArgs a) {
-  typedef TileFeed<bf16, D, kTileShift> Feed;
+  typedef TileFeed<bf16, D, kTileShift, TREE> Feed;
   constexpr int ROWB = Feed::ROWB, TILE = Feed::TILE, KS = C / 16, DB = C / 32, AHEAD = 4;
   __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
   int run;
@@ -556,7 +594,8 @@ paged_chunk_kernel(PagedArgs a) {
     int at = f.f_first;
     const PagedArgs& b = args_again<PagedArgs>();
     const ItemRow x = item_row(b, s, 32 * w + lr);
-    const KeyRange see = seen_keys(b.w, s.q, x.token);
+    KeyRange see = seen_keys(b.w, s.q, x.token);
+    if constexpr (TREE) tree_keys(b, s.q, x, see);
     bf16x8 q[KS];
     {
       const bf16* const qr = (const bf16*)b.Q + (size_t)(s.q.first + (x.there ? x.token : 0)) * b.q_row + (size_t)(x.there ? x.head : 0) * b.q_head;
@@ -577,7 +616,8 @@ paged_chunk_kernel(PagedArgs a) {
     const int most = min(b.w.tokens, s.q.n - s.block * b.w.tokens) - 1;
     const int t0 = s.block * b.w.tokens + 32 * w / b.part_heads, t1 = s.block * b.w.tokens + min((32 * w + 31) / b.part_heads, most);
     const bool rows_here = 32 * w / b.part_heads <= most;
-    const KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+    KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+    if constexpr (TREE) tree_block_keys(b.w, s.q, first, last);
 #pragma unroll 1
     for (; at < end; at++, buf ^= 1) {
       __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
@@ -609,14 +649,27 @@ paged_chunk_kernel(PagedArgs a) {
         }
       }
       if (none != 0 || key0 < last.lo || key0 + kTile - 1 > first.hi) {   // register r of block kb: key 32 kb + 8 (r / 4) + 4 h + r % 4
-        const int lo = see.lo - key0 - 4 * h, hi = see.hi - key0 - 4 * h;
+        if constexpr (TREE) {
+          unsigned long long bits = tree_sight(args_again<PagedArgs>(), s.q, x, see, key0);
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++)
+          for (int i = 0; i < 4; i++)
+            if (((none >> i) & 1) != 0) bits &= ~(0xffffull << (16 * i));
+          bits >>= 4 * h;
 #pragma unroll
-          for (int r = 0; r < 16; r++) {
-            const int k = kb * 32 + 8 * (r >> 2) + (r & 3);
-            if (k < lo || k > hi || ((none >> (2 * kb + (r >> 3))) & 1)) sc[kb][r] = BURST_NEG_INF;
-          }
+          for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+              if ((bits >> (kb * 32 + 8 * (r >> 2) + (r & 3)) & 1) == 0) sc[kb][r] = BURST_NEG_INF;
+        } else {
+          const int lo = see.lo - key0 - 4 * h, hi = see.hi - key0 - 4 * h;
+#pragma unroll
+          for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+              const int k = kb * 32 + 8 * (r >> 2) + (r & 3);
+              if (k < lo || k > hi || ((none >> (2 * kb + (r >> 3))) & 1)) sc[kb][r] = BURST_NEG_INF;
+            }
+        }
       }
       float mx = sc[0][0];
 #pragma unroll
@@ -700,17 +753,17 @@ paged_chunk_kernel(PagedArgs a) {
         else { to.ml[0] = mn; to.ml[kChunkRows] = l; }
       }
     }
-    for (; redo != 0; redo &= redo - 1) row_again<bf16>(b, s, seg_s, run, kChunkRows, 32 * w + __builtin_ctz(redo), lane);
+    for (; redo != 0; redo &= redo - 1) row_again<bf16, TREE>(b, s, seg_s, run, kChunkRows, 32 * w + __builtin_ctz(redo), lane);
   } while (f.more);
 }
 
 // fp32: tiles of 32 keys, products as in the short kernel, two blocks of 16 rows a wavefront (each operand of K and V read from LDS serves
 // both).  C: columns of the first product; the second one computes all D, whose blocks of 16 columns each hold every fourth column of 64.
 // Bound by the fp32 matrix rate: 4096 tokens over themselves, causal, 8 heads, d = 128, 324 us (106 TFLOP/s; a large library product 153).
-template <int D, int C>
+template <int D, int C, bool TREE>
 __global__ void __launch_bounds__(256, 2)
 paged_chunk_f32_kernel(PagedArgs a) {
-  typedef TileFeed<float, D, kTileShiftF32> Feed;
+  typedef TileFeed<float, D, kTileShiftF32, TREE> Feed;
   constexpr int ROWB = Feed::ROWB, TILE = Feed::TILE, GR = Feed::GR, KEYS = 1 << kTileShiftF32;
   constexpr int KS = C / 16, HV = GR / 16, OB = D / 16;   // granule steps of a product over d; 64-column parts; 16-column blocks of O^T
   __shared__ __attribute__((aligned(16))) char smem[4 * TILE];   // K[2], V[2]
@@ -741,6 +794,7 @@ paged_chunk_f32_kernel(PagedArgs a) {
     for (int i = 0; i < 2; i++) {
       x[i] = item_row(b, s, 32 * w + 16 * i + r);
       see[i] = seen_keys(b.w, s.q, x[i].token);
+      if constexpr (TREE) tree_keys(b, s.q, x[i], see[i]);
       const float* const qr = (const float*)b.Q + (size_t)(s.q.first + (x[i].there ? x[i].token : 0)) * b.q_row + (size_t)(x[i].there ? x[i].head : 0) * b.q_head;
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) {
@@ -754,7 +808,8 @@ paged_chunk_f32_kernel(PagedArgs a) {
     const int most = min(b.w.tokens, s.q.n - s.block * b.w.tokens) - 1;
     const int t0 = s.block * b.w.tokens + 32 * w / b.part_heads, t1 = s.block * b.w.tokens + min((32 * w + 31) / b.part_heads, most);
     const bool rows_here = 32 * w / b.part_heads <= most;
-    const KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+    KeyRange first = seen_keys(b.w, s.q, t0), last = seen_keys(b.w, s.q, t1);
+    if constexpr (TREE) tree_block_keys(b.w, s.q, first, last);
 #pragma unroll 1
     for (; at < end; at++, buf ^= 1) {
       __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0), lgkmcnt(0): the tile landed, reads of the one before are done
@@ -786,13 +841,15 @@ paged_chunk_f32_kernel(PagedArgs a) {
 #pragma unroll
       for (int i = 0; i < 2; i++) {
         mx[i] = BURST_NEG_INF;
+        unsigned bits = 0;
+        if (TREE && masked) bits = (unsigned)(tree_sight(args_again<PagedArgs>(), s.q, x[i], see[i], key0) >> (4 * g));
 #pragma unroll
         for (int kb = 0; kb < 2; kb++)
 #pragma unroll
           for (int j = 0; j < 4; j++) {
             float v = product(sc[i][kb][j], a.scale);
             const int key = key0 + 16 * kb + 4 * g + j;
-            if (masked && (((none >> kb) & 1) != 0 || key < see[i].lo || key > see[i].hi)) v = BURST_NEG_INF;
+            if (masked && (((none >> kb) & 1) != 0 || (TREE ? (bits >> (16 * kb + j) & 1) == 0 : key < see[i].lo || key > see[i].hi))) v = BURST_NEG_INF;
             sc[i][kb][j] = v;
             mx[i] = fmaxf(mx[i], v);
           }
@@ -859,7 +916,7 @@ paged_chunk_f32_kernel(PagedArgs a) {
           else { to.ml[0] = m[i]; to.ml[kChunkRows] = l[i]; }
         }
       }
-      for (; redo != 0; redo &= redo - 1) row_again<float>(b, s, seg_s, run, kChunkRows, 32 * w + 16 * i + __builtin_ctz(redo), lane);
+      for (; redo != 0; redo &= redo - 1) row_again<float, TREE>(b, s, seg_s, run, kChunkRows, 32 * w + 16 * i + __builtin_ctz(redo), lane);
     }
   } while (f.more);
 }
@@ -950,32 +1007,42 @@ paged_merge_kernel(PagedArgs a, int rows_of_item) {
 }
 
 // ------------------------------------------------------------------------------- launches
-int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s) {
+template <bool TREE>
+static void enqueue_short(const PagedArgs& a, int dtype, hipStream_t s) {
   const dim3 grid((unsigned)a.runs), block(64);
   if (dtype == BURST_BF16) {
-    if (a.d <= 64) BURST_LAUNCH((paged_short_kernel<bf16, 64>), grid, block, 0, s, a);
-    else BURST_LAUNCH((paged_short_kernel<bf16, 128>), grid, block, 0, s, a);
+    if (a.d <= 64) BURST_LAUNCH((paged_short_kernel<bf16, 64, TREE>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_short_kernel<bf16, 128, TREE>), grid, block, 0, s, a);
   } else {
-    if (a.d <= 64) BURST_LAUNCH((paged_short_kernel<float, 64>), grid, block, 0, s, a);
-    else BURST_LAUNCH((paged_short_kernel<float, 128>), grid, block, 0, s, a);
+    if (a.d <= 64) BURST_LAUNCH((paged_short_kernel<float, 64, TREE>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_short_kernel<float, 128, TREE>), grid, block, 0, s, a);
   }
+}
+int launch_paged_short(const PagedArgs& a, int dtype, hipStream_t s) {
+  if (a.tree != nullptr) enqueue_short<true>(a, dtype, s);
+  else enqueue_short<false>(a, dtype, s);
   return launch_status();
 }
-int launch_paged_chunk(const PagedArgs& a, int dtype, hipStream_t s) {
+template <bool TREE>
+static void enqueue_chunk(const PagedArgs& a, int dtype, hipStream_t s) {
   const dim3 grid((unsigned)a.runs), block(256);
   if (dtype == BURST_BF16) {
     const bool one = !a.full_p && (a.d == 64 || a.d == 128);
-    if (a.d <= 32) BURST_LAUNCH((paged_chunk_kernel<64, 32, 2>), grid, block, 0, s, a);
-    else if (a.d <= 64 && one) BURST_LAUNCH((paged_chunk_kernel<64, 64, 1>), grid, block, 0, s, a);
-    else if (a.d <= 64) BURST_LAUNCH((paged_chunk_kernel<64, 64, 2>), grid, block, 0, s, a);
-    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_kernel<128, 96, 2>), grid, block, 0, s, a);
-    else if (one) BURST_LAUNCH((paged_chunk_kernel<128, 128, 1>), grid, block, 0, s, a);
-    else BURST_LAUNCH((paged_chunk_kernel<128, 128, 2>), grid, block, 0, s, a);
+    if (a.d <= 32) BURST_LAUNCH((paged_chunk_kernel<64, 32, 2, TREE>), grid, block, 0, s, a);
+    else if (a.d <= 64 && one) BURST_LAUNCH((paged_chunk_kernel<64, 64, 1, TREE>), grid, block, 0, s, a);
+    else if (a.d <= 64) BURST_LAUNCH((paged_chunk_kernel<64, 64, 2, TREE>), grid, block, 0, s, a);
+    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_kernel<128, 96, 2, TREE>), grid, block, 0, s, a);
+    else if (one) BURST_LAUNCH((paged_chunk_kernel<128, 128, 1, TREE>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_chunk_kernel<128, 128, 2, TREE>), grid, block, 0, s, a);
   } else {
-    if (a.d <= 64) BURST_LAUNCH((paged_chunk_f32_kernel<64, 64>), grid, block, 0, s, a);
-    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_f32_kernel<128, 96>), grid, block, 0, s, a);
-    else BURST_LAUNCH((paged_chunk_f32_kernel<128, 128>), grid, block, 0, s, a);
+    if (a.d <= 64) BURST_LAUNCH((paged_chunk_f32_kernel<64, 64, TREE>), grid, block, 0, s, a);
+    else if (a.d <= 96) BURST_LAUNCH((paged_chunk_f32_kernel<128, 96, TREE>), grid, block, 0, s, a);
+    else BURST_LAUNCH((paged_chunk_f32_kernel<128, 128, TREE>), grid, block, 0, s, a);
   }
+}
+int launch_paged_chunk(const PagedArgs& a, int dtype, hipStream_t s) {
+  if (a.tree != nullptr) enqueue_chunk<true>(a, dtype, s);
+  else enqueue_chunk<false>(a, dtype, s);
   return launch_status();
 }
 int launch_paged_merge(const PagedArgs& a, int rows_of_item, hipStream_t s) {

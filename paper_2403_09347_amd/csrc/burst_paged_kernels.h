@@ -21,6 +21,9 @@ struct PagedArgs {
   int runs, slack, few, o_f32;       // slack, few: see paged_deal
   int full_p;                        // see paged_chunk_kernel's TERMS
   float scale;
+  const unsigned long long* tree;    // masks of the rows, tree_row words apart; nullptr: no trees
+  long long tree_row;
+  int words;
 };
 // What a run tells the merging launch: the item that is joined from the parts of n runs, from the run before it on (n = 0: none); run 0, which
 // cuts none: the number of runs that have work, in n.
@@ -40,7 +43,8 @@ __device__ __forceinline__ int scalar_at(const int* p, I i) {
   return ((const int __attribute__((address_space(4)))*)p)[i];
 }
 struct ScalarRead { static __device__ __forceinline__ int at(const int* p, int i) { return scalar_at(p, __builtin_amdgcn_readfirstlane(i)); } };
-typedef PagedCursor<ScalarRead> DeviceCursor;
+template <bool TREE>
+using DeviceCursor = PagedCursor<ScalarRead, TREE>;
 
 __device__ __forceinline__ int wave_scan(int x) {  // inclusive
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr:1, 2, 4, 8
@@ -65,7 +69,8 @@ __device__ __forceinline__ int wave_most(int x) {  // of numbers that are not ne
 // Of sequences with many blocks the lanes share the blocks where there are few such sequences: going through them takes as long as
 // the longest has blocks, sharing about four blocks' time for every 64.  (us a call, lanes by themselves / so: 131072 tokens with a window of
 // 1024, 8 heads over one, 1361 / 817; 16384 tokens causal 657 / 591; 4096, 32 heads over 8, 158 / 152; single tokens 0.1 more.)
-__device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane, bool tell, DeviceCursor& cur, int& run) {
+template <bool TREE>
+__device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane, bool tell, DeviceCursor<TREE>& cur, int& run) {
   const PagedWork& w = a.w;
   PagedSeq q;
   PagedTotals mine = {0, 0, 0, 0}, all = {0, 0, 0, 0};
@@ -85,17 +90,17 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane,
       const int most = wave_most(n);
       if (4LL * __builtin_popcountll(longer) * ((most + 63) / 64) >= most) longer = 0;
     }
-    if (((longer >> lane) & 1) == 0) mine = w.totals(q, n, 0, 1);
+    if (((longer >> lane) & 1) == 0) mine = w.totals<TREE>(q, n, 0, 1);
 #pragma unroll 1
     for (; longer != 0; longer &= longer - 1) {
       const int at = __builtin_ctzll(longer);
       const PagedSeq there = {0, __builtin_amdgcn_readlane(q.n, at), __builtin_amdgcn_readlane(q.len, at), __builtin_amdgcn_readlane(q.at, at)};
-      PagedTotals t = w.totals(there, __builtin_amdgcn_readlane(n, at), lane, 64);
+      PagedTotals t = w.totals<TREE>(there, __builtin_amdgcn_readlane(n, at), lane, 64);
       t.units = __builtin_amdgcn_readlane(wave_scan(t.units), 63);
       t.most = wave_most(t.most);
       if (lane == at) mine = t;
     }
-    mine.pair = w.pair(q, n, mine.most);
+    mine.pair = w.pair<TREE>(q, n, mine.most);
   };
 #pragma unroll 1
   for (int base = 0; base < w.sequences; base += 64) {
@@ -132,7 +137,7 @@ __device__ __forceinline__ bool start_run(const PagedArgs& a, int bid, int lane,
                        int place = 0;
 #pragma unroll 1
                        for (; n - place > 8; place += 64) {
-                         const int c = place + lane < n ? w.cost(there, w.block_at(place + lane, n)) : 0, sum = wave_scan(c);
+                         const int c = place + lane < n ? w.cost<TREE>(there, w.block_at(place + lane, n)) : 0, sum = wave_scan(c);
                          if (rem < __builtin_amdgcn_readlane(sum, 63)) {
                            const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rem < sum));
                            rem -= __builtin_amdgcn_readlane(sum - c, i);

@@ -759,12 +759,19 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
 
 std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_pages, const Tensor& v_pages, const Tensor& table, const Tensor& lengths,
                                            const Tensor& starts, double scale, bool causal, int64_t window, int64_t max_new,
-                                           const std::optional<Tensor>& o_out, const std::optional<Tensor>& lse_out, bool full_p) {
+                                           const std::optional<Tensor>& o_out, const std::optional<Tensor>& lse_out, bool full_p,
+                                           const std::optional<Tensor>& tree) {
   burst_paged_params p = describe_paged(k_pages, v_pages, table, lengths, starts);
   check_tokens(q_in, k_pages, "q");
   TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && (k_pages.requires_grad() || v_pages.requires_grad())),
                     "pages that require a gradient: the paged calls have no gradient (call them under torch.no_grad)");
   TORCH_CHECK_VALUE(max_new >= 0 && max_new <= 0x7fffffff && window >= 0, "max_new, window: not negative expected");
+  if (tree.has_value()) {
+    TORCH_CHECK_VALUE(tree->scalar_type() == torch::kLong && tree->device() == k_pages.device() && tree->dim() == 2 && tree->size(0) == q_in.size(0) &&
+                      tree->size(1) >= 1 && tree->size(1) <= 1 << 20 && (tree->size(1) == 1 || tree->stride(1) == 1) &&
+                      (tree->size(0) <= 1 || tree->stride(0) >= tree->size(1)), "tree: int64 [rows, words] on the pages' device, its rows contiguous, expected");
+    TORCH_CHECK_VALUE(causal, "tree: masks of a causal call expected");
+  }
   const c10::DeviceGuard on(k_pages.device());
   const int64_t unit = 16 / (int64_t)q_in.element_size();
   const Tensor q = tokens_in_place(q_in, unit) ? q_in : q_in.contiguous();
@@ -800,8 +807,12 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   set_token_strides(p.o_strides, O);
   const size_t need = burst_paged_workspace_bytes(&p);
   const Tensor ws = need ? torch::empty({(int64_t)need}, q.options().dtype(torch::kByte)) : Tensor();
-  check(burst_paged_fwd(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), O.data_ptr(), lse.data_ptr<float>(), ptr(ws), bytes(ws), &p, stream_of(q)),
-        "burst_paged_fwd");
+  if (tree.has_value())
+    check(burst_paged_tree_fwd(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), O.data_ptr(), lse.data_ptr<float>(), tree->data_ptr<int64_t>(),
+                               (int)tree->size(1), tree->size(0) > 1 ? tree->stride(0) : 0, ptr(ws), bytes(ws), &p, stream_of(q)), "burst_paged_tree_fwd");
+  else
+    check(burst_paged_fwd(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), O.data_ptr(), lse.data_ptr<float>(), ptr(ws), bytes(ws), &p, stream_of(q)),
+          "burst_paged_fwd");
   if (o_out.has_value()) written(O);
   if (lse_out.has_value()) written(lse);
   return {O, lse};

@@ -29,7 +29,7 @@ def burst_cache_append(k, v, k_pages, v_pages, table, lengths, starts, q=None, t
         raise B.from_native(e) from None
 
 
-def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=None, causal=True, window=0, max_new=0, out=None, lse=None, full_p=False):
+def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=None, causal=True, window=0, max_new=0, out=None, lse=None, full_p=False, tree=None):
     """Attention of the new tokens q [rows, H, d] (H a multiple of kv_heads) over the keys of their sequences up to their own positions (causal =
     False: all of them), the last `window` of them if that is not 0.  Returns (O [rows, H, d], lse [rows, H] fp32): new tensors, or out
     (of q's type or float32) and lse; rows behind the last sequence are not written, tokens that see no key get 0 and -inf.
@@ -37,10 +37,14 @@ def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=Non
     of keys and values, have one that is made for them).  0: not known; 1 is taken where there are no more rows than sequences.
     O as float32, lse and a sum of 1 are a state that binding.burst_merge_state joins with those of
     the ring's other devices.  full_p (bfloat16): probabilities enter the product with the values with 16 bits in any call; otherwise the kernel
-    of longer chunks rounds them to 8 at d = 64 and d = 128, as the walks do.  No gradient."""
+    of longer chunks rounds them to 8 at d = 64 and d = 128, as the walks do.
+    tree: int64 [rows, words], the masks of drafted tokens: new token t of a sequence sees all keys before the sequence's new tokens, and new token j if bit
+    j % 64 of word j // 64 of its row is set (its own among them).  A window then counts back from the first new token's position + the token's
+    depth (bits - 1) among the keys before; the mask alone says which new tokens are seen.  Sequences with more than 64 * words new tokens are chunks of
+    prompts, as without masks.  No gradient."""
     scale = float(scale) if scale is not None else q.shape[-1] ** -0.5
     try:
         return B.load_torch_module().paged_attention(q, k_pages, v_pages, table, lengths, starts, scale, bool(causal), int(window), int(max_new), out, lse,
-                                                      bool(full_p))
+                                                      bool(full_p), tree)
     except RuntimeError as e:
         raise B.from_native(e) from None
