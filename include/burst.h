@@ -413,6 +413,36 @@ size_t burst_paged_workspace_bytes(const burst_paged_params* p);
 int burst_paged_tree_fwd(const void* Q, const void* K_pages, const void* V_pages, void* O, float* lse, const int64_t* tree, int words, int64_t tree_stride,
                          void* workspace, size_t workspace_bytes, const burst_paged_params* p, void* stream);
 
+/* The books of such a cache, kept on the device: what a step's calls read, from the lengths of its sequences.
+ * Sequences are served in their order, those that do not fit are passed over: their new tokens have to fit into the token tensors behind those of the sequences served before,
+ * all of their tokens into a row of the table, and the pages that they still lack have to be on the stack.  Entries of a served sequence's row that new
+ * tokens lie in and that hold no page (nothing in 0 .. pages - 1) get the pages from the top of the stack, in their order; what is there is kept, so that the same call again
+ * changes nothing.  Sequences that have ended give the pages of their row back first, in order, and have -1 in all of it. */
+typedef struct burst_plan {
+  int32_t sequences, rows;           /* 0 .. 4096; 0 .. 2^20 - 1, of the token tensors */
+  int32_t pages, page, width;        /* as in burst_paged_params */
+  int32_t words, most;               /* of the masks; columns of parents */
+  int32_t reserved;                  /* 0 */
+  const int32_t* added;              /* DEVICE [sequences]: new tokens; negative: the sequence has ended */
+  const int32_t* lengths;            /* DEVICE [sequences]: tokens that are in the cache (cut to 0 .. 2^30) */
+  int32_t* table; int64_t table_stride;   /* DEVICE [sequences][width], read and written; stride as in burst_paged_params */
+  int32_t* free_pages; int32_t* free_count;   /* DEVICE [pages], [1]: the stack of pages that are free, its top at free_count - 1 (cut to 0 .. pages); read and written */
+  const int32_t* parents; int64_t parents_stride;   /* DEVICE [sequences][most] (stride: 0 = most): the new token that each new token hangs on, one before it; negative, another, or not among
+                                      * the columns: none.  NULL: no trees */
+  int32_t* starts; int32_t* totals;  /* written, DEVICE [sequences + 1], [sequences]: starts and lengths for the paged calls (a sequence that was passed over has no new tokens) */
+  int64_t* slots; int64_t* positions;   /* written, DEVICE [rows]: see burst_store; -1 behind the last sequence.  Positions of trees: tokens before the new ones + depth */
+  int64_t* tree;                     /* written if there are parents, DEVICE [rows][words]: see burst_paged_tree_fwd; 0 for chunks of more than 64 * words tokens, whose parents are
+                                      * not looked at */
+} burst_plan;
+/* The arrays that are written lie apart from one another and from those that are read. */
+int burst_cache_plan(const burst_plan* p, void* stream);
+/* Keeps some of the new tokens of every sequence, in all layers' pages: with b = lengths[s] - the number of new tokens, the row at position b + kept[s * kept_stride + j] goes to
+ * position b + j, for j < counts[s] (cut to 0 .. most and to the new tokens), and lengths_out[s] is b + counts[s].  The numbers in kept (kept_stride: 0 = most) increase within a
+ * sequence; where they do not, or are none of a new token, it is not defined which row is where (it is some new token's, or what was there).  Rows whose place is in no
+ * page stay.  pools: HOST array of n different tensors of pages, keys' and values', that lie as page_strides say.  lengths_out is none of the arrays that are read.  sequences: at most 65535. */
+int burst_cache_keep(void* const* pools, int n, const int32_t* kept, int64_t kept_stride, int most, const int32_t* counts, int32_t* lengths_out,
+                     const burst_paged_params* p, void* stream);
+
 /* For tests and tuning (no counterpart in the paper): which of the two kernel families serves
  * bf16, d = 128 calls.  0 = chosen per call (the default): forward and dQ from how well the call's
  * workgroups fill the chip and from the flags' block edge, dK/dV always hand-scheduled, with 64

@@ -25,6 +25,7 @@ EXPORTS = [
     "burst_kernel_family_for", "burst_local_bwd_static", "burst_probe_mfma", "burst_probe_atomic_dq",
     "burst_walk_fwd", "burst_walk_bwd", "burst_walk_workspace_bytes", "burst_walk_dkv_form",
     "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_norm_workspace_bytes", "burst_cache_append", "burst_cache_store", "burst_paged_fwd", "burst_paged_workspace_bytes", "burst_paged_tree_fwd",
+    "burst_cache_plan", "burst_cache_keep",
 ]
 
 
@@ -72,6 +73,13 @@ class BurstStore(ctypes.Structure):
     _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("q_weight_f32", ctypes.c_int32), ("k_weight_f32", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("offsets", ctypes.c_void_p)]
+
+
+class BurstPlan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "rows", "pages", "page", "width", "words", "most", "reserved")] + [
+        ("added", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("parents", ctypes.c_void_p), ("parents_stride", ctypes.c_int64),
+        ("starts", ctypes.c_void_p), ("totals", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("tree", ctypes.c_void_p)]
 
 
 class BurstPagedParams(ctypes.Structure):
@@ -180,7 +188,9 @@ def load():
     lib.burst_norm_workspace_bytes.restype = sz
     lib.burst_cache_store.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(BurstStore), rp, gp, vp]
     lib.burst_paged_tree_fwd.argtypes = [vp, vp, vp, vp, fp, vp, ci, ctypes.c_int64, vp, sz, gp, vp]
-    for name in ("burst_paged_tree_fwd", "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_cache_append", "burst_cache_store", "burst_paged_fwd"):
+    lib.burst_cache_plan.argtypes = [ctypes.POINTER(BurstPlan), vp]
+    lib.burst_cache_keep.argtypes = [ctypes.POINTER(vp), ci, vp, ctypes.c_int64, ci, vp, vp, gp, vp]
+    for name in ("burst_cache_plan", "burst_cache_keep", "burst_paged_tree_fwd", "burst_rotate", "burst_norm_rotate", "burst_norm_rotate_bwd", "burst_cache_append", "burst_cache_store", "burst_paged_fwd"):
         getattr(lib, name).restype = ci
     lib.burst_paged_workspace_bytes.argtypes = [gp]
     lib.burst_paged_workspace_bytes.restype = sz
@@ -710,6 +720,46 @@ def burst_paged_tree_fwd(Q, k_pages, v_pages, O, lse, tree, p, workspace=None):
                                        _tokens(O, p.H, p.o_strides, p, "O", torch.float32 if p.out_f32 else None), _f32(lse),
                                        ctypes.c_void_p(tree.data_ptr()), tree.shape[1], tree.stride(0) if p.rows > 1 else 0, _ptr(workspace), _bytes(workspace),
                                        ctypes.byref(p), _stream()), "burst_paged_tree_fwd")
+
+
+def burst_cache_plan(added, lengths, table, free_pages, free_count, page, starts, totals, slots, positions, parents=None, tree=None):
+    """int32 device tensors added, lengths, totals [sequences], table [sequences, width], free_pages [pages], free_count [1], starts [sequences + 1], parents
+    [sequences, most] or None; int64 ones slots, positions [rows], tree [rows, words] or None (see burst.h)."""
+    S, rows = added.shape[0], slots.shape[0]
+    shapes = dict(added=(added, (S,)), lengths=(lengths, (S,)), totals=(totals, (S,)), starts=(starts, (S + 1,)), free_count=(free_count, (1,)),
+                  free_pages=(free_pages, (free_pages.numel(),)), table=(table, (S, table.shape[-1])), slots=(slots, (rows,)), positions=(positions, (rows,)))
+    if (parents is None) != (tree is None):
+        raise ValueError("parents and tree: both or none expected")
+    if parents is not None:
+        shapes.update(parents=(parents, (S, parents.shape[-1])), tree=(tree, (rows, tree.shape[-1])))
+    for name, (t, shape) in shapes.items():
+        if t.dtype != (torch.int64 if name in ("slots", "positions", "tree") else torch.int32) or tuple(t.shape) != shape:
+            raise ValueError(f"{name}: {'int64' if name in ('slots', 'positions', 'tree') else 'int32'} tensor {list(shape)} expected")
+        rows_of_it = name in ("table", "parents")
+        if not (t.is_contiguous() if not rows_of_it else (shape[1] <= 1 or t.stride(1) == 1) and (shape[0] <= 1 or t.stride(0) >= shape[1])):
+            raise ValueError(f"{name}: contiguous expected")
+        _here(t, name)
+    p = BurstPlan(sequences=S, rows=rows, pages=free_pages.shape[0], page=page, width=table.shape[1], added=added.data_ptr(), lengths=lengths.data_ptr(),
+                  table=table.data_ptr(), table_stride=table.stride(0) if S > 1 else 0, free_pages=free_pages.data_ptr(), free_count=free_count.data_ptr(),
+                  starts=starts.data_ptr(), totals=totals.data_ptr(), slots=slots.data_ptr(), positions=positions.data_ptr())
+    if parents is not None:
+        p.words, p.most, p.tree, p.parents = tree.shape[1], parents.shape[1], tree.data_ptr(), parents.data_ptr()
+        p.parents_stride = parents.stride(0) if S > 1 else 0
+    _check(load().burst_cache_plan(ctypes.byref(p), _stream()), "burst_cache_plan")
+
+
+def burst_cache_keep(pools, kept, counts, lengths_out, p):
+    """pools: all layers' k_pages and v_pages, which lie as the parameter block says; kept [sequences, most], counts, lengths_out [sequences]: int32 device
+    tensors."""
+    for t, shape, what in ((kept, (p.sequences, kept.shape[-1]), "kept"), (counts, (p.sequences,), "counts"), (lengths_out, (p.sequences,), "lengths_out")):
+        if t.dtype != torch.int32 or tuple(t.shape) != shape or (t.dim() == 1 and not t.is_contiguous()):
+            raise ValueError(f"{what}: int32 tensor {list(shape)} expected")
+        _here(t, what)
+    if (kept.shape[1] > 1 and kept.stride(1) != 1) or (p.sequences > 1 and kept.stride(0) < kept.shape[1]):
+        raise ValueError("kept: contiguous rows expected")
+    at = (ctypes.c_void_p * len(pools))(*[_pages(t, p, "pools").value for t in pools])
+    _check(load().burst_cache_keep(at, len(pools), ctypes.c_void_p(kept.data_ptr()), kept.stride(0) if p.sequences > 1 else 0, kept.shape[1],
+                                   ctypes.c_void_p(counts.data_ptr()), ctypes.c_void_p(lengths_out.data_ptr()), ctypes.byref(p), _stream()), "burst_cache_keep")
 
 
 class Event:

@@ -10,6 +10,7 @@
 #include "burst_common.h"
 #include "burst_norm.h"
 #include "burst_paged_kernels.h"
+#include "burst_plan.h"
 #include "burst_rotary.h"
 
 namespace burst {
@@ -1439,6 +1440,78 @@ int burst_cache_store(const void* K, const void* V, void* K_pages, void* V_pages
   add(V, V_pages, g.kv, p->kv_heads, nullptr, 0, 0, 1);
   const long long blocks = burst::set_tiles(a, p->dtype, false);
   return blocks < 0 ? (int)BURST_ERR_SHAPE : burst::launch_norm(a, p->dtype, blocks, (hipStream_t)stream);
+}
+
+int burst_cache_plan(const burst_plan* p, void* stream) {
+  if (p == nullptr) return BURST_ERR_NULL;
+  if (p->sequences < 0 || p->sequences > burst::kPlanSequences || p->rows < 0 || p->rows > burst::kPlanMostRows || p->pages < 0 || p->width < 0 ||
+      p->most < 0 || p->words < 0 || p->words > 1 << 20) return BURST_ERR_SHAPE;
+  if (p->page < 16 || (p->page & (p->page - 1)) != 0 || (long long)p->width * p->page >= 1LL << 30) return BURST_ERR_SHAPE;
+  if ((p->table_stride != 0 && p->table_stride < p->width) || (p->parents_stride != 0 && p->parents_stride < p->most)) return BURST_ERR_SHAPE;
+  if (p->parents != nullptr && p->words < 1) return BURST_ERR_SHAPE;
+  if (p->sequences > 0) {
+    REQUIRE_ALIGNED(p->added, 4); REQUIRE_ALIGNED(p->lengths, 4); REQUIRE_ALIGNED(p->totals, 4);
+    if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
+  }
+  if (p->pages > 0) REQUIRE_ALIGNED(p->free_pages, 4);
+  REQUIRE_ALIGNED(p->free_count, 4); REQUIRE_ALIGNED(p->starts, 4);
+  if (p->rows > 0) {
+    REQUIRE_ALIGNED(p->slots, 8); REQUIRE_ALIGNED(p->positions, 8);
+    if (p->parents != nullptr) REQUIRE_ALIGNED(p->tree, 8);
+  }
+  if ((reinterpret_cast<uintptr_t>(p->parents) & 3u) != 0) return BURST_ERR_ALIGN;
+  int st;
+  if ((st = check_arch()) != BURST_OK) return st;
+  burst::PlanArgs a = {};
+  a.added = p->added; a.lengths = p->lengths; a.table = p->table; a.free_pages = p->free_pages; a.count = p->free_count; a.parents = p->parents;
+  a.starts = p->starts; a.totals = p->totals; a.slots = (long long*)p->slots; a.positions = (long long*)p->positions; a.tree = (unsigned long long*)p->tree;
+  a.table_stride = p->table_stride != 0 ? p->table_stride : p->width; a.parents_stride = p->parents_stride != 0 ? p->parents_stride : p->most;
+  a.sequences = p->sequences; a.rows = p->rows; a.pages = p->pages; a.page_shift = __builtin_ctz((unsigned)p->page); a.width = p->width;
+  a.words = p->parents != nullptr ? p->words : 0; a.most = p->most;
+  return burst::launch_plan(a, (hipStream_t)stream);
+}
+
+int burst_cache_keep(void* const* pools, int n, const int32_t* kept, int64_t kept_stride, int most, const int32_t* counts, int32_t* lengths_out,
+                     const burst_paged_params* p, void* stream) {
+  Paged g;
+  int st = check_paged(p, g, false);
+  if (st != BURST_OK) return st;
+  if (n < 0 || most < 0 || (kept_stride != 0 && kept_stride < most) || p->sequences > 65535) return BURST_ERR_SHAPE;
+  if (p->sequences == 0) return BURST_OK;
+  if (n > 0 && pools == nullptr) return BURST_ERR_NULL;
+  const unsigned size = p->dtype == BURST_BF16 ? 2 : 4;
+  try {
+    std::vector<void*> each(pools, pools + n);
+    if (p->pages > 0)
+      for (void* pool : each) REQUIRE_ALIGNED(pool, size);
+    std::sort(each.begin(), each.end());
+    if (p->pages > 0 && std::adjacent_find(each.begin(), each.end()) != each.end()) return BURST_ERR_SHAPE;   // (rows would move twice)
+  } catch (const std::bad_alloc&) {
+    return BURST_ERR_ALLOC;
+  }
+  REQUIRE_ALIGNED(p->starts, 4); REQUIRE_ALIGNED(p->lengths, 4); REQUIRE_ALIGNED(counts, 4); REQUIRE_ALIGNED(lengths_out, 4);
+  if (p->width > 0) REQUIRE_ALIGNED(p->table, 4);
+  if (most > 0) REQUIRE_ALIGNED(kept, 4);
+  if (lengths_out == p->lengths || lengths_out == counts) return BURST_ERR_SHAPE;
+  if ((st = check_arch()) != BURST_OK) return st;
+  burst::KeepArgs a = {};
+  a.starts = p->starts; a.lengths = p->lengths; a.table = p->table; a.kept = kept; a.counts = counts; a.out = lengths_out;
+  a.table_stride = g.table_stride; a.kept_stride = kept_stride != 0 ? kept_stride : most;
+  a.p_page = g.page[0]; a.p_head = g.page[1]; a.p_row = g.page[2];
+  a.sequences = p->sequences; a.rows = p->rows; a.cap = p->width * p->page; a.pages = p->pages; a.page_shift = g.page_shift; a.most = most;
+  a.heads = p->kv_heads; a.d = p->d;
+  const int all = p->pages > 0 ? n : 0;
+  return validated([&] {
+    int i = 0;
+    do {
+      a.pools = std::min(all - i, burst::kMaxKeepPools);
+      std::copy(pools + i, pools + i + a.pools, a.pool);
+      const int e = burst::launch_keep(a, (int)size, (hipStream_t)stream);
+      if (e != BURST_OK) return e;
+      i += a.pools;
+    } while (i < all);
+    return (int)BURST_OK;
+  });
 }
 
 size_t burst_paged_workspace_bytes(const burst_paged_params* p) {

@@ -818,6 +818,84 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   return {O, lse};
 }
 
+std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(const Tensor& added, const Tensor& lengths, const Tensor& table, const Tensor& free_pages,
+                                                                             const Tensor& free_count, int64_t page, int64_t rows,
+                                                                             const std::optional<Tensor>& parents, int64_t words) {
+  TORCH_CHECK_VALUE(table.is_cuda(), "table: device tensor expected");
+  for (const Tensor* t : {&added, &lengths, &table, &free_pages, &free_count})
+    TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == table.device(), "new, lengths, table, free, count: int32 tensors on one device expected");
+  TORCH_CHECK_VALUE(added.dim() == 1 && lengths.sizes() == added.sizes() && table.dim() == 2 && table.size(0) == added.size(0) && free_pages.dim() == 1 &&
+                    free_count.numel() == 1, "new, lengths [sequences], table [sequences, width], free [pages], count [1] expected");
+  TORCH_CHECK_VALUE(added.is_contiguous() && lengths.is_contiguous() && free_pages.is_contiguous() && (table.size(1) <= 1 || table.stride(1) == 1) &&
+                    (table.size(0) <= 1 || table.stride(0) >= table.size(1)), "new, lengths, free and the table's rows: contiguous expected");
+  fits_int(table);
+  fits_int(free_pages);
+  TORCH_CHECK_VALUE(added.size(0) <= 4096 && rows >= 0 && rows < 1 << 20, "at most 4096 sequences and 2^20 - 1 rows expected");
+  TORCH_CHECK_VALUE(page >= 16 && page < 1 << 30, "page: a power of two from 16 on expected");
+  // (tensors that are written must not be read as another: the same memory twice)
+  for (const Tensor* t : {&added, &lengths, &free_count}) TORCH_CHECK_VALUE(t->numel() == 0 || (t->data_ptr() != table.data_ptr() && t->data_ptr() != free_pages.data_ptr()),
+                                                                            "the table and the stack: memory of their own expected");
+  TORCH_CHECK_VALUE(table.numel() == 0 || table.data_ptr() != free_pages.data_ptr(), "the table and the stack: memory of their own expected");
+  if (parents.has_value()) {
+    TORCH_CHECK_VALUE(parents->scalar_type() == torch::kInt && parents->device() == table.device() && parents->dim() == 2 && parents->size(0) == added.size(0) &&
+                      (parents->size(1) <= 1 || parents->stride(1) == 1) && (parents->size(0) <= 1 || parents->stride(0) >= parents->size(1)),
+                      "parents: int32 [sequences, most] on the table's device, its rows contiguous, expected");
+    fits_int(*parents);
+    TORCH_CHECK_VALUE(words >= 1 && words <= 1 << 20, "words: at least one expected");
+  }
+  const c10::DeviceGuard on(table.device());
+  const auto i32 = table.options(), i64 = i32.dtype(torch::kLong);
+  Tensor starts = torch::empty({added.size(0) + 1}, i32), totals = torch::empty({added.size(0)}, i32), slots = torch::empty({rows}, i64), positions = torch::empty({rows}, i64);
+  std::optional<Tensor> tree;
+  burst_plan p{};
+  p.sequences = (int32_t)added.size(0); p.rows = (int32_t)rows; p.pages = (int32_t)free_pages.size(0); p.page = (int32_t)page; p.width = (int32_t)table.size(1);
+  p.added = added.data_ptr<int>(); p.lengths = lengths.data_ptr<int>(); p.table = table.data_ptr<int>(); p.free_pages = free_pages.data_ptr<int>();
+  p.free_count = free_count.data_ptr<int>();
+  p.table_stride = table.size(0) > 1 ? table.stride(0) : 0;
+  p.starts = starts.data_ptr<int>(); p.totals = totals.data_ptr<int>(); p.slots = slots.data_ptr<int64_t>(); p.positions = positions.data_ptr<int64_t>();
+  if (parents.has_value()) {
+    tree = torch::empty({rows, words}, i64);
+    p.words = (int32_t)words; p.most = (int32_t)parents->size(1); p.tree = tree->data_ptr<int64_t>();
+    p.parents_stride = parents->size(0) > 1 ? parents->stride(0) : 0;
+    static const int none = -1;                    // (not read: no columns, or no sequences)
+    p.parents = parents->numel() > 0 ? parents->data_ptr<int>() : &none;
+  }
+  check(burst_cache_plan(&p, stream_of(table)), "burst_cache_plan");
+  for (const Tensor* t : {&table, &free_pages, &free_count}) written(*t);
+  return {starts, totals, slots, positions, tree};
+}
+
+Tensor cache_keep(const std::vector<Tensor>& k_pages, const std::vector<Tensor>& v_pages, const Tensor& table, const Tensor& lengths, const Tensor& starts,
+                  const Tensor& kept, const Tensor& counts) {
+  TORCH_CHECK_VALUE(!k_pages.empty() && k_pages.size() == v_pages.size(), "as many v_pages as k_pages, one at least, expected");
+  burst_paged_params p = describe_paged(k_pages[0], v_pages[0], table, lengths, starts);
+  std::vector<void*> pools;
+  for (size_t i = 0; i < k_pages.size(); i++)
+    for (const Tensor* t : {&k_pages[i], &v_pages[i]}) {
+      TORCH_CHECK_VALUE(t->scalar_type() == k_pages[0].scalar_type() && t->device() == k_pages[0].device() && t->sizes() == k_pages[0].sizes() &&
+                        t->strides() == k_pages[0].strides(), "all layers' pages: like the first one's in type, sizes and strides expected");
+      refuse_tangent(*t);
+      TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && t->requires_grad()), "pages that require a gradient are not written");
+      for (void* other : pools) TORCH_CHECK_VALUE(t->numel() == 0 || other != t->data_ptr(), "pages: every layer's keys and values once expected");
+      pools.push_back(t->data_ptr());
+    }
+  for (const Tensor* t : {&kept, &counts})
+    TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == table.device(), "kept, counts: int32 tensors on the pages' device expected");
+  TORCH_CHECK_VALUE(kept.dim() == 2 && kept.size(0) == lengths.size(0) && counts.sizes() == lengths.sizes() && counts.is_contiguous() &&
+                    (kept.size(1) <= 1 || kept.stride(1) == 1) && (kept.size(0) <= 1 || kept.stride(0) >= kept.size(1)),
+                    "kept [sequences, most], its rows contiguous, counts [sequences] expected");
+  fits_int(kept);
+  const c10::DeviceGuard on(table.device());
+  p.rows = (1 << 30) - 1;                          // (there are no token tensors)
+  p.H = p.kv_heads;
+  Tensor out = torch::empty(lengths.sizes(), lengths.options());
+  check(burst_cache_keep(pools.data(), (int)pools.size(), kept.data_ptr<int>(), kept.size(0) > 1 ? kept.stride(0) : 0, (int)kept.size(1), counts.data_ptr<int>(),
+                         out.data_ptr<int>(), &p, stream_of(table)), "burst_cache_keep");
+  for (const auto* l : {&k_pages, &v_pages})
+    for (const Tensor& t : *l) written(t);
+  return out;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -825,6 +903,8 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("norm_rotate", &norm_rotate, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("rotate", &rotate, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("cache_append", &cache_append, pybind11::call_guard<pybind11::gil_scoped_release>());
+  m.def("cache_plan", &cache_plan, pybind11::call_guard<pybind11::gil_scoped_release>());
+  m.def("cache_keep", &cache_keep, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("paged_attention", &paged_attention, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("walk_forward", &walk_forward, pybind11::call_guard<pybind11::gil_scoped_release>());
   m.def("walk_backward", &walk_backward, pybind11::call_guard<pybind11::gil_scoped_release>());

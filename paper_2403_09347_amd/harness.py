@@ -374,17 +374,24 @@ class PagedWalk:
     """A cache in pages and what a step of serving does with it: the new tokens' keys and values are appended, rotated by their
     positions (turns: see rotary.rotary_turns; None: not rotated), and the new tokens attend to their sequences.  k_pages, v_pages, and
     the table, lengths and starts of a step, and full_p: see the paged module.  Nothing is kept but the pages: a captured step reads
-    its token tensors and the three arrays where they lie, and can be replayed with other contents."""
+    its token tensors and the three arrays where they lie, and can be replayed with other contents.
+    norms, eps: weights [d] of queries and keys, which are normalised before the rotation (see rotary.burst_norm_rotary)."""
 
-    def __init__(self, k_pages, v_pages, scale, turns=None, interleaved=False, amplitude=1.0, window=0, full_p=False):
+    def __init__(self, k_pages, v_pages, scale, turns=None, interleaved=False, amplitude=1.0, window=0, full_p=False, norms=None, eps=1e-6):
         self.k_pages, self.v_pages, self.scale, self.window, self.full_p = k_pages, v_pages, float(scale), int(window), bool(full_p)
         self.rotary = {} if turns is None else dict(turns=turns, interleaved=interleaved, amplitude=amplitude)
+        self.norms = {} if norms is None else dict(q_norm=norms[0], k_norm=norms[1], eps=eps)
 
-    def step(self, q, k, v, table, lengths, starts, max_new=0):
-        """q [rows, H, d], k, v [rows, kv_heads, d]; returns (O, lse) of the new tokens."""
-        turned = burst_cache_append(k, v, self.k_pages, self.v_pages, table, lengths, starts, q=q if self.rotary else None, **self.rotary)
+    def step(self, q, k, v, table, lengths, starts, max_new=0, slots=None, positions=None, tree=None):
+        """q [rows, H, d], k, v [rows, kv_heads, d]; returns (O, lse) of the new tokens.  slots, positions, tree: of paged.burst_cache_plan."""
+        turned = burst_cache_append(k, v, self.k_pages, self.v_pages, table, lengths, starts, q=q if self.rotary or self.norms else None, slots=slots,
+                                    positions=positions, **self.rotary, **self.norms)
         return burst_paged_attention(q if turned is None else turned, self.k_pages, self.v_pages, table, lengths, starts, self.scale,
-                                     window=self.window, max_new=max_new, full_p=self.full_p)
+                                     window=self.window, max_new=max_new, full_p=self.full_p, tree=tree)
+
+    def planned_step(self, q, k, v, table, plan, max_new=0):
+        """A step with a plan of paged.burst_cache_plan."""
+        return self.step(q, k, v, table, plan.lengths, plan.starts, max_new, plan.slots, plan.positions, plan.tree)
 
 
 class SpanWalk:

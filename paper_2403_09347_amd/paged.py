@@ -1,6 +1,6 @@
 """A cache of keys and values in pages, and attention of new tokens over it: what serves a sequence token by token (or a prompt
 chunk by chunk) after, or instead of, the walks over resident chunks.  Marshalling is native (csrc/burst_torch.cpp), the
-kernels are csrc/burst_rotary.hip and csrc/burst_paged.hip.
+kernels are csrc/burst_rotary.hip, csrc/burst_norm.hip, csrc/burst_paged.hip and csrc/burst_plan.hip.
 
 Several sequences at once: token tensors [rows, heads, d] hold the new tokens of sequence s in rows starts[s] .. starts[s + 1] - 1
 (views of a packed projection are read in place); lengths[s] counts all tokens of the sequence, the new ones among them; position p of
@@ -8,7 +8,14 @@ it is row p % page of page table[s, p // page] of k_pages and v_pages [pages, kv
 dimension; page: a power of two, 16 or more).  table, lengths and starts are int32 tensors on the device and are read there, so
 that a captured call can be replayed with other contents (they are not to change while a call runs); values outside their
 ranges are cut to them, a page that is not one of the pages holds no keys, nor does a position behind the table's row (new tokens there are
-not kept, and see the keys that are), and attention with starts that decrease writes nothing."""
+not kept, and see the keys that are), and attention with starts that decrease writes nothing.
+
+A step of serving with drafted tokens: burst_cache_plan (once), burst_cache_append and burst_paged_attention (in every layer), and when it is
+known which branch of every tree is right, burst_cache_keep (once, for all layers)."""
+from typing import NamedTuple, Optional
+
+import torch
+
 from . import binding as B
 
 
@@ -46,5 +53,43 @@ def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=Non
     try:
         return B.load_torch_module().paged_attention(q, k_pages, v_pages, table, lengths, starts, scale, bool(causal), int(window), int(max_new), out, lse,
                                                       bool(full_p), tree)
+    except RuntimeError as e:
+        raise B.from_native(e) from None
+
+
+class CachePlan(NamedTuple):
+    """What a step's calls read: starts [sequences + 1] and lengths [sequences] (int32; lengths with the new tokens), slots and positions [rows] (int64) of
+    burst_cache_append, and tree [rows, words] (int64; None without parents) of burst_paged_attention."""
+    starts: torch.Tensor
+    lengths: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+    tree: Optional[torch.Tensor]
+
+
+def burst_cache_plan(new, lengths, table, free, count, page, rows, parents=None, words=1):
+    """Plans a step on the device, from int32 tensors: new [sequences], the new tokens of each (negative: the sequence has ended), lengths [sequences], the tokens
+    that each has in the cache, table [sequences, width] (-1: no page), free [pages] and count [1], a stack of the pages that are free, its top at
+    count - 1.  rows: of the step's token tensors (up to 2^20 - 1; at most 4096 sequences).
+    Sequences are served in their order; one whose new tokens do not fit into the rows that are left, whose tokens do not fit into a row of the table, or that
+    lacks more pages than are free, is passed over (it has no new tokens in starts).  Entries of the table in which new tokens lie get a page where they
+    have none; ended sequences give theirs back first.  table, free and count are written; the same call again changes nothing.
+    parents: int32 [sequences, most], the new token (one before it) that each new token hangs on, -1: none; then the plan has the trees' masks of 64 * words bits,
+    and positions go by depth; sequences with more new tokens than that are chunks of prompts.  Returns a CachePlan; rows behind the last
+    sequence have slot and position -1.  One launch, two of more than 2048 rows."""
+    try:
+        return CachePlan(*B.load_torch_module().cache_plan(new, lengths, table, free, count, int(page), int(rows), parents, int(words)))
+    except RuntimeError as e:
+        raise B.from_native(e) from None
+
+
+def burst_cache_keep(k_pages, v_pages, table, lengths, starts, kept, counts):
+    """Keeps some of the new tokens of every sequence (a branch of its tree), in all layers at once: k_pages, v_pages, a tensor or a list of every layer's,
+    which lie alike; kept: int32 [sequences, most], the numbers of the tokens that are kept among the new ones, increasing; counts: int32 [sequences], how many.  Their
+    keys and values move to where the first new tokens were; returns the new lengths [sequences], int32 (the pages behind them stay in the table, for the next
+    tokens).  One launch (400 tensors each); no gradient."""
+    ks, vs = ([p] if isinstance(p, torch.Tensor) else list(p) for p in (k_pages, v_pages))
+    try:
+        return B.load_torch_module().cache_keep(ks, vs, table, lengths, starts, kept, counts)
     except RuntimeError as e:
         raise B.from_native(e) from None
