@@ -52,6 +52,21 @@ struct NormSlots {
 };
 template <typename T, int E>
 struct Granule { typedef __attribute__((ext_vector_type(E))) T vec; };
+// sum + the squares of a granule (bf16: two at a time, no conversions).
+template <typename T, int E>
+__device__ __forceinline__ float add_squares(const typename Granule<T, E>::vec& x, float sum) {
+  if constexpr (sizeof(T) == 2 && E > 1) {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const bf16x2 p = {x[e], x[e + 1]};
+      sum = __builtin_amdgcn_fdot2_f32_bf16(p, p, sum, false);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e++) sum = __builtin_fmaf((float)x[e], (float)x[e], sum);
+  }
+  return sum;
+}
 // Weights of a granule's columns.
 template <typename T, int E>
 __device__ __forceinline__ void load_weights(float (&out)[E], const NormItem& it, int c, bool there) {
@@ -169,12 +184,11 @@ norm_kernel(NormArgs a) {
   s.set(tid & (lanes - 1), it.lanes_shift, pairs, a.d);
   const bool row_there = r < t.rows;
 
-  const T* const x = (const T*)it.x + t.b * it.xs_b + (t.row0 + (row_there ? r : 0)) * it.xs_r;
+  const T* xh = (const T*)it.x + t.b * it.xs_b + (t.row0 + (row_there ? r : 0)) * it.xs_r + (t.h0 + sub) * it.xs_h;
   vec u[NH][N], v[NH][N];
 #pragma unroll
-  for (int j = 0; j < NH; j++) {
+  for (int j = 0; j < NH; j++, xh += subs * it.xs_h) {
     const int h = t.h0 + sub + j * subs;
-    const T* const xh = x + h * it.xs_h;
 #pragma unroll
     for (int k = 0; k < N; k++) {
       u[j][k] = v[j][k] = (vec)(T)0.f;
@@ -203,25 +217,32 @@ norm_kernel(NormArgs a) {
       const float2 cv = turn[some ? r * pairs + s.pair[k] + p : 0];
       cs[k][p] = some ? cv.x : 1.f; sn[k][p] = some ? cv.y : 0.f;
     }
-  const long long dst = row_there ? to[r] : -1;
-  T* const y = (T*)it.y + dst;
+  // (the weights go into cos and sin, which all heads share: r (x (w cos) - x' (w' sin)))
+  float wc1[N][E], wc2[N][E], ws1[N][E], ws2[N][E];
 #pragma unroll
-  for (int j = 0; j < NH; j++) {
+  for (int k = 0; k < N; k++)
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+      const int p = TWO ? e : e / 2, o = TWO ? e : e ^ 1;
+      wc1[k][e] = w1[k][e] * cs[k][p]; ws1[k][e] = (TWO ? w2[k][e] : w1[k][o]) * sn[k][p];
+      if (TWO) { wc2[k][e] = w2[k][e] * cs[k][p]; ws2[k][e] = w1[k][e] * sn[k][p]; }
+    }
+  const long long dst = row_there ? to[r] : -1;
+  T* yh = (T*)it.y + dst + (t.h0 + sub) * it.ys_h;
+#pragma unroll
+  for (int j = 0; j < NH; j++, yh += subs * it.ys_h) {
     const int h = t.h0 + sub + j * subs;
     float f = 1.f;
     if (it.normed) {
       float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < N; k++)
-#pragma unroll
-        for (int e = 0; e < E; e++) {
-          sum = __builtin_fmaf((float)u[j][k][e], (float)u[j][k][e], sum);
-          if (TWO) sum = __builtin_fmaf((float)v[j][k][e], (float)v[j][k][e], sum);
-        }
+      for (int k = 0; k < N; k++) {
+        sum = add_squares<T, E>(u[j][k], sum);
+        if (TWO) sum = add_squares<T, E>(v[j][k], sum);
+      }
       f = 1.f / sqrtf(group_sum(sum, it.lanes_shift) / (float)a.d + a.eps);
     }
     if (dst < 0 || h >= it.heads) continue;
-    T* const yh = y + h * it.ys_h;
 #pragma unroll
     for (int k = 0; k < N; k++) {
       if (!s.there[k]) continue;
@@ -235,18 +256,18 @@ norm_kernel(NormArgs a) {
       } else if constexpr (TWO) {
 #pragma unroll
         for (int e = 0; e < E; e++) {
-          const float p = (float)u[j][k][e] * f * w1[k][e], q = (float)v[j][k][e] * f * w2[k][e];
-          o1[e] = (T)(p * cs[k][e] - q * sn[k][e]);
-          o2[e] = (T)(q * cs[k][e] + p * sn[k][e]);
+          const float p = (float)u[j][k][e], q = (float)v[j][k][e];
+          o1[e] = (T)(f * (p * wc1[k][e] - q * ws1[k][e]));
+          o2[e] = (T)(f * (q * wc2[k][e] + p * ws2[k][e]));
         }
         *reinterpret_cast<vec*>(yh + s.c1[k]) = o1;
         *reinterpret_cast<vec*>(yh + s.c2[k]) = o2;
       } else {
 #pragma unroll
         for (int e = 0; e < P; e++) {
-          const float p = (float)u[j][k][2 * e] * f * w1[k][2 * e], q = (float)u[j][k][2 * e + 1] * f * w1[k][2 * e + 1];
-          o1[2 * e] = (T)(p * cs[k][e] - q * sn[k][e]);
-          o1[2 * e + 1] = (T)(q * cs[k][e] + p * sn[k][e]);
+          const float p = (float)u[j][k][2 * e], q = (float)u[j][k][2 * e + 1];
+          o1[2 * e] = (T)(f * (p * wc1[k][2 * e] - q * ws1[k][2 * e]));
+          o1[2 * e + 1] = (T)(f * (q * wc1[k][2 * e + 1] + p * ws1[k][2 * e + 1]));
         }
         *reinterpret_cast<vec*>(yh + s.c1[k]) = o1;
       }
@@ -254,10 +275,11 @@ norm_kernel(NormArgs a) {
   }
 }
 
-// The gradient, tiles as above, several a workgroup, which keeps the sums of dw over all of them: its rows' lanes each have a part of them, which
-// are added up in LDS at the end and left in `part`, a row for every workgroup.
-template <typename T, int E, bool INTER, int NH>
-__global__ void __launch_bounds__(kNormThreads)
+// The gradient.  Tiles as above with one head a thread; a workgroup takes several, one after the other: the next one's rows are asked for before this one's
+// are worked on, and neighbouring tiles are other heads of the same rows, whose cos and sin stay.  It keeps the sums of dw over all of its tiles:
+// its rows' lanes each have a part of them, which are added up in LDS at the end and left in `part`, a row for every workgroup.
+template <typename T, int E, bool INTER>
+__global__ void __launch_bounds__(kNormThreads, 3)
 norm_bwd_kernel(NormArgs a) {
   typedef NormSlots<E, INTER> Slots;
   typedef typename Granule<T, E>::vec vec;
@@ -272,11 +294,41 @@ norm_bwd_kernel(NormArgs a) {
   const NormItem& it = a.it[i];
   const int lanes = 1 << it.lanes_shift, pairs = it.rotated ? a.dims / 2 : 0;
   const int rs = tid >> it.lanes_shift, r = rs & ((1 << it.rows_shift) - 1), sub = rs >> it.rows_shift;
-  const int subs = kNormThreads >> (it.lanes_shift + it.rows_shift);
-  const int tiles = it.B * it.row_tiles * it.head_tiles, first = (bid - it.first_block) * a.tiles_each;
+  const int first = (bid - it.first_block) * a.tiles_each, tiles = min(a.tiles_each, it.B * it.row_tiles * it.head_tiles - first);
+  const int heads = kNormThreads >> (it.lanes_shift + it.rows_shift);   // of a tile
   Slots s;
   s.set(tid & (lanes - 1), it.lanes_shift, pairs, a.d);
-  float w1[N][E], w2[N][E], d1[N][E], d2[N][E];
+  // the tile whose rows are asked for: its heads' number ht of the rows' number rt of batch entry b
+  vec u[N], v[N], gu[N], gv[N];
+  int ht = first % it.head_tiles, rt = first / it.head_tiles, b = rt / it.row_tiles;
+  rt -= b * it.row_tiles;
+  const T *x, *g;
+  int rows;
+  auto enter = [&]() __attribute__((always_inline)) {   // the first of some rows' tiles
+    const int row0 = rt << it.rows_shift;
+    rows = min(1 << it.rows_shift, it.rows - row0);
+    const long long row = row0 + (r < rows ? r : 0), h = ht * heads + sub;
+    x = (const T*)it.x + b * it.xs_b + row * it.xs_r + h * it.xs_h;
+    g = (const T*)it.g + b * it.gs_b + row * it.gs_r + h * it.gs_h;
+  };
+  auto fetch = [&]() __attribute__((always_inline)) {
+    const bool there = r < rows && ht * heads + sub < it.heads;
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+      u[k] = v[k] = gu[k] = gv[k] = (vec)(T)0.f;
+      if (there && s.there[k]) {
+        u[k] = *reinterpret_cast<const vec*>(x + s.c1[k]);
+        gu[k] = *reinterpret_cast<const vec*>(g + s.c1[k]);
+        if (TWO && s.turned[k]) {
+          v[k] = *reinterpret_cast<const vec*>(x + s.c2[k]);
+          gv[k] = *reinterpret_cast<const vec*>(g + s.c2[k]);
+        }
+      }
+    }
+  };
+  enter();
+  fetch();
+  float w1[N][E], w2[N][E], d1[N][E], d2[N][E], cs[N][P], sn[N][P];
 #pragma unroll
   for (int k = 0; k < N; k++) {
     load_weights<T, E>(w1[k], it, s.c1[k], s.there[k]);
@@ -284,102 +336,97 @@ norm_bwd_kernel(NormArgs a) {
 #pragma unroll
     for (int e = 0; e < E; e++) d1[k][e] = d2[k][e] = 0.f;
   }
+  const float inv_d = 1.f / (float)a.d;
+  bool other = true;                               // other rows than those that cos and sin are of
+  T* y = nullptr;
 #pragma unroll 1
-  for (int tile = first; tile < min(first + a.tiles_each, tiles); tile++) {
-    const NormTile t = tile_of(a, it, tile);
-    const bool row_there = r < t.rows;
-    const long long row = t.row0 + (row_there ? r : 0);
-    const T* const x = (const T*)it.x + t.b * it.xs_b + row * it.xs_r;
-    const T* const g = (const T*)it.g + t.b * it.gs_b + row * it.gs_r;
-    vec u[NH][N], v[NH][N], gu[NH][N], gv[NH][N];
+  for (int tile = 0; tile < tiles; tile++) {
+    const int h = ht * heads + sub;
+    const bool row_there = r < rows, store = it.y != nullptr && row_there && h < it.heads;
+    if (other) {
+      __syncthreads();                             // (the rows before have been read)
+      find_rows(a, it, b, rt << it.rows_shift, rows, at, to);
+      __syncthreads();
+      if (pairs > 0) {
+        find_turns(a, pairs, rows, at, sh.turn);
+        __syncthreads();
+      }
+      y = (T*)it.y + (row_there ? to[r] : 0) + h * it.ys_h;
 #pragma unroll
-    for (int j = 0; j < NH; j++) {
-      const int h = t.h0 + sub + j * subs;
-      const T *const xh = x + h * it.xs_h, *const gh = g + h * it.gs_h;
+      for (int k = 0; k < N; k++)
 #pragma unroll
-      for (int k = 0; k < N; k++) {
-        u[j][k] = v[j][k] = gu[j][k] = gv[j][k] = (vec)(T)0.f;
-        if (row_there && h < it.heads && s.there[k]) {
-          u[j][k] = *reinterpret_cast<const vec*>(xh + s.c1[k]);
-          gu[j][k] = *reinterpret_cast<const vec*>(gh + s.c1[k]);
-          if (TWO && s.turned[k]) {
-            v[j][k] = *reinterpret_cast<const vec*>(xh + s.c2[k]);
-            gv[j][k] = *reinterpret_cast<const vec*>(gh + s.c2[k]);
-          }
+        for (int p = 0; p < P; p++) {
+          const bool some = row_there && s.turned[k];
+          const float2 cv = sh.turn[some ? r * pairs + s.pair[k] + p : 0];
+          cs[k][p] = some ? cv.x : 1.f; sn[k][p] = some ? cv.y : 0.f;
+        }
+    }
+    vec x1[N], x2[N];
+    float h1[N][E], h2[N][E], ss = 0.f, ux = 0.f;  // R^T g; sums of x^2 and of u x
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+      x1[k] = u[k]; x2[k] = v[k];
+      if constexpr (TWO) {
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+          const float p = (float)gu[k][e], q = (float)gv[k][e];
+          h1[k][e] = p * cs[k][e] + q * sn[k][e];
+          h2[k][e] = q * cs[k][e] - p * sn[k][e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < P; e++) {
+          const float p = (float)gu[k][2 * e], q = (float)gu[k][2 * e + 1];
+          h1[k][2 * e] = p * cs[k][e] + q * sn[k][e];
+          h1[k][2 * e + 1] = q * cs[k][e] - p * sn[k][e];
         }
       }
     }
-    find_rows(a, it, t.b, t.row0, t.rows, at, to);
-    __syncthreads();
-    if (pairs > 0) find_turns(a, pairs, t.rows, at, sh.turn);
-    __syncthreads();
-    float cs[N][P], sn[N][P];
-#pragma unroll
-    for (int k = 0; k < N; k++)
-#pragma unroll
-      for (int p = 0; p < P; p++) {
-        const bool some = row_there && s.turned[k];
-        const float2 cv = sh.turn[some ? r * pairs + s.pair[k] + p : 0];
-        cs[k][p] = some ? cv.x : 1.f; sn[k][p] = some ? cv.y : 0.f;
+    other = ht + 1 == it.head_tiles;
+    if (tile + 1 < tiles) {
+      if (other) {
+        ht = 0;
+        if (++rt == it.row_tiles) { rt = 0; b++; }
+        enter();
+      } else {
+        ht++;
+        x += heads * it.xs_h;
+        g += heads * it.gs_h;
       }
-    T* const y = (T*)it.y + (row_there ? to[r] : 0);
+      fetch();
+    }
 #pragma unroll
-    for (int j = 0; j < NH; j++) {
-      const int h = t.h0 + sub + j * subs;
-      float h1[N][E], h2[N][E], ss = 0.f, ux = 0.f;   // R^T g; sums of x^2 and of u x
+    for (int k = 0; k < N; k++) {
+      ss = add_squares<T, E>(x1[k], ss);
+      if (TWO) ss = add_squares<T, E>(x2[k], ss);
 #pragma unroll
-      for (int k = 0; k < N; k++) {
-        if constexpr (TWO) {
-#pragma unroll
-          for (int e = 0; e < E; e++) {
-            const float p = (float)gu[j][k][e], q = (float)gv[j][k][e];
-            h1[k][e] = p * cs[k][e] + q * sn[k][e];
-            h2[k][e] = q * cs[k][e] - p * sn[k][e];
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < P; e++) {
-            const float p = (float)gu[j][k][2 * e], q = (float)gu[j][k][2 * e + 1];
-            h1[k][2 * e] = p * cs[k][e] + q * sn[k][e];
-            h1[k][2 * e + 1] = q * cs[k][e] - p * sn[k][e];
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < E; e++) {
-          const float x1 = (float)u[j][k][e];
-          ss = __builtin_fmaf(x1, x1, ss);
-          ux = __builtin_fmaf(h1[k][e] * w1[k][e], x1, ux);
-          if (TWO) {
-            const float x2 = (float)v[j][k][e];
-            ss = __builtin_fmaf(x2, x2, ss);
-            ux = __builtin_fmaf(h2[k][e] * w2[k][e], x2, ux);
-          }
-        }
-      }
-      const float inv_d = 1.f / (float)a.d;
-      const float f = 1.f / sqrtf(group_sum(ss, it.lanes_shift) / (float)a.d + a.eps);
-      const float c = group_sum(ux, it.lanes_shift) * inv_d * f * f;
-      const bool store = it.y != nullptr && row_there && h < it.heads;
-#pragma unroll
-      for (int k = 0; k < N; k++) {
-        vec o1, o2;
-#pragma unroll
-        for (int e = 0; e < E; e++) {
-          const float x1 = (float)u[j][k][e];
-          d1[k][e] = __builtin_fmaf(h1[k][e], x1 * f, d1[k][e]);
-          o1[e] = (T)(f * (h1[k][e] * w1[k][e] - x1 * c));
-          if (TWO) {
-            const float x2 = (float)v[j][k][e];
-            d2[k][e] = __builtin_fmaf(h2[k][e], x2 * f, d2[k][e]);
-            o2[e] = (T)(f * (h2[k][e] * w2[k][e] - x2 * c));
-          }
-        }
-        if (store && s.there[k]) {
-          *reinterpret_cast<vec*>(y + h * it.ys_h + s.c1[k]) = o1;
-          if (TWO && s.turned[k]) *reinterpret_cast<vec*>(y + h * it.ys_h + s.c2[k]) = o2;
-        }
+      for (int e = 0; e < E; e++) {
+        ux = __builtin_fmaf(h1[k][e] * (float)x1[k][e], w1[k][e], ux);
+        if (TWO) ux = __builtin_fmaf(h2[k][e] * (float)x2[k][e], w2[k][e], ux);
       }
     }
+    const float f = 1.f / sqrtf(group_sum(ss, it.lanes_shift) / (float)a.d + a.eps);
+    const float c = group_sum(ux, it.lanes_shift) * inv_d * f * f;
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+      vec o1, o2;
+#pragma unroll
+      for (int e = 0; e < E; e++) {
+        const float f1 = (float)x1[k][e];
+        d1[k][e] = __builtin_fmaf(h1[k][e] * f1, f, d1[k][e]);
+        o1[e] = (T)(f * (h1[k][e] * w1[k][e] - f1 * c));
+        if (TWO) {
+          const float f2 = (float)x2[k][e];
+          d2[k][e] = __builtin_fmaf(h2[k][e] * f2, f, d2[k][e]);
+          o2[e] = (T)(f * (h2[k][e] * w2[k][e] - f2 * c));
+        }
+      }
+      if (store && s.there[k]) {
+        *reinterpret_cast<vec*>(y + s.c1[k]) = o1;
+        if (TWO && s.turned[k]) *reinterpret_cast<vec*>(y + s.c2[k]) = o2;
+      }
+    }
+    y += heads * it.ys_h;
   }
   if (it.part < 0) return;
   __syncthreads();                                 // (the last tile's cos and sin have been read)
@@ -426,6 +473,7 @@ norm_sums_kernel(NormSums a) {
   }
 }
 
+constexpr int kBackBlocks = 768;                   // workgroups of a backward launch: three a CU, as many as are there at once
 long long set_tiles(NormArgs& a, int dtype, bool backward) {
   const int size = dtype == BURST_BF16 ? 2 : 4;
   // Granules of 16 bytes (bf16: else 8): every one of a row starts on its own size, and no pair is cut by one.
@@ -443,7 +491,7 @@ long long set_tiles(NormArgs& a, int dtype, bool backward) {
   const int E = a.granule;
   double all = 0;                                  // rows x heads
   for (int i = 0; i < a.n; i++) all += (double)a.it[i].B * a.it[i].rows * a.it[i].heads;
-  a.heads_each = all >= 32768 ? 4 : 1;
+  a.heads_each = !backward && all >= 32768 ? 4 : 1;
   long long blocks = 0;
   auto lay = [&](int tiles_each) {
     blocks = 0;
@@ -469,8 +517,8 @@ long long set_tiles(NormArgs& a, int dtype, bool backward) {
   };
   a.tiles_each = 1;
   lay(1);
-  if (backward && blocks > 1280) {                 // about five workgroups a CU: what they leave has to be added up
-    a.tiles_each = (int)((blocks + 1279) / 1280);
+  if (backward && blocks > kBackBlocks) {
+    a.tiles_each = (int)((blocks + kBackBlocks - 1) / kBackBlocks);
     lay(a.tiles_each);
   }
   return blocks;
@@ -479,8 +527,7 @@ long long set_tiles(NormArgs& a, int dtype, bool backward) {
 template <typename T, int E, bool INTER>
 static void enqueue(const NormArgs& a, bool backward, long long blocks, hipStream_t s) {
   const dim3 grid((unsigned)blocks), block(kNormThreads);
-  if (backward && a.heads_each > 1) BURST_LAUNCH((norm_bwd_kernel<T, E, INTER, 4>), grid, block, 0, s, a);
-  else if (backward) BURST_LAUNCH((norm_bwd_kernel<T, E, INTER, 1>), grid, block, 0, s, a);
+  if (backward) BURST_LAUNCH((norm_bwd_kernel<T, E, INTER>), grid, block, 0, s, a);
   else if (a.heads_each > 1) BURST_LAUNCH((norm_kernel<T, E, INTER, 4>), grid, block, 0, s, a);
   else BURST_LAUNCH((norm_kernel<T, E, INTER, 1>), grid, block, 0, s, a);
 }

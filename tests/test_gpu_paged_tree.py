@@ -29,7 +29,7 @@ def check(b, window=0, name="", **kw):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [8, 32, 64, 80, 96, 104, 128])
-@pytest.mark.parametrize("H,KV", [(2, 2), (8, 2), (3, 1)])
+@pytest.mark.parametrize("H,KV", [(2, 2), (8, 2), (3, 1), (17, 1)])
 def test_kernels(dtype, d, H, KV):
     """Few rows a sequence (the short kernel; max_new tells it), and more."""
     for lengths, news, most in (([40, 5, 130, 3], [4, 4, 2, 3], 4), ([70, 300, 5, 129], [40, 64, 5, 1], 0)):
@@ -211,9 +211,17 @@ def test_errors():
 
 
 def test_c_entry():
-    b = TreeBatch([200, 31], [20, 31], 4, 2, 64, seed=1)
-    p = B.paged_params(51, 4, 2, 64, BF16, b.k_pages, b.table, b.lengths, b.starts, scale=b.scale)
-    O, lse = torch.empty_like(b.q), torch.empty(51, 4, device=DEV)
-    ws = torch.empty(B.burst_paged_workspace_bytes(p), dtype=torch.uint8, device=DEV)
-    B.burst_paged_tree_fwd(b.q, b.k_pages, b.v_pages, O, lse, b.tree, p, ws)
-    b.check(O, lse)
+    """With a workspace of exactly the size that it asks for, between guards."""
+    for dtype, H, news in ((BF16, 4, [1, 2]), (BF16, 4, [20, 31]), (BF16, 16, [20, 31]), (F32, 4, [20, 31]), (F32, 2, [1, 2])):
+        b = TreeBatch([2000, 900], news, H, 2, 64, dtype=dtype, seed=1)
+        T = sum(news)
+        p = B.paged_params(T, H, 2, 64, dtype, b.k_pages, b.table, b.lengths, b.starts, scale=b.scale, max_new=max(news))
+        O, lse = torch.full((T + 8, H, 64), 3.0, dtype=dtype, device=DEV), torch.full((T + 8, H), 3.0, device=DEV)
+        need = B.burst_paged_workspace_bytes(p)
+        ws = torch.full((need + 8192,), 77, dtype=torch.uint8, device=DEV)
+        B.burst_paged_tree_fwd(b.q, b.k_pages, b.v_pages, O[4:-4], lse[4:-4], b.tree, p, ws[4096:4096 + need])
+        b.check(O[4:-4], lse[4:-4])
+        assert (ws[:4096] == 77).all() and (ws[4096 + need:] == 77).all()
+        assert (O[:4] == 3).all() and (O[-4:] == 3).all() and (lse[:4] == 3).all() and (lse[-4:] == 3).all()
+        with pytest.raises(B.BurstError):
+            B.burst_paged_tree_fwd(b.q, b.k_pages, b.v_pages, O[4:-4], lse[4:-4], b.tree, p, ws[4096:4096 + need - 16])
