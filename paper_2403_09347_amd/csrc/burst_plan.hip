@@ -1,7 +1,7 @@
 // The books of a paged cache: what the calls of a step read, made from the lengths of its sequences (burst_cache_plan), and the rows of
 // drafted tokens that are kept, moved together (burst_cache_keep).
 // Bound by latency: nearly nothing is read, but one thing tells where the next one is.  Measured: a plan of 256 single tokens 5.2 us, of 400 sequences with
-// trees and prompts, 128 thousand rows, 10 + 6.3 (20 when every page is new); the kept rows of 96 trees in 24 layers, 8 heads, 37 us.
+// trees and prompts, 128 thousand rows, 10 + 4 (20 when every page is new); the kept rows of 96 trees in 24 layers, 8 heads, 37 us.
 #include "burst_paged_kernels.h"
 #include "burst_plan.h"
 
@@ -282,8 +282,8 @@ plan_kernel(PlanArgs a) {
 }
 
 // The rows of a call of many, and behind them the trees.
-constexpr int kFillRows = 1024;                    // of a workgroup
-__global__ void __launch_bounds__(256)
+constexpr int kFillRows = 256;                     // of a workgroup: one a thread (128 thousand rows: four a thread 16.7 us a call, two 14.6, so 13.7)
+__global__ void __launch_bounds__(kFillRows)
 plan_rows_kernel(PlanArgs a, int row_blocks) {
   if ((int)blockIdx.x >= row_blocks) {             // a sequence a wavefront
     const int s = ((int)blockIdx.x - row_blocks) * 4 + (threadIdx.x >> 6);
@@ -293,18 +293,17 @@ plan_rows_kernel(PlanArgs a, int row_blocks) {
     return;
   }
   __shared__ int start[kPlanSequences + 1];
-  for (int s = threadIdx.x; s <= a.sequences; s += 256) start[s] = a.starts[s];
+  for (int s = threadIdx.x; s <= a.sequences; s += kFillRows) start[s] = a.starts[s];
   __syncthreads();
-  const int end = min(((int)blockIdx.x + 1) * kFillRows, a.rows);
-  for (int row = blockIdx.x * kFillRows + threadIdx.x; row < end; row += 256)
-    fill_row(a, row, start, [&](int s, int n) { return a.totals[s] - n; });
+  const int row = blockIdx.x * kFillRows + threadIdx.x;
+  if (row < a.rows) fill_row(a, row, start, [&](int s, int n) { return a.totals[s] - n; });
 }
 
 int launch_plan(const PlanArgs& a, hipStream_t s) {
   BURST_LAUNCH(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
   if (a.rows > kPlanRows) {
     const int blocks = (a.rows + kFillRows - 1) / kFillRows, trees = a.parents != nullptr ? (a.sequences + 3) / 4 : 0;
-    BURST_LAUNCH(plan_rows_kernel, dim3((unsigned)(blocks + trees)), dim3(256), 0, s, a, blocks);
+    BURST_LAUNCH(plan_rows_kernel, dim3((unsigned)(blocks + trees)), dim3(kFillRows), 0, s, a, blocks);
   }
   return launch_status();
 }
