@@ -385,7 +385,7 @@ typedef struct burst_store {
   float   eps;                                  /* of the norms, > 0 if there are any */
   int32_t reserved;                             /* 0 */
   const int64_t* slots;                         /* DEVICE [rows]: row i's key and value go to row slots[i] % page of page slots[i] / page, instead of by the
-                                                 * table; negative, or in a page that is none: left out */
+                                                 * table; negative, or in a page that is none: left out.  No two rows go to one place */
   const int64_t* positions;                     /* DEVICE [rows]: positions of the rotation, instead of the place in the sequence; negative: the row is left out */
   const int64_t* offsets;                       /* as burst_cache_append's; NULL if there are positions */
 } burst_store;

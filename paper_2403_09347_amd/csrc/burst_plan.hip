@@ -68,7 +68,7 @@ __device__ __forceinline__ void fill_row(const PlanArgs& a, int row, const int* 
   a.positions[row] = pos;
 }
 // Positions and masks of a tree of n <= 64 tokens, by a wavefront: every token takes over what the token that it has come to sees, and goes on to where that one
-// has come to, twice as far each time.  (Going up branch by branch, a load each step, the rows of 400 sequences took 12.8 us; so 6.3.)
+// has come to, twice as far each time.  (Going up branch by branch, a load each step, the rows of 400 sequences took 12.8 us; so 6.3, of which the rest is rows of chunks.)
 __device__ __forceinline__ void fill_tree(const PlanArgs& a, int s, int first, int n, int base) {
   const int t = threadIdx.x & 63, up = t < n && t < a.most ? a.parents[(long long)s * a.parents_stride + t] : -1;
   int at = up >= 0 && up < t ? up : -1;

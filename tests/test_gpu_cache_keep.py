@@ -119,6 +119,16 @@ def test_anything_in_the_lists_stays_among_the_new_tokens():
         torch.cuda.synchronize()
 
 
+def test_nothing_is_kept():
+    b = make([40, 9], [20, 9])[0]
+    before = [b.k_pages.clone(), b.v_pages.clone()]
+    for kept, counts in ((torch.zeros(2, 0, dtype=torch.int32, device=DEV), i32([5, 0])), (i32([[3], [1]]), i32([0, 0]))):
+        assert burst_cache_keep(b.k_pages, b.v_pages, b.table, b.lengths, b.starts, kept, counts).tolist() == [20, 0]
+        assert torch.equal(b.k_pages, before[0]) and torch.equal(b.v_pages, before[1])
+    none = torch.zeros(0, 2, 16, 64, dtype=BF16, device=DEV)
+    assert burst_cache_keep(none, none, b.table, b.lengths, b.starts, i32([[3], [1]]), i32([1, 1])).tolist() == [21, 1]
+
+
 def test_captured():
     news, lengths = [20, 33], [60, 33]
     b = make(lengths, news)[0]
