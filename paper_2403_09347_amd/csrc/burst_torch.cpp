@@ -499,6 +499,7 @@ struct NormRotaryBackward : public torch::autograd::Node {
     }
     if (like == nullptr) return out;
     const c10::DeviceGuard on(like->device());
+    refuse_outside_of_capture();
     Tensor t;
     variable_list given(x);                        // (as they are part of a graph)
     given.insert(given.end(), g.begin(), g.end());
@@ -549,6 +550,19 @@ struct NormRotaryBackward : public torch::autograd::Node {
       for (Tensor& v : out) if (v.defined()) torch::autograd::set_history(v, end);
     }
     return out;
+  }
+  // Gradients of a captured pass go to nodes of their own streams.  A leaf whose node was made by an earlier graph on the default stream, and lives because
+  // that graph does, has the engine make that stream wait for the captured one, which no capture allows and the process may not survive.
+  void refuse_outside_of_capture() const {
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
+    for (size_t i = 0; i < num_outputs(); i++) {
+      const auto& to = next_edge(i).function;
+      if (to == nullptr || !task_should_compute_output(i)) continue;
+      const auto stream = to->stream();
+      TORCH_CHECK(!stream.has_value() || stream->id() != c10::hip::getDefaultHIPStream(stream->device_index()).id(),
+                  "burst_norm_rotary: a captured backward pass whose gradients go to a graph that was made on the default stream and still lives (let it go "
+                  "before the capture, or make its tensors' graph in it)");
+    }
   }
   void release_variables() override {
     const std::lock_guard<std::mutex> lock(mutex_);

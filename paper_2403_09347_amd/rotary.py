@@ -57,7 +57,8 @@ def burst_norm_rotary(x, weights, turns=None, eps=1e-6, offset=0, positions=None
     burst_rotary does (turns, offset, positions, interleaved, amplitude: see there; turns=None: not rotated), out of place, by one launch (12
     tensors each).  All of it in 32 bits (the angles in 64), rounded once; sums of squares beyond 32 bits' range count as infinite.  Returns a
     tensor or a list; results lie in memory like x.  Gradients flow to x and to the weights, whose gradients are summed in fp32 over all rows of all
-    tensors that share them (the same tensor in the list) and rounded once; gradients of gradients are an error."""
+    tensors that share them (the same tensor in the list) and rounded once; gradients of gradients are an error, and so is a captured backward pass
+    to tensors that an earlier graph, made on the default stream, still holds."""
     one = isinstance(x, torch.Tensor)
     xs = [x] if one else list(x)
     ws = [weights] * len(xs) if weights is None or isinstance(weights, torch.Tensor) else list(weights)

@@ -267,6 +267,34 @@ def test_captured_pass_with_other_contents():
         assert all(torch.equal(a, b) for a, b in zip(out, want)), seed
 
 
+def test_captured_pass_beside_a_graph_of_the_same_leaves_that_lives():
+    """The leaves' nodes are then the earlier graph's, on the default stream, which must not wait for a captured one: an error before it would, with
+    nothing lost; when that graph is gone, passes are captured."""
+    x, w, g = rand(1, 4, 100, 64, dtype=BF16).requires_grad_(True), weight(64).requires_grad_(True), rand(1, 4, 100, 64, dtype=BF16, seed=1)
+    turns = default_turns(64)
+    early = burst_norm_rotary(x, w, turns, EPS, 9)
+    want = [early.detach(), *torch.autograd.grad(early, [x, w], g, retain_graph=True)]
+    torch.cuda.synchronize()
+    for wanted in ([x, w], [x], [w]):
+        with pytest.raises(RuntimeError, match="captured backward pass"):
+            with torch.cuda.graph(torch.cuda.CUDAGraph()):
+                torch.autograd.grad(burst_norm_rotary(x, w, turns, EPS, 9), wanted, g)
+    torch.cuda.synchronize()
+    again = torch.autograd.grad(early, [x, w], g)
+    assert all(torch.equal(a, b) for a, b in zip(again, want[1:]))
+    del early
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = burst_norm_rotary(x, w, turns, EPS, 9)
+        out = [y.detach(), *torch.autograd.grad(y, [x, w], g)]
+    for _ in range(3):
+        for o in out:
+            o.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
 def test_c_entries_in_place_and_without_some_gradients():
     x, w, g, turns = rand(1, 3, 21, 64), weight(64), rand(1, 3, 21, 64, seed=1), default_turns(64)
     r = B.rotary(turns, amplitude=1.5)
