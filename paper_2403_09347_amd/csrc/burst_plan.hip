@@ -155,7 +155,7 @@ plan_kernel(PlanArgs a) {
           const bool is = checked_page(page[k], a.pages) >= 0;
           const unsigned long long bal = __builtin_amdgcn_ballot_w64(is);
           const int at = to + __builtin_popcountll(bal & ((1ull << lane) - 1));
-          if (is && at < a.pages) a.free_pages[at] = page[k];
+          if (is && (unsigned)at < (unsigned)a.pages) a.free_pages[at] = page[k];   // (a page that several entries name can come back more often than there is room)
           if (c < a.width && page[k] != -1) row[c] = -1;
           to += __builtin_popcountll(bal);
         }

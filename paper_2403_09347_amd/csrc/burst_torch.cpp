@@ -855,6 +855,8 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(con
                       (parents->size(1) <= 1 || parents->stride(1) == 1) && (parents->size(0) <= 1 || parents->stride(0) >= parents->size(1)),
                       "parents: int32 [sequences, most] on the table's device, its rows contiguous, expected");
     fits_int(*parents);
+    TORCH_CHECK_VALUE(parents->numel() == 0 || (parents->data_ptr() != table.data_ptr() && parents->data_ptr() != free_pages.data_ptr()),
+                      "the table and the stack: memory of their own expected");
     TORCH_CHECK_VALUE(words >= 1 && words <= 1 << 20, "words: at least one expected");
   }
   const c10::DeviceGuard on(table.device());

@@ -69,7 +69,7 @@ class CachePlan(NamedTuple):
 
 def burst_cache_plan(new, lengths, table, free, count, page, rows, parents=None, words=1):
     """Plans a step on the device, from int32 tensors: new [sequences], the new tokens of each (negative: the sequence has ended), lengths [sequences], the tokens
-    that each has in the cache, table [sequences, width] (-1: no page), free [pages] and count [1], a stack of the pages that are free, its top at
+    that each has in the cache, table [sequences, width] (-1: no page; a page is one entry's, or the stack's), free [pages] and count [1], a stack of the pages that are free, its top at
     count - 1.  rows: of the step's token tensors (up to 2^20 - 1; at most 4096 sequences).
     Sequences are served in their order; one whose new tokens do not fit into the rows that are left, whose tokens do not fit into a row of the table, or that
     lacks more pages than are free, is passed over (it has no new tokens in starts).  Entries of the table in which new tokens lie get a page where they

@@ -160,7 +160,7 @@ def test_errors():
     burst_cache_plan(**good)
     for bad in (dict(new=new.long()), dict(new=new[:1]), dict(lengths=lengths.cpu()), dict(table=table[0]), dict(table=table[:1]), dict(free=table), dict(count=new), dict(rows=-1),
                 dict(rows=1 << 20), dict(page=8), dict(page=24), dict(page=1 << 30), dict(free=free[::2]), dict(table=table.expand(2, 5)), dict(parents=table.long()), dict(parents=table[:1]),
-                dict(parents=table, words=0), dict(free=lengths), dict(table=table[:, :0], page=0)):
+                dict(parents=table.clone(), words=0), dict(parents=table), dict(parents=free[:2, None]), dict(free=lengths), dict(table=table[:, :0], page=0)):
         with pytest.raises((ValueError, B.BurstError)):
             burst_cache_plan(**dict(good, **bad))
     version = table._version
