@@ -141,8 +141,7 @@ def _news(c):
 def work(case):
     """Every input read once and every output written once.  norm: x and y, then x, g and dx, 30 operations a value.  tree: the keys
     and values that some new token sees, 4 d operations a visible pair and query head (half of a tree's pairs taken for visible).  plan: what a
-    sequence and a row have in the arrays, and the table's entries that rows lie in.  keep: the rows of a branch (a token t has t / ((bushy + 1) / 2)
-before it in the mean, and the branch's last one is any of the n)."""
+    sequence and a row have in the arrays, and the table's entries that rows lie in.  keep: moved rows (taken as three a sequence)."""
     c = case
     if c["kind"] == "plan":
         T, S = sum(_news(c)), c["S"]
@@ -152,8 +151,7 @@ before it in the mean, and the branch's last one is any of the n)."""
         n = 1.0 * c["B"] * (c["H"] + c["KV"]) * c["N"] * c["d"]
         return {"bytes": 5 * n * e, "flops": 30 * n}
     if c["kind"] == "keep":
-        rows = sum(max(1.0, n / (c["bushy"] + 1)) for n in _news(c))
-        return {"bytes": 4.0 * rows * c["layers"] * c["KV"] * c["d"] * e, "flops": 0.0}
+        return {"bytes": 12.0 * c["S"] * c["layers"] * c["KV"] * c["d"] * e, "flops": 0.0}
     T = sum(_news(c))
     if c["kind"] == "append":
         return {"bytes": 2.0 * T * (c["H"] + 2 * c["KV"]) * c["d"] * e, "flops": 10.0 * T * (c["H"] + c["KV"]) * c["d"]}
