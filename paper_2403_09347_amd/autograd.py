@@ -18,7 +18,7 @@ def burst_attention(q, k_chunks, v_chunks, scale=None, causal=False, q_off=0, wi
     block_masks: one uint8 device tensor of block flags per chunk (see binding.params) with blocks
     of `block` rows / keys, or None for a chunk without flags; or None.
     turns, interleaved, amplitude: q and the keys are rotated by their global positions first (see rotary.burst_rotary).
-    norms, eps: a pair of weights [d], q's and the keys': their rows are normalised before that (see rotary.burst_norm_rotary); gradients
+    norms, eps: a pair of weights [d], q's and the keys' (None: 1 for every column): their rows are normalised before that (see rotary.burst_norm_rotary); gradients
     flow to the weights.
     Results are the same bits whenever a call is repeated; the order of the fp32 sums, and with it the last bits, depends on all
     sizes of a call, the number of heads among them.

@@ -375,12 +375,15 @@ class PagedWalk:
     positions (turns: see rotary.rotary_turns; None: not rotated), and the new tokens attend to their sequences.  k_pages, v_pages, and
     the table, lengths and starts of a step, and full_p: see the paged module.  Nothing is kept but the pages: a captured step reads
     its token tensors and the three arrays where they lie, and can be replayed with other contents.
-    norms, eps: weights [d] of queries and keys, which are normalised before the rotation (see rotary.burst_norm_rotary)."""
+    norms, eps: a pair of weights [d], the queries' and the keys' (None: 1 for every column): their rows are normalised before the rotation (see
+    rotary.burst_norm_rotary)."""
 
     def __init__(self, k_pages, v_pages, scale, turns=None, interleaved=False, amplitude=1.0, window=0, full_p=False, norms=None, eps=1e-6):
         self.k_pages, self.v_pages, self.scale, self.window, self.full_p = k_pages, v_pages, float(scale), int(window), bool(full_p)
         self.rotary = {} if turns is None else dict(turns=turns, interleaved=interleaved, amplitude=amplitude)
-        self.norms = {} if norms is None else dict(q_norm=norms[0], k_norm=norms[1], eps=eps)
+        # (for burst_cache_append no weight is no norm)
+        weights = [torch.ones(k_pages.shape[-1], device=k_pages.device) if w is None else w for w in norms or ()]
+        self.norms = {} if norms is None else dict(q_norm=weights[0], k_norm=weights[1], eps=eps)
 
     def step(self, q, k, v, table, lengths, starts, max_new=0, slots=None, positions=None, tree=None):
         """q [rows, H, d], k, v [rows, kv_heads, d]; returns (O, lse) of the new tokens.  slots, positions, tree: of paged.burst_cache_plan."""

@@ -25,7 +25,7 @@ def burst_cache_append(k, v, k_pages, v_pages, table, lengths, starts, q=None, t
     rotary.burst_rotary; None: not rotated); q [rows, H, d], if given, is rotated likewise and returned as a new tensor (rows behind the
     last sequence are not written).  offsets: int64 [sequences], added to the positions of the rotation (what of the
     sequence lies on the ring's other devices).  q_norm, k_norm [d] (of the pages' type or float32): q, k are normalised first, as
-    rotary.burst_norm_rotary does, with these weights and eps.  slots: int64 [rows], the places of the tokens' keys and values (row slots[i] %
+    rotary.burst_norm_rotary does, with these weights and eps (None: not normalised, which a norm without weights is not: that has ones).  slots: int64 [rows], the places of the tokens' keys and values (row slots[i] %
     page of page slots[i] // page, no two of them one place; negative or no page: left out) instead of those that the table says; positions: int64 [rows], the positions of the rotation
     instead of the places in the sequences (a tree's tokens have those of their depth; negative: the row is left out).  With both, the batch's three arrays
     are not read.  One launch; no gradient."""
