@@ -743,7 +743,8 @@ def burst_cache_plan(added, lengths, table, free_pages, free_count, page, starts
                   table=table.data_ptr(), table_stride=table.stride(0) if S > 1 else 0, free_pages=free_pages.data_ptr(), free_count=free_count.data_ptr(),
                   starts=starts.data_ptr(), totals=totals.data_ptr(), slots=slots.data_ptr(), positions=positions.data_ptr())
     if parents is not None:
-        p.words, p.most, p.tree, p.parents = tree.shape[1], parents.shape[1], tree.data_ptr(), parents.data_ptr()
+        # (an empty tensor has no address, and a block without one says that there are no trees; this one is not read)
+        p.words, p.most, p.tree, p.parents = tree.shape[1], parents.shape[1], tree.data_ptr(), parents.data_ptr() or starts.data_ptr()
         p.parents_stride = parents.stride(0) if S > 1 else 0
     _check(load().burst_cache_plan(ctypes.byref(p), _stream()), "burst_cache_plan")
 
