@@ -592,6 +592,11 @@ def burst_norm_rotate_bwd(tensors, weights, eps, r, workspace=None):
     _check(load().burst_norm_rotate_bwd(items, n, ws, k, eps, rp, d, dtype, _ptr(workspace), _bytes(workspace), _stream()), "burst_norm_rotate_bwd")
 
 
+def _rows_lie(t):
+    """Whether the rows of a matrix are contiguous, one behind the other (those of an empty one may have any strides)."""
+    return t.numel() == 0 or ((t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]))
+
+
 def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts, scale=1.0, causal=True, window=0, max_new=0, out_f32=False, full_p=False):
     """k_pages: [pages, kv_heads, page, d] (its strides go into the block; V_pages lies likewise); table [sequences, width], lengths
     [sequences], starts [sequences + 1]: int32 device tensors.  Token tensors are dense unless their strides are set in the block."""
@@ -599,8 +604,7 @@ def paged_params(q_rows, H, kv_heads, d, dtype, k_pages, table, lengths, starts,
     if any(t.dtype != torch.int32 for t in (table, lengths, starts)) or table.dim() != 2 or lengths.shape != table.shape[:1] or \
             starts.shape != (table.shape[0] + 1,):
         raise ValueError("table [sequences, width], lengths [sequences], starts [sequences + 1]: int32 tensors expected")
-    if not lengths.is_contiguous() or not starts.is_contiguous() or (table.shape[1] > 1 and table.stride(1) != 1) or \
-            (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
+    if not lengths.is_contiguous() or not starts.is_contiguous() or not _rows_lie(table):
         raise ValueError("lengths, starts and the table's rows: contiguous expected")
     if k_pages.dim() != 4 or tuple(k_pages.shape[1::2]) != (kv_heads, d) or (d > 1 and k_pages.stride(3) != 1):
         raise ValueError("k_pages: [pages, kv_heads, page, d] with a contiguous last dimension expected")
@@ -712,8 +716,7 @@ def burst_paged_tree_fwd(Q, k_pages, v_pages, O, lse, tree, p, workspace=None):
     """tree: int64 device tensor [rows, words] with contiguous rows (see burst.h)."""
     if lse.numel() < p.rows * p.H:
         raise ValueError("lse: [rows, H] expected")
-    if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != p.rows or (tree.shape[1] > 1 and tree.stride(1) != 1) or \
-            (p.rows > 1 and tree.stride(0) < tree.shape[1]):
+    if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != p.rows or not _rows_lie(tree):
         raise ValueError("tree: int64 [rows, words] with contiguous rows expected")
     _here(tree, "tree")
     _check(load().burst_paged_tree_fwd(_tokens(Q, p.H, p.q_strides, p, "Q"), _pages(k_pages, p, "k_pages"), _pages(v_pages, p, "v_pages"),
@@ -735,8 +738,7 @@ def burst_cache_plan(added, lengths, table, free_pages, free_count, page, starts
     for name, (t, shape) in shapes.items():
         if t.dtype != (torch.int64 if name in ("slots", "positions", "tree") else torch.int32) or tuple(t.shape) != shape:
             raise ValueError(f"{name}: {'int64' if name in ('slots', 'positions', 'tree') else 'int32'} tensor {list(shape)} expected")
-        rows_of_it = name in ("table", "parents")
-        if not (t.is_contiguous() if not rows_of_it else (shape[1] <= 1 or t.stride(1) == 1) and (shape[0] <= 1 or t.stride(0) >= shape[1])):
+        if not (_rows_lie(t) if name in ("table", "parents") else t.is_contiguous()):
             raise ValueError(f"{name}: contiguous expected")
         _here(t, name)
     p = BurstPlan(sequences=S, rows=rows, pages=free_pages.shape[0], page=page, width=table.shape[1], added=added.data_ptr(), lengths=lengths.data_ptr(),
@@ -756,7 +758,7 @@ def burst_cache_keep(pools, kept, counts, lengths_out, p):
         if t.dtype != torch.int32 or tuple(t.shape) != shape or (t.dim() == 1 and not t.is_contiguous()):
             raise ValueError(f"{what}: int32 tensor {list(shape)} expected")
         _here(t, what)
-    if (kept.shape[1] > 1 and kept.stride(1) != 1) or (p.sequences > 1 and kept.stride(0) < kept.shape[1]):
+    if not _rows_lie(kept):
         raise ValueError("kept: contiguous rows expected")
     at = (ctypes.c_void_p * len(pools))(*[_pages(t, p, "pools").value for t in pools])
     _check(load().burst_cache_keep(at, len(pools), ctypes.c_void_p(kept.data_ptr()), kept.stride(0) if p.sequences > 1 else 0, kept.shape[1],

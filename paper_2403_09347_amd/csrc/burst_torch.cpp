@@ -665,6 +665,8 @@ void set_token_strides(int64_t (&out)[2], const Tensor& t) {
   out[0] = t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
   out[1] = t.size(1) > 1 ? t.stride(1) : t.size(2);
 }
+// Whether the rows of a matrix can be handed on: contiguous, one behind the other (of an empty one they may have any strides).
+bool rows_lie(const Tensor& t) { return t.numel() == 0 || ((t.size(1) <= 1 || t.stride(1) == 1) && (t.size(0) <= 1 || t.stride(0) >= t.size(1))); }
 burst_paged_params describe_paged(const Tensor& k_pages, const Tensor& v_pages, const Tensor& table, const Tensor& lengths, const Tensor& starts) {
   TORCH_CHECK_VALUE(k_pages.dim() == 4 && k_pages.is_cuda() && (k_pages.scalar_type() == torch::kBFloat16 || k_pages.scalar_type() == torch::kFloat),
                     "k_pages: device tensor [pages, kv_heads, page, d] of bfloat16 or float32 expected");
@@ -681,8 +683,7 @@ burst_paged_params describe_paged(const Tensor& k_pages, const Tensor& v_pages, 
     TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == k_pages.device(), "table, lengths, starts: int32 tensors on the pages' device expected");
   TORCH_CHECK_VALUE(lengths.dim() == 1 && starts.dim() == 1 && starts.size(0) == lengths.size(0) + 1 && table.dim() == 2 && table.size(0) == lengths.size(0),
                     "table [sequences, width], lengths [sequences], starts [sequences + 1] expected");
-  TORCH_CHECK_VALUE(lengths.is_contiguous() && starts.is_contiguous() && (table.size(1) <= 1 || table.stride(1) == 1) &&
-                    (table.size(0) <= 1 || table.stride(0) >= table.size(1)), "lengths, starts and the table's rows: contiguous expected");
+  TORCH_CHECK_VALUE(lengths.is_contiguous() && starts.is_contiguous() && rows_lie(table), "lengths, starts and the table's rows: contiguous expected");
   burst_paged_params p{};
   p.sequences = (int32_t)lengths.size(0); p.kv_heads = (int32_t)k_pages.size(1); p.d = (int32_t)k_pages.size(3);
   p.dtype = k_pages.scalar_type() == torch::kBFloat16 ? BURST_BF16 : BURST_F32;
@@ -782,8 +783,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
   TORCH_CHECK_VALUE(max_new >= 0 && max_new <= 0x7fffffff && window >= 0, "max_new, window: not negative expected");
   if (tree.has_value()) {
     TORCH_CHECK_VALUE(tree->scalar_type() == torch::kLong && tree->device() == k_pages.device() && tree->dim() == 2 && tree->size(0) == q_in.size(0) &&
-                      tree->size(1) >= 1 && tree->size(1) <= 1 << 20 && (tree->size(1) == 1 || tree->stride(1) == 1) &&
-                      (tree->size(0) <= 1 || tree->stride(0) >= tree->size(1)), "tree: int64 [rows, words] on the pages' device, its rows contiguous, expected");
+                      tree->size(1) >= 1 && tree->size(1) <= 1 << 20 && rows_lie(*tree), "tree: int64 [rows, words] on the pages' device, its rows contiguous, expected");
     TORCH_CHECK_VALUE(causal, "tree: masks of a causal call expected");
   }
   const c10::DeviceGuard on(k_pages.device());
@@ -840,8 +840,7 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(con
     TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == table.device(), "new, lengths, table, free, count: int32 tensors on one device expected");
   TORCH_CHECK_VALUE(added.dim() == 1 && lengths.sizes() == added.sizes() && table.dim() == 2 && table.size(0) == added.size(0) && free_pages.dim() == 1 &&
                     free_count.numel() == 1, "new, lengths [sequences], table [sequences, width], free [pages], count [1] expected");
-  TORCH_CHECK_VALUE(added.is_contiguous() && lengths.is_contiguous() && free_pages.is_contiguous() && (table.size(1) <= 1 || table.stride(1) == 1) &&
-                    (table.size(0) <= 1 || table.stride(0) >= table.size(1)), "new, lengths, free and the table's rows: contiguous expected");
+  TORCH_CHECK_VALUE(added.is_contiguous() && lengths.is_contiguous() && free_pages.is_contiguous() && rows_lie(table), "new, lengths, free and the table's rows: contiguous expected");
   fits_int(table);
   fits_int(free_pages);
   TORCH_CHECK_VALUE(added.size(0) <= 4096 && rows >= 0 && rows < 1 << 20, "at most 4096 sequences and 2^20 - 1 rows expected");
@@ -851,8 +850,7 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(con
                                                                             "the table and the stack: memory of their own expected");
   TORCH_CHECK_VALUE(table.numel() == 0 || table.data_ptr() != free_pages.data_ptr(), "the table and the stack: memory of their own expected");
   if (parents.has_value()) {
-    TORCH_CHECK_VALUE(parents->scalar_type() == torch::kInt && parents->device() == table.device() && parents->dim() == 2 && parents->size(0) == added.size(0) &&
-                      (parents->size(1) <= 1 || parents->stride(1) == 1) && (parents->size(0) <= 1 || parents->stride(0) >= parents->size(1)),
+    TORCH_CHECK_VALUE(parents->scalar_type() == torch::kInt && parents->device() == table.device() && parents->dim() == 2 && parents->size(0) == added.size(0) && rows_lie(*parents),
                       "parents: int32 [sequences, most] on the table's device, its rows contiguous, expected");
     fits_int(*parents);
     TORCH_CHECK_VALUE(parents->numel() == 0 || (parents->data_ptr() != table.data_ptr() && parents->data_ptr() != free_pages.data_ptr()),
@@ -897,8 +895,7 @@ Tensor cache_keep(const std::vector<Tensor>& k_pages, const std::vector<Tensor>&
     }
   for (const Tensor* t : {&kept, &counts})
     TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == table.device(), "kept, counts: int32 tensors on the pages' device expected");
-  TORCH_CHECK_VALUE(kept.dim() == 2 && kept.size(0) == lengths.size(0) && counts.sizes() == lengths.sizes() && counts.is_contiguous() &&
-                    (kept.size(1) <= 1 || kept.stride(1) == 1) && (kept.size(0) <= 1 || kept.stride(0) >= kept.size(1)),
+  TORCH_CHECK_VALUE(kept.dim() == 2 && kept.size(0) == lengths.size(0) && counts.sizes() == lengths.sizes() && counts.is_contiguous() && rows_lie(kept),
                     "kept [sequences, most], its rows contiguous, counts [sequences] expected");
   fits_int(kept);
   const c10::DeviceGuard on(table.device());
