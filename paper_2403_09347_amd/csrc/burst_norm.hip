@@ -373,14 +373,14 @@ norm_bwd_kernel(NormArgs a) {
         for (int e = 0; e < E; e++) {
           const float p = (float)gu[k][e], q = (float)gv[k][e];
           h1[k][e] = p * cs[k][e] + q * sn[k][e];
-          h2[k][e] = q * cs[k][e] - p * sn[k][e];
+          h2[k][e] = s.turned[k] ? q * cs[k][e] - p * sn[k][e] : 0.f;   // (p may be infinite: sn = 0 does not keep it out)
         }
       } else {
 #pragma unroll
         for (int e = 0; e < P; e++) {
           const float p = (float)gu[k][2 * e], q = (float)gu[k][2 * e + 1];
-          h1[k][2 * e] = p * cs[k][e] + q * sn[k][e];
-          h1[k][2 * e + 1] = q * cs[k][e] - p * sn[k][e];
+          h1[k][2 * e] = s.turned[k] ? p * cs[k][e] + q * sn[k][e] : p;   // (as above)
+          h1[k][2 * e + 1] = s.turned[k] ? q * cs[k][e] - p * sn[k][e] : q;
         }
       }
     }
