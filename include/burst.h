@@ -334,7 +334,7 @@ typedef struct burst_norm_weight {
   int32_t f32;                       /* w and dw are fp32 whatever the dtype */
   int32_t reserved;                  /* 0 */
 } burst_norm_weight;
-/* n tensors with `weights` weights, each of one tensor or of several; r = NULL: not rotated.  eps > 0.  y is x itself (then with the same strides)
+/* n tensors with `weights` weights, each of one tensor or of several; r = NULL: not rotated.  eps >= 2^-126.  y is x itself (then with the same strides)
  * or memory that x does not share. */
 int burst_norm_rotate(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
                       int dtype, void* stream);
@@ -382,7 +382,7 @@ int burst_cache_append(const void* K, const void* V, void* K_pages, void* V_page
 typedef struct burst_store {
   const void* q_weight; const void* k_weight;   /* DEVICE [d]: Q, K are normalised first (see burst_norm_rotate); NULL: not */
   int32_t q_weight_f32, k_weight_f32;           /* these weights are fp32 whatever the dtype */
-  float   eps;                                  /* of the norms, > 0 if there are any */
+  float   eps;                                  /* of the norms, >= 2^-126 if there are any */
   int32_t reserved;                             /* 0 */
   const int64_t* slots;                         /* DEVICE [rows]: row i's key and value go to row slots[i] % page of page slots[i] / page, instead of by the
                                                  * table; negative, or in a page that is none: left out.  No two rows go to one place */

@@ -781,6 +781,12 @@ int plan_paged(const burst_paged_params* p, const Paged& g, PagedPlan& plan) {
 }
 
 // ---- rows normalised and rotated
+// Whether a norm can have this eps: a positive number of full precision.  (The roots of smaller ones, which rows of zeros take, are 0 on the device.)
+bool norm_eps(float eps) {
+  unsigned bits;
+  std::memcpy(&bits, &eps, sizeof(bits));
+  return bits - 0x00800000u < 0x7f000000u;         // 2^-126 up to the largest
+}
 // One item of a call that normalises rows, checked.  `some`: it has rows.
 int norm_item(const burst_norm_rows& t, const burst_norm_weight* w, int weights, const burst_rotary* r, int d, unsigned size, bool backward,
               burst::NormItem& it, bool& some) {
@@ -820,7 +826,7 @@ struct NormPlan {
 };
 int plan_norm(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d, int dtype,
               bool backward, NormPlan& plan) {
-  if (n < 0 || weights < 0 || d < 2 || d > 128 || !(eps > 0.f) || !std::isfinite(eps)) return BURST_ERR_SHAPE;
+  if (n < 0 || weights < 0 || d < 2 || d > 128 || !norm_eps(eps)) return BURST_ERR_SHAPE;
   if (dtype != BURST_BF16 && dtype != BURST_F32) return BURST_ERR_DTYPE;
   int st;
   if (r != nullptr && (st = check_rotary(r, d)) != BURST_OK) return st;
@@ -1403,7 +1409,7 @@ int burst_cache_store(const void* K, const void* V, void* K_pages, void* V_pages
   if (r != nullptr && (st = check_rotary(r, p->d)) != BURST_OK) return st;
   if (r != nullptr && r->inverse != 0) return BURST_ERR_SHAPE;
   const bool norms = how->q_weight != nullptr || how->k_weight != nullptr;
-  if (norms && (!(how->eps > 0.f) || !std::isfinite(how->eps))) return BURST_ERR_SHAPE;
+  if (norms && !norm_eps(how->eps)) return BURST_ERR_SHAPE;
   if (how->positions != nullptr && how->offsets != nullptr) return BURST_ERR_SHAPE;
   const bool told = how->slots != nullptr && how->positions != nullptr;   // the rows' places, all of them
   if (p->rows == 0 || (p->sequences == 0 && !told)) return BURST_OK;

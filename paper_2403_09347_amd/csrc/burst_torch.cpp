@@ -585,7 +585,7 @@ std::vector<Tensor> norm_rotate(const std::vector<Tensor>& xs, const std::vector
     refuse_tangent(x);
   }
   TORCH_CHECK_VALUE(xs[0].size(3) >= 2, "at least two columns expected");
-  TORCH_CHECK_VALUE(eps > 0 && std::isfinite((float)eps) && (float)eps > 0, "eps: positive expected");
+  TORCH_CHECK_VALUE(eps > 0 && std::isnormal((float)eps), "eps: positive, in fp32 2^-126 at least, expected");
   variable_list weights;
   for (const Tensor& w : weights_in) {
     check_weight(w, xs[0]);
@@ -719,7 +719,7 @@ std::optional<Tensor> cache_append(const Tensor& k_in, const Tensor& v_in, const
                       "q_norm, k_norm: [d] on the pages' device, of their type or float32, expected");
     refuse_tangent(*w);
     TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && w->requires_grad()), "q_norm, k_norm: the paged calls have no gradient (call them under torch.no_grad)");
-    TORCH_CHECK_VALUE(eps > 0 && std::isfinite((float)eps) && (float)eps > 0, "eps: positive expected");
+    TORCH_CHECK_VALUE(eps > 0 && std::isnormal((float)eps), "eps: positive, in fp32 2^-126 at least, expected");
     norms[i] = w->contiguous();
     (i ? how.k_weight : how.q_weight) = norms[i].data_ptr();
     (i ? how.k_weight_f32 : how.q_weight_f32) = w->scalar_type() == torch::kFloat;

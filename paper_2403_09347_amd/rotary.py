@@ -53,7 +53,7 @@ def burst_rotary(x, turns, offset=0, positions=None, interleaved=False, amplitud
 
 def burst_norm_rotary(x, weights, turns=None, eps=1e-6, offset=0, positions=None, interleaved=False, amplitude=1.0):
     """x: a [B, heads, rows, d] tensor or a list of them (bfloat16 or float32, d from 2 to 128), every row divided by the root of its mean square
-    (+ eps, positive), multiplied by the weights [d] (of x's type or float32; one tensor for all, or a list with an entry for each, None: 1), and rotated as
+    (+ eps, positive: 2^-126 at least), multiplied by the weights [d] (of x's type or float32; one tensor for all, or a list with an entry for each, None: 1), and rotated as
     burst_rotary does (turns, offset, positions, interleaved, amplitude: see there; turns=None: not rotated), out of place, by one launch (12
     tensors each).  All of it in 32 bits (the angles in 64), rounded once; sums of squares beyond 32 bits' range count as infinite.  Returns a
     tensor or a list; results lie in memory like x.  Gradients flow to x and to the weights, whose gradients are summed in fp32 over all rows of all
