@@ -422,13 +422,14 @@ typedef struct burst_plan {
   int32_t sequences, rows;           /* 0 .. 4096; 0 .. 2^20 - 1, of the token tensors */
   int32_t pages, page, width;        /* as in burst_paged_params */
   int32_t words, most;               /* of the masks; columns of parents */
-  int32_t reserved;                  /* 0 */
+  int32_t window;                    /* masks name the last so many tokens of a branch, the token itself among them: what a window of the attention leaves of it (0: all of it).  A
+                                      * token so deep sees no key before the new ones either, which that number of bits tells burst_paged_tree_fwd as well */
   const int32_t* added;              /* DEVICE [sequences]: new tokens; negative: the sequence has ended */
   const int32_t* lengths;            /* DEVICE [sequences]: tokens that are in the cache (cut to 0 .. 2^30) */
   int32_t* table; int64_t table_stride;   /* DEVICE [sequences][width], read and written; stride as in burst_paged_params */
   int32_t* free_pages; int32_t* free_count;   /* DEVICE [pages], [1]: the stack of pages that are free, its top at free_count - 1 (cut to 0 .. pages); read and written */
   const int32_t* parents; int64_t parents_stride;   /* DEVICE [sequences][most] (stride: 0 = most): the new token that each new token hangs on, one before it; negative, another, or not among
-                                      * the columns: none.  NULL: no trees */
+                                      * the columns: none.  NULL: no trees (with most = 0 any other address has them) */
   int32_t* starts; int32_t* totals;  /* written, DEVICE [sequences + 1], [sequences]: starts and lengths for the paged calls (a sequence that was passed over has no new tokens) */
   int64_t* slots; int64_t* positions;   /* written, DEVICE [rows]: see burst_store; -1 behind the last sequence.  Positions of trees: tokens before the new ones + depth */
   int64_t* tree;                     /* written if there are parents, DEVICE [rows][words]: see burst_paged_tree_fwd; 0 for chunks of more than 64 * words tokens, whose parents are

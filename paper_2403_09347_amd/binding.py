@@ -76,7 +76,7 @@ class BurstStore(ctypes.Structure):
 
 
 class BurstPlan(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "rows", "pages", "page", "width", "words", "most", "reserved")] + [
+    _fields_ = [(n, ctypes.c_int32) for n in ("sequences", "rows", "pages", "page", "width", "words", "most", "window")] + [
         ("added", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
         ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("parents", ctypes.c_void_p), ("parents_stride", ctypes.c_int64),
         ("starts", ctypes.c_void_p), ("totals", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("tree", ctypes.c_void_p)]
@@ -725,7 +725,7 @@ def burst_paged_tree_fwd(Q, k_pages, v_pages, O, lse, tree, p, workspace=None):
                                        ctypes.byref(p), _stream()), "burst_paged_tree_fwd")
 
 
-def burst_cache_plan(added, lengths, table, free_pages, free_count, page, starts, totals, slots, positions, parents=None, tree=None):
+def burst_cache_plan(added, lengths, table, free_pages, free_count, page, starts, totals, slots, positions, parents=None, tree=None, window=0):
     """int32 device tensors added, lengths, totals [sequences], table [sequences, width], free_pages [pages], free_count [1], starts [sequences + 1], parents
     [sequences, most] or None; int64 ones slots, positions [rows], tree [rows, words] or None (see burst.h)."""
     S, rows = added.shape[0], slots.shape[0]
@@ -747,7 +747,7 @@ def burst_cache_plan(added, lengths, table, free_pages, free_count, page, starts
     if parents is not None:
         # (an empty tensor has no address, and a block without one says that there are no trees; this one is not read)
         p.words, p.most, p.tree, p.parents = tree.shape[1], parents.shape[1], tree.data_ptr(), parents.data_ptr() or starts.data_ptr()
-        p.parents_stride = parents.stride(0) if S > 1 else 0
+        p.parents_stride, p.window = parents.stride(0) if S > 1 else 0, window
     _check(load().burst_cache_plan(ctypes.byref(p), _stream()), "burst_cache_plan")
 
 

@@ -1451,7 +1451,7 @@ int burst_cache_store(const void* K, const void* V, void* K_pages, void* V_pages
 int burst_cache_plan(const burst_plan* p, void* stream) {
   if (p == nullptr) return BURST_ERR_NULL;
   if (p->sequences < 0 || p->sequences > burst::kPlanSequences || p->rows < 0 || p->rows > burst::kPlanMostRows || p->pages < 0 || p->width < 0 ||
-      p->most < 0 || p->words < 0 || p->words > 1 << 20) return BURST_ERR_SHAPE;
+      p->most < 0 || p->words < 0 || p->words > 1 << 20 || p->window < 0) return BURST_ERR_SHAPE;
   if (p->page < 16 || (p->page & (p->page - 1)) != 0 || (long long)p->width * p->page >= 1LL << 30) return BURST_ERR_SHAPE;
   if ((p->table_stride != 0 && p->table_stride < p->width) || (p->parents_stride != 0 && p->parents_stride < p->most)) return BURST_ERR_SHAPE;
   if (p->parents != nullptr && p->words < 1) return BURST_ERR_SHAPE;
@@ -1474,6 +1474,7 @@ int burst_cache_plan(const burst_plan* p, void* stream) {
   a.table_stride = p->table_stride != 0 ? p->table_stride : p->width; a.parents_stride = p->parents_stride != 0 ? p->parents_stride : p->most;
   a.sequences = p->sequences; a.rows = p->rows; a.pages = p->pages; a.page_shift = __builtin_ctz((unsigned)p->page); a.width = p->width;
   a.words = p->parents != nullptr ? p->words : 0; a.most = p->most;
+  a.window = p->window > 0 ? p->window : 0x7fffffff;
   return burst::launch_plan(a, (hipStream_t)stream);
 }
 
@@ -1611,6 +1612,6 @@ const char* burst_strerror(int status) {
   }
 }
 
-int burst_version(void) { return 116; }
+int burst_version(void) { return 117; }
 
 }  // extern "C"

@@ -15,6 +15,7 @@ struct PlanArgs {
   int* starts; int* totals; long long* slots; long long* positions; unsigned long long* tree;
   long long table_stride, parents_stride;
   int sequences, rows, pages, page_shift, width, words, most;
+  int window;                                      // tokens of a branch that a mask names, at most
 };
 int launch_plan(const PlanArgs& a, hipStream_t s);
 

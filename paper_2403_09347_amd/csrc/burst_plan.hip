@@ -53,7 +53,7 @@ __device__ __forceinline__ void fill_row(const PlanArgs& a, int row, const int* 
           mask[word] = bits;
           bits = 0;
         }
-        bits |= 1ull << (at & 63);
+        if (depth + 1 < a.window) bits |= 1ull << (at & 63);
         const int up = at < a.most ? parents[at] : -1;
         at = up < at ? up : -1;                    // (negative: a root; one that is not before the token is taken for none)
       }
@@ -66,6 +66,14 @@ __device__ __forceinline__ void fill_row(const PlanArgs& a, int row, const int* 
   if (mask != nullptr)
     for (; word >= 0; word--) mask[word] = 0;
   a.positions[row] = pos;
+}
+// The highest n of the bits that are set (n >= 1): those from the highest b on above which so many are.
+__device__ __forceinline__ unsigned long long highest_bits(unsigned long long x, int n) {
+  int b = 0;
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1)
+    if (__builtin_popcountll(x >> (b + step)) >= n) b += step;
+  return x >> b << b;
 }
 // Positions and masks of a tree of n <= 64 tokens, by a wavefront: every token takes over what the token that it has come to sees, and goes on to where that one
 // has come to, twice as far each time.  (Going up branch by branch, a load each step, the rows of 400 sequences took 12.8 us; so 6.3, of which the rest is rows of chunks.)
@@ -84,7 +92,8 @@ __device__ __forceinline__ void fill_tree(const PlanArgs& a, int s, int first, i
   const size_t row = (size_t)first + t;
   a.positions[row] = base + __builtin_popcount(lo) + __builtin_popcount(hi) - 1;
   unsigned long long* const mask = a.tree + row * a.words;
-  mask[0] = (unsigned long long)hi << 32 | lo;
+  const unsigned long long branch = (unsigned long long)hi << 32 | lo;
+  mask[0] = a.window < 64 ? highest_bits(branch, a.window) : branch;
   for (int w = 1; w < a.words; w++) mask[w] = 0;
 }
 

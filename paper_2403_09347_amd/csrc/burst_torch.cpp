@@ -834,7 +834,7 @@ std::tuple<Tensor, Tensor> paged_attention(const Tensor& q_in, const Tensor& k_p
 
 std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(const Tensor& added, const Tensor& lengths, const Tensor& table, const Tensor& free_pages,
                                                                              const Tensor& free_count, int64_t page, int64_t rows,
-                                                                             const std::optional<Tensor>& parents, int64_t words) {
+                                                                             const std::optional<Tensor>& parents, int64_t words, int64_t window) {
   TORCH_CHECK_VALUE(table.is_cuda(), "table: device tensor expected");
   for (const Tensor* t : {&added, &lengths, &table, &free_pages, &free_count})
     TORCH_CHECK_VALUE(t->scalar_type() == torch::kInt && t->device() == table.device(), "new, lengths, table, free, count: int32 tensors on one device expected");
@@ -856,6 +856,7 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(con
     TORCH_CHECK_VALUE(parents->numel() == 0 || (parents->data_ptr() != table.data_ptr() && parents->data_ptr() != free_pages.data_ptr()),
                       "the table and the stack: memory of their own expected");
     TORCH_CHECK_VALUE(words >= 1 && words <= 1 << 20, "words: at least one expected");
+    TORCH_CHECK_VALUE(window >= 0, "window: not negative expected");
   }
   const c10::DeviceGuard on(table.device());
   const auto i32 = table.options(), i64 = i32.dtype(torch::kLong);
@@ -869,7 +870,7 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, std::optional<Tensor>> cache_plan(con
   p.starts = starts.data_ptr<int>(); p.totals = totals.data_ptr<int>(); p.slots = slots.data_ptr<int64_t>(); p.positions = positions.data_ptr<int64_t>();
   if (parents.has_value()) {
     tree = torch::empty({rows, words}, i64);
-    p.words = (int32_t)words; p.most = (int32_t)parents->size(1); p.tree = tree->data_ptr<int64_t>();
+    p.words = (int32_t)words; p.window = (int32_t)std::min<int64_t>(window, 0x7fffffff); p.most = (int32_t)parents->size(1); p.tree = tree->data_ptr<int64_t>();
     p.parents_stride = parents->size(0) > 1 ? parents->stride(0) : 0;
     static const int none = -1;                    // (not read: no columns, or no sequences)
     p.parents = parents->numel() > 0 ? parents->data_ptr<int>() : &none;

@@ -393,7 +393,11 @@ class PagedWalk:
                                      window=self.window, max_new=max_new, full_p=self.full_p, tree=tree)
 
     def planned_step(self, q, k, v, table, plan, max_new=0):
-        """A step with a plan of paged.burst_cache_plan."""
+        """A step with a plan of paged.burst_cache_plan, whose masks, if it has some, are for this walk's window (or for branches that are shorter).  max_new: the
+        most new tokens of a sequence, where it is known: token tensors with rows behind the last sequence, as captured steps have, do not tell that all of
+        them have one or few, which other kernels take (see paged.burst_paged_attention)."""
+        if not plan.masks_for(self.window):
+            raise ValueError(f"a plan with masks for a window of {plan.window}, and a walk with one of {self.window}: burst_cache_plan(window={self.window}) expected")
         return self.step(q, k, v, table, plan.lengths, plan.starts, max_new, plan.slots, plan.positions, plan.tree)
 
 

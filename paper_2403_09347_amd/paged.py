@@ -47,7 +47,7 @@ def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=Non
     of longer chunks rounds them to 8 at d = 64 and d = 128, as the walks do.
     tree: int64 [rows, words], the masks of drafted tokens: new token t of a sequence sees all keys before the sequence's new tokens, and new token j if bit
     j % 64 of word j // 64 of its row is set (its own among them).  A window then counts back from the first new token's position + the token's
-    depth (bits - 1) among the keys before; the mask alone says which new tokens are seen.  Sequences with more than 64 * words new tokens are chunks of
+    depth (bits - 1) among the keys before; the mask alone says which new tokens are seen (masks of a burst_cache_plan with the same window: those in it).  Sequences with more than 64 * words new tokens are chunks of
     prompts, as without masks.  No gradient."""
     scale = float(scale) if scale is not None else q.shape[-1] ** -0.5
     try:
@@ -57,9 +57,7 @@ def burst_paged_attention(q, k_pages, v_pages, table, lengths, starts, scale=Non
         raise B.from_native(e) from None
 
 
-class CachePlan(NamedTuple):
-    """What a step's calls read: starts [sequences + 1] and lengths [sequences] (int32; lengths with the new tokens), slots and positions [rows] (int64) of
-    burst_cache_append, and tree [rows, words] (int64; None without parents) of burst_paged_attention."""
+class _Arrays(NamedTuple):
     starts: torch.Tensor
     lengths: torch.Tensor
     slots: torch.Tensor
@@ -67,7 +65,21 @@ class CachePlan(NamedTuple):
     tree: Optional[torch.Tensor]
 
 
-def burst_cache_plan(new, lengths, table, free, count, page, rows, parents=None, words=1):
+class CachePlan(_Arrays):
+    """What a step's calls read: starts [sequences + 1] and lengths [sequences] (int32; lengths with the new tokens), slots and positions [rows] (int64) of
+    burst_cache_append, and tree [rows, words] (int64; None without parents) of burst_paged_attention.
+    Beside the arrays: window, which the masks are made for (0: none), and longest, the most tokens that a branch can have (None: as many as bits)."""
+    window, longest = 0, None
+
+    def masks_for(self, window):
+        """Whether the masks are those of attention with this window."""
+        if self.tree is None:
+            return True
+        longest = self.longest or 64 * self.tree.shape[1]
+        return min(self.window or longest, longest) == min(window or longest, longest)
+
+
+def burst_cache_plan(new, lengths, table, free, count, page, rows, parents=None, words=1, window=0):
     """Plans a step on the device, from int32 tensors: new [sequences], the new tokens of each (negative: the sequence has ended), lengths [sequences], the tokens
     that each has in the cache, table [sequences, width] (-1: no page; a page is one entry's, or the stack's), free [pages] and count [1], a stack of the pages that are free, its top at
     count - 1.  rows: of the step's token tensors (up to 2^20 - 1; at most 4096 sequences).
@@ -75,12 +87,16 @@ def burst_cache_plan(new, lengths, table, free, count, page, rows, parents=None,
     lacks more pages than are free, is passed over (it has no new tokens in starts).  Entries of the table in which new tokens lie get a page where they
     have none; ended sequences give theirs back first.  table, free and count are written; the same call again changes nothing.
     parents: int32 [sequences, most], the new token (one before it) that each new token hangs on, -1: none; then the plan has the trees' masks of 64 * words bits,
-    and positions go by depth; sequences with more new tokens than that are chunks of prompts.  Returns a CachePlan; rows behind the last
+    and positions go by depth; sequences with more new tokens than that are chunks of prompts.  window: of the attention that the masks are for, which sees that much of a branch (0: all of
+    it; layers with other windows have a plan of their own, made by the same call again).  Returns a CachePlan; rows behind the last
     sequence have slot and position -1.  One launch, two of more than 2048 rows."""
     try:
-        return CachePlan(*B.load_torch_module().cache_plan(new, lengths, table, free, count, int(page), int(rows), parents, int(words)))
+        plan = CachePlan(*B.load_torch_module().cache_plan(new, lengths, table, free, count, int(page), int(rows), parents, int(words), int(window)))
     except RuntimeError as e:
         raise B.from_native(e) from None
+    if parents is not None:
+        plan.window, plan.longest = int(window), max(1, min(64 * int(words), parents.shape[1], int(rows)))
+    return plan
 
 
 def burst_cache_keep(k_pages, v_pages, table, lengths, starts, kept, counts):
