@@ -23,7 +23,8 @@ def burst_attention(q, k_chunks, v_chunks, scale=None, causal=False, q_off=0, wi
     Results are the same bits whenever a call is repeated; the order of the fp32 sums, and with it the last bits, depends on all
     sizes of a call, the number of heads among them.
     The node saves its inputs, O and lse as torch's own operations do: a tensor changed in place before the backward is
-    an error, and a second backward needs retain_graph."""
+    an error, and a second backward needs retain_graph; so is a captured backward pass to tensors that an earlier graph, made on the default stream,
+    still holds."""
     if isinstance(k_chunks, torch.Tensor):
         k_chunks, v_chunks = [k_chunks], [v_chunks]
     assert len(k_chunks) == len(v_chunks) and len(k_chunks) > 0

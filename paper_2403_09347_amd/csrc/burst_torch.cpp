@@ -107,6 +107,21 @@ void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 size_t bytes(const Tensor& t) { return t.defined() ? (size_t)t.nbytes() : 0; }
 void* stream_of(const Tensor& t) { return (void*)c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
 
+// Gradients of a captured pass go to nodes of their own streams.  A leaf whose node was made by an earlier graph on the default stream, and lives because
+// that graph does, has the engine make that stream wait for the captured one, which no capture allows and the process may not survive.  (On the
+// device's guard.)
+void refuse_outside_of_capture(const torch::autograd::Node& node, const char* what) {
+  if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
+  for (size_t i = 0; i < node.num_outputs(); i++) {
+    const auto& to = node.next_edge(i).function;
+    if (to == nullptr || !node.task_should_compute_output(i)) continue;
+    const auto stream = to->stream();
+    TORCH_CHECK(!stream.has_value() || stream->id() != c10::hip::getDefaultHIPStream(stream->device_index()).id(), what,
+                ": a captured backward pass whose gradients go to a graph that was made on the default stream and still lives (let it go before the capture, or "
+                "make its tensors' graph in it)");
+  }
+}
+
 class Attention : public torch::autograd::Function<Attention> {
  public:
   // kvm: the keys of n chunks, then their values, then the block flags of those that have some (mask_of)
@@ -145,6 +160,7 @@ class Attention : public torch::autograd::Function<Attention> {
     variable_list out(1 + (s.size() - 3) + 7);    // q, kvm, and seven arguments that are no tensors
     if (!grads[0].defined()) return out;
     const c10::DeviceGuard on(s[0].device());
+    if (const auto node = torch::autograd::get_current_node()) refuse_outside_of_capture(*node, "burst_attention");
     // Hooks on saved tensors may have returned each of them in another layout than it was saved in.
     const Tensor q = addressable(s[0]) ? s[0] : s[0].contiguous(), O = lying_like(s[1], q), lse = s[2].contiguous();
     variable_list ks(s.begin() + 3, s.begin() + 3 + n), vs(s.begin() + 3 + n, s.begin() + 3 + 2 * n), masks(s.begin() + 3 + 2 * n, s.end());
@@ -364,6 +380,8 @@ struct RotateBackward : public torch::autograd::Node {
       back.offsets.push_back(how.offsets[i]);
     }
     if (some.empty()) return out;
+    const c10::DeviceGuard on(some[0].device());
+    refuse_outside_of_capture(*this, "burst_rotary");
     const Tensor t = turns.unpack().contiguous();  // (hooks on saved tensors may return them in another layout than they were saved in)
     check_turns(t, some[0].size(3), some[0]);
     const variable_list g = rotate_differentiably(some, t, where, back);   // (create_graph: a rotation again)
@@ -499,7 +517,7 @@ struct NormRotaryBackward : public torch::autograd::Node {
     }
     if (like == nullptr) return out;
     const c10::DeviceGuard on(like->device());
-    refuse_outside_of_capture();
+    refuse_outside_of_capture(*this, "burst_norm_rotary");
     Tensor t;
     variable_list given(x);                        // (as they are part of a graph)
     given.insert(given.end(), g.begin(), g.end());
@@ -550,19 +568,6 @@ struct NormRotaryBackward : public torch::autograd::Node {
       for (Tensor& v : out) if (v.defined()) torch::autograd::set_history(v, end);
     }
     return out;
-  }
-  // Gradients of a captured pass go to nodes of their own streams.  A leaf whose node was made by an earlier graph on the default stream, and lives because
-  // that graph does, has the engine make that stream wait for the captured one, which no capture allows and the process may not survive.
-  void refuse_outside_of_capture() const {
-    if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
-    for (size_t i = 0; i < num_outputs(); i++) {
-      const auto& to = next_edge(i).function;
-      if (to == nullptr || !task_should_compute_output(i)) continue;
-      const auto stream = to->stream();
-      TORCH_CHECK(!stream.has_value() || stream->id() != c10::hip::getDefaultHIPStream(stream->device_index()).id(),
-                  "burst_norm_rotary: a captured backward pass whose gradients go to a graph that was made on the default stream and still lives (let it go "
-                  "before the capture, or make its tensors' graph in it)");
-    }
   }
   void release_variables() override {
     const std::lock_guard<std::mutex> lock(mutex_);

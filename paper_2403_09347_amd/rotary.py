@@ -39,7 +39,8 @@ def burst_rotary(x, turns, offset=0, positions=None, interleaved=False, amplitud
     returns a tensor or a list.  Row n is at position offset + n, or offset + positions[n] (positions: int64 [rows] or
     [B, rows]); offset and positions: one for all tensors, or a list.  turns: see rotary_turns; columns from 2 len(turns) on are copied.
     interleaved: columns 2 i and 2 i + 1 are a pair instead of i and i + len(turns).  Results lie in memory like x; views with
-    a contiguous last dimension are read in place.  Gradients flow to x, rounded to its type."""
+    a contiguous last dimension are read in place.  Gradients flow to x, rounded to its type; a captured backward pass to
+    tensors that an earlier graph, made on the default stream, still holds is an error."""
     one = isinstance(x, torch.Tensor)
     xs = [x] if one else list(x)
     offsets = [int(o) for o in offset] if isinstance(offset, (list, tuple)) else [int(offset)] * len(xs)
