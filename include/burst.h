@@ -338,8 +338,8 @@ typedef struct burst_norm_weight {
  * or memory that x does not share. */
 int burst_norm_rotate(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
                       int dtype, void* stream);
-/* Gradients of all of them, those of a weight summed over every row of all its tensors (in fp32, in an order that follows from the sizes of the call; rounded
- * once).  r as in the forward call (r->inverse = 0).  workspace: burst_norm_workspace_bytes of the same arguments, 16-byte aligned; none is needed where no
+/* Gradients of all of them, those of a weight summed over every row of all its tensors (in fp32, in an order that follows from the sizes, strides and alignments
+ * of the call; rounded once).  r as in the forward call (r->inverse = 0).  workspace: burst_norm_workspace_bytes of the same arguments, 16-byte aligned; none is needed where no
  * weight's gradient is wanted. */
 int burst_norm_rotate_bwd(const burst_norm_rows* tensors, int n, const burst_norm_weight* w, int weights, float eps, const burst_rotary* r, int d,
                           int dtype, void* workspace, size_t workspace_bytes, void* stream);

@@ -4,8 +4,8 @@
 //   h = R^T g;  dw = sum over the rows of h x r;  u = h w;  dx = r (u - x r^2 (sum of u x) / d)
 // All of it in 32 bits (angles in 64), rounded once; sums over a row by the lanes that hold it, in a fixed order.
 // Bound by HBM: the forward reads and writes every row once, the backward reads x and g and writes dx; r is computed again, which costs
-// nothing beside x, which the gradient needs anyway.  Measured, d = 128, bf16: 40 heads of 8192 rows forward 40 us, 4.2 TB/s, backward 66 us with its
-// sums, 3.8 TB/s (a device copy moves 5.1); fp32, 20 heads of 4096 rows, 20 and 36 us.  Where the loads of all workgroups and their stores take turns
+// nothing beside x, which the gradient needs anyway.  Measured, d = 128, bf16: 40 heads of 8192 rows forward 44 us, 3.8 TB/s, backward 56 us and its sums
+// 4, 4.2 TB/s (a device copy moves 5.1); fp32, 20 heads of 4096 rows, 19, 30 and 4 us.  Where the loads of all workgroups and their stores take turns
 // (5 a CU do these sizes in one or two rounds) nothing overlaps the arithmetic, 8 us of the first of these.
 #include <type_traits>
 
@@ -493,8 +493,10 @@ long long set_tiles(NormArgs& a, int dtype, bool backward) {
   const int E = a.granule;
   double all = 0;                                  // rows x heads
   for (int i = 0; i < a.n; i++) all += (double)a.it[i].B * a.it[i].rows * a.it[i].heads;
-  // Heads of a thread: four where there is enough to fill the chip (us forward, 40 heads of 4096 rows: one 21.5, four 20.7; of fewer rows one, which leaves
-  // no CU idle).  The backward takes one, with the next tile's on their way (four of them: 44 instead of 40).
+  // Heads of a thread: four where there are many rows, one, which leaves no CU idle, elsewhere.  us forward, bf16, 32 + 8 heads, one / four: d = 128, in all
+  // 16384 rows 5.5 / 7.3, 32768 6.8 / 8.2, 65536 10.7 / 12.2, 131072 16.4 / 16.1, 262144 30.6 / 28.0; d = 64, 32768 5.5 / 7.3, 131072 11.0 / 11.8, 262144 16.2 /
+  // 15.7; so one would serve up to about 100 thousand rows, d = 128, and 200 thousand, d = 64, better, by up to 1.8 us.  The backward takes one,
+  // with the next tile's on their way (four of them: 44 instead of 40).
   a.heads_each = !backward && all >= 32768 ? 4 : 1;
   long long blocks = 0;
   auto lay = [&](int tiles_each) {

@@ -1,7 +1,8 @@
 // The books of a paged cache: what the calls of a step read, made from the lengths of its sequences (burst_cache_plan), and the rows of
 // drafted tokens that are kept, moved together (burst_cache_keep).
-// Bound by latency: nearly nothing is read, but one thing tells where the next one is.  Measured: a plan of 256 single tokens 5.2 us, of 400 sequences with
-// trees and prompts, 128 thousand rows, 10 + 4 (20 when every page is new); the kept rows of 96 trees in 24 layers, 8 heads, 37 us.
+// Bound by latency: nearly nothing is read, but one thing tells where the next one is.  Measured: a plan of 256 single tokens, a few of which start a
+// page, 7.2 us (again, with nothing to give, 5.1), of 400 sequences with trees and prompts, 20 of them ended, 87 thousand rows, 20.6 + 4 (again 10.8 + 4); where pages
+// or rows do not suffice 33 and 73 + 5; the kept rows of 96 trees in 24 layers, 8 heads, 37 us.
 #include "burst_paged_kernels.h"
 #include "burst_plan.h"
 
@@ -232,7 +233,9 @@ plan_kernel(PlanArgs a) {
         need += all;
       }
     if (((unsigned)rows <= (unsigned)a.rows && need <= left) || round == 1) break;
-    // Not enough: one sequence after the other, those that do not fit are passed over.  (start, flat: rows and pages that each needs.)
+    // Not enough: one sequence after the other, those that do not fit are passed over.  (start, flat: rows and pages that each needs.)  A thread reads all of a
+    // sequence's entries, and one goes through all sequences: 8 sequences of 8000 new tokens 19 us (8.6 where there are pages for all), 256 single tokens 33 (7.2),
+    // 400 with trees and prompts 73 (20.6), 4096 of two tokens 557 (18).
     __syncthreads();
     for (int s = tid; s < S; s += kPlanThreads) {
       int before, e, pages = 0;
@@ -291,7 +294,7 @@ plan_kernel(PlanArgs a) {
 }
 
 // The rows of a call of many, and behind them the trees.
-constexpr int kFillRows = 256;                     // of a workgroup: one a thread (128 thousand rows: four a thread 16.7 us a call, two 14.6, so 13.7)
+constexpr int kFillRows = 256;                     // of a workgroup: one a thread (87 thousand rows: four a thread 16.7 us a call, two 14.6, so 13.7)
 __global__ void __launch_bounds__(kFillRows)
 plan_rows_kernel(PlanArgs a, int row_blocks) {
   if ((int)blockIdx.x >= row_blocks) {             // a sequence a wavefront
